@@ -15,16 +15,8 @@
 #include <vector>
 
 #include "c3c.h"
+#include "c3c_ctx.h"
 #include "c3c_internal.h"
-
-struct c3c_ctx {
-  uint32_t mode = 0;
-  c3c_counters ctr{};
-  std::vector<c3c_sig_count> shapes;
-  std::string last_error;
-  void* ws = nullptr;      // caller's split-K workspace (device memory)
-  size_t ws_bytes = 0;
-};
 
 namespace c3c {
 namespace {
@@ -148,17 +140,6 @@ int decide(const Geo& g, uint32_t mode) {
   if (d.Kt < 2 && !spatial_3x3(d)) return C3C_REASON_KT1;
   if (!spatial_3x3(d) && !spatial_1x1(d)) return C3C_REASON_SPATIAL;
   return C3C_REASON_NONE;
-}
-
-bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes) {
-  if (!a || !b || abytes <= 0 || bbytes <= 0) return false;
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-  return a0 < b0 + static_cast<uintptr_t>(bbytes) && b0 < a0 + static_cast<uintptr_t>(abytes);
-}
-
-int fail(c3c_ctx* ctx, int status, const std::string& msg) {
-  if (ctx) ctx->last_error = msg;
-  return status;
 }
 
 void record_shape(c3c_ctx* ctx, int reason, const c3c_conv_desc& d) {

@@ -1,0 +1,84 @@
+// Device helpers of the token operators' kernels: element types, 16-byte
+// access at any alignment, reductions over a wave.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace c3c {
+
+typedef float tok_f32x4 __attribute__((ext_vector_type(4)));
+typedef float tok_f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t tok_u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t tok_u32x2 __attribute__((ext_vector_type(2)));
+typedef int32_t tok_i32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 tok_bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 tok_bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 tok_f16x2 __attribute__((ext_vector_type(2)));
+
+// element types by their storage: widen() is exact, narrow() rounds to
+// nearest even
+struct ElemBf16 {
+  typedef uint16_t store;
+  static constexpr int VEC = 8;  // elements of a 16-byte access
+  __device__ static float widen(store v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+  __device__ static store narrow(float f) {
+    return static_cast<store>(
+        __builtin_bit_cast(uint32_t, __builtin_convertvector((tok_f32x2{f, 0.f}), tok_bf16x2)));
+  }
+};
+struct ElemF16 {
+  typedef uint16_t store;
+  static constexpr int VEC = 8;
+  __device__ static float widen(store v) { return static_cast<float>(__builtin_bit_cast(_Float16, v)); }
+  __device__ static store narrow(float f) { return __builtin_bit_cast(store, static_cast<_Float16>(f)); }
+};
+struct ElemF32 {
+  typedef float store;
+  static constexpr int VEC = 4;
+  __device__ static float widen(store v) { return v; }
+  __device__ static store narrow(float f) { return f; }
+};
+
+// VEC elements from p (any alignment of the element's size), of which the
+// first m exist; the others are 0
+template <class E>
+__device__ inline void load_vec(const typename E::store* p, int m, float (&f)[E::VEC]) {
+  typename E::store v[E::VEC];
+  if (m >= E::VEC) {
+    __builtin_memcpy(v, p, 16);
+#pragma unroll
+    for (int e = 0; e < E::VEC; ++e) f[e] = E::widen(v[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E::VEC; ++e) f[e] = e < m ? E::widen(p[e]) : 0.f;
+  }
+}
+
+template <class E>
+__device__ inline void store_vec(typename E::store* p, int m, const float (&f)[E::VEC]) {
+  typename E::store v[E::VEC];
+#pragma unroll
+  for (int e = 0; e < E::VEC; ++e) v[e] = E::narrow(f[e]);
+  if (m >= E::VEC) {
+    __builtin_memcpy(p, v, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E::VEC - 1; ++e)
+      if (e < m) p[e] = v[e];
+  }
+}
+
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+__device__ inline float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+
+}  // namespace c3c

@@ -1,0 +1,130 @@
+"""The 8-bit matrix product against exact integer sums in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_31938_amd import c3c, tokens
+import token_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def context(M, N, K, xd, yd):
+    ctx = c3c.Context()
+    n = tokens.linear_i8_workspace_bytes(M, N, K, xd, yd)
+    if n:
+        ctx.set_workspace(torch.empty(n, dtype=torch.uint8, device="cuda"))
+    return ctx
+
+
+def weights(N, K, seed=3):
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randint(-127, 128, (N, K), generator=g, dtype=torch.int8).cuda()
+    return w, 0.01 + 0.02 * torch.rand(N, generator=g).cuda(), torch.randn(N, generator=g).cuda()
+
+
+def check(y, q, s, w, ws, bias, dtype):
+    """Integer sums exact; their conversion, two products and a sum in fp32,
+    then the output's rounding."""
+    acc = q.astype(np.float64) @ w.cpu().numpy().astype(np.float64).T
+    z = acc * s.astype(np.float64)[:, None] * ref.f64(ws)
+    r = z if bias is None else z + ref.f64(bias)
+    size = np.abs(z) + (0 if bias is None else np.abs(ref.f64(bias)))
+    ref.assert_within(y, r, ref.UNIT[dtype] * np.abs(r) + 4 * ref.EPS32 * size + ref.TINY[dtype])
+
+
+SHAPES = [(1, 1, 1), (1, 64, 128), (1, 4096, 512), (2, 33, 1000), (16, 40, 4096), (17, 100, 160), (33, 65, 100),
+          (64, 257, 513), (65, 64, 128), (65, 129, 2048), (100, 300, 1111), (128, 128, 16), (200, 77, 4000),
+          (333, 777, 1111), (300, 1000, 640), (1000, 1024, 272), (2049, 2049, 400)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_float_activations(dtype, M, N, K):
+    x = ref.randn(5, M, K).to(ref.TORCH[dtype])
+    w, ws, bias = weights(N, K)
+    y = tokens.linear_i8(context(M, N, K, dtype, dtype), x, w, ws, bias)
+    q, s = ref.quantize(x)
+    check(y, q, s, w, ws, bias, dtype)
+
+
+@pytest.mark.parametrize("yd", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("M,N,K,ld", [(1, 48, 100, 100), (5, 48, 96, 112), (70, 130, 96, 112), (70, 130, 97, 99),
+                                      (600, 515, 1024, 1024), (5000, 5000, 128, 128)])
+def test_8_bit_activations(yd, M, N, K, ld):
+    """Codes as they come, rows strided; and -128, which quantize_rows never makes."""
+    g = torch.Generator().manual_seed(9)
+    x = torch.randint(-128, 128, (M, ld), generator=g, dtype=torch.int8).cuda()[:, :K]
+    s = 0.01 + torch.rand(M, generator=g).cuda()
+    w, ws, _ = weights(N, K)
+    y = tokens.linear_i8(context(M, N, K, "i8", yd), x, w, ws, x_scale=s, out_dtype=yd)
+    check(y, x.cpu().numpy(), s.cpu().numpy(), w, ws, None, yd)
+
+
+@pytest.mark.parametrize("M", [1, 16, 200])
+def test_largest_sums(M):
+    """K at its limit with the largest codes: the int32 sum does not overflow."""
+    K, N = 131071, 20
+    x = torch.full((M, K), -128, dtype=torch.int8, device="cuda")
+    w = torch.full((N, K), -128, dtype=torch.int8, device="cuda")
+    one = torch.ones(N, device="cuda")
+    y = tokens.linear_i8(context(M, N, K, "i8", "f32"), x, w, one, x_scale=torch.ones(M, device="cuda"), out_dtype="f32")
+    assert (y == float(np.float32(128 * 128 * K))).all()
+
+
+def test_split_and_unsplit_give_the_same_bits():
+    M, N, K = 100, 300, 9000
+    x = ref.randn(5, M, K).to(torch.bfloat16)
+    w, ws, bias = weights(N, K)
+    full = tokens.linear_i8_workspace_bytes(M, N, K)
+    rows = tokens.linear_i8_workspace_bytes(1, N, K)
+    assert full > M * K + rows, "the call does not split"
+    want = tokens.linear_i8(context(M, N, K, "bf16", "bf16"), x, w, ws, bias)
+    ctx = c3c.Context()
+    ctx.set_workspace(torch.empty(M * 9008 + 2048, dtype=torch.uint8, device="cuda"))
+    assert torch.equal(want, tokens.linear_i8(ctx, x, w, ws, bias))
+
+
+@pytest.mark.parametrize("M", [3, 100])
+@pytest.mark.parametrize("offset", [1, 4, 8])
+def test_unaligned_tensors(M, offset):
+    K, N = 256, 64
+    w, ws, _ = weights(N, K)
+    buf = torch.empty(N * K + 16, dtype=torch.int8, device="cuda")
+    w2 = buf[offset:offset + N * K].view(N, K)
+    w2.copy_(w)
+    x, s = torch.randint(-127, 128, (M, K), dtype=torch.int8).cuda(), torch.ones(M, device="cuda")
+    ctx = context(M, N, K, "i8", "f32")
+    assert torch.equal(tokens.linear_i8(ctx, x, w, ws, x_scale=s), tokens.linear_i8(ctx, x, w2, ws, x_scale=s))
+
+
+@pytest.mark.parametrize("M", [2, 80])
+def test_rows_of_zeros_and_nan(M):
+    K, N = 200, 40
+    x = ref.randn(6, M, K)
+    x[0] = 0
+    x[1, 7] = float("nan")
+    w, ws, bias = weights(N, K)
+    y = tokens.linear_i8(context(M, N, K, "f32", "f32"), x, w, ws, bias)
+    assert torch.equal(y[0], bias) and y[1].isnan().all() and y[2:].isfinite().all()
+
+
+def test_no_rows_and_strided_float_rows():
+    w, ws, _ = weights(24, 48)
+    assert tokens.linear_i8(c3c.Context(), torch.empty(0, 48, device="cuda"), w, ws).shape == (0, 24)
+    x = ref.randn(4, 9, 100)
+    ctx = context(9, 24, 48, "f32", "f32")
+    assert torch.equal(tokens.linear_i8(ctx, x[:, 3:51], w, ws), tokens.linear_i8(ctx, x[:, 3:51].contiguous(), w, ws))
+
+
+def test_large_offsets():
+    """Rows past 2^31 bytes of x, and y past 2^32 bytes."""
+    M, N, K = 140000, 16384, 16400
+    x = torch.zeros(M, K, dtype=torch.int8, device="cuda")
+    x[-300:] = torch.randint(-127, 128, (300, K), dtype=torch.int8).cuda()
+    s = torch.ones(M, device="cuda")
+    w, ws, _ = weights(N, K)
+    y = tokens.linear_i8(c3c.Context(), x, w, ws, x_scale=s)
+    rows = [M - 300, M - 1]
+    check(y[rows], x[rows].cpu().numpy(), np.ones(2, np.float32), w, ws, None, "bf16")
+    assert (y[0] == 0).all()
