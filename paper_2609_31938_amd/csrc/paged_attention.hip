@@ -141,6 +141,135 @@ __device__ inline Seq sequence(const AttendArgs& a, int64_t b) {
   return {r0, static_cast<int>(n > 0 ? n : 0), static_cast<int>(len < cap ? len : cap), static_cast<int>(len - n)};
 }
 
+// Index among the cache's 16-token blocks (of head hk) of block blk of a
+// sequence, or -1 where it has no page or begins at `end` or later.  pow: log2
+// of a page's blocks, or -1.
+struct Find {
+  const int32_t* table;
+  int cols, nb, pow, heads, hk;
+  int64_t pages;
+  __device__ int64_t operator()(int blk, int end) const {
+    const int col = pow >= 0 ? blk >> pow : blk / nb;
+    if (blk * 16 >= end || col >= cols) return -1;
+    const int64_t page = table[col];
+    if (page < 0 || page >= pages) return -1;
+    return (page * heads + hk) * nb + (blk - col * nb);
+  }
+};
+__device__ inline Find finder(const AttendArgs& a, int64_t b, int hk) {
+  const int nb = static_cast<int>(a.c.page) / 16;
+  return {a.b.table + b * a.b.cols, static_cast<int>(a.b.cols), nb, (nb & (nb - 1)) == 0 ? __builtin_ctz(nb) : -1,
+          static_cast<int>(a.c.heads), hk, a.c.pages};
+}
+
+// The query of column (qi, qh), as terms, in the order of K's fragments:
+// element e of step k is channel 64 (k / 2) + 16 g + 8 (k % 2) + e.
+template <class E, int KS>
+__device__ inline void load_query(const AttendArgs& a, int64_t row, int qh, int g, tok_u32x4 (&qf)[KS][Form<E>::NQ]) {
+  const int D = static_cast<int>(a.c.dim);
+  const typename E::store* qp = static_cast<const typename E::store*>(a.q) + row * a.ld_q + static_cast<int64_t>(qh) * D;
+#pragma unroll
+  for (int k = 0; k < KS; ++k) {
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int d = (k >> 1) * 64 + g * 16 + (k & 1) * 8 + e;
+      f[e] = d < D ? E::widen(qp[d]) : 0.f;
+    }
+    to_terms<typename Form<E>::Q2, Form<E>::NQ>(f, qf[k]);
+  }
+}
+
+// An edge tile's scores: what a column does not see becomes -inf.  base: the
+// first token of this lane's block.
+__device__ inline void hide(tok_f32x4 (&s)[4], int base, const Sight& mine, bool page) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int tok = base + 4 * t + i;
+      if (tok < mine.begin || tok >= mine.end || !page) s[t][i] = -kInf;
+    }
+}
+// mask of dword t of a value fragment: the bytes of tokens in [ub, ue)
+__device__ inline uint32_t kept(int base, int t, int ub, int ue) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (base + 4 * t + i >= ub && base + 4 * t + i < ue) m |= 255u << (8 * i);
+  return m;
+}
+// NaN that were taken out of an edge tile's values come back to the channels
+// of the columns that see them.  vb: this lane's block.
+template <int DT>
+__device__ inline void put_nan(const AttendArgs& a, int64_t vb, int tok0, int g, const Sight& mine, tok_f32x4 (&acc)[DT]) {
+  const int D = static_cast<int>(a.c.dim);
+  for (int o = 0; o < 4; ++o) {
+    const int64_t ob = __shfl(vb, 16 * o);
+    if (ob < 0) continue;
+    for (int t = 0; t < 16; ++t) {
+      const int tok = tok0 + 16 * o + t;
+      if (tok < mine.begin || tok >= mine.end) continue;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int ch = d * 16 + g * 4 + i;
+          if (ch < D && (static_cast<const uint8_t*>(a.c.v)[(ob * D + ch) * 16 + t] & 127) == 127)
+            acc[d][i] = __builtin_nanf("");
+        }
+    }
+  }
+}
+
+// The running softmax of one column tile over one 64-token tile: the new
+// maximum, the accumulator in its units, the probabilities as terms.
+// cg: c times the scale of this lane's block; f: what of its value exponent
+// goes to P; shrink: 2^(E before - E now).
+template <int DT, int NP>
+__device__ inline void soften(const tok_f32x4 (&s)[4], float cg, int f, bool low, float shrink, float& m, float& l,
+                              tok_f32x4 (&acc)[DT], tok_u32x4 (&pf)[2][NP]) {
+  float top = -kInf;
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
+  top *= cg;
+  top = fmaxf(top, __shfl_xor(top, 16));
+  top = fmaxf(top, __shfl_xor(top, 32));
+  const float next = fmaxf(m, top);
+  const float ref = next == -kInf ? 0.f : next;
+  if (__ballot(next > m) || shrink != 1.f) {
+    const float down = __builtin_amdgcn_exp2f(m - ref);
+    l *= down;
+    const float all = down * shrink;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] *= all;
+    m = next;
+  }
+  const float lift = kLift - ref;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    float p[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * u + (e >> 2)][e & 3], cg, lift));
+      l += p[e];
+    }
+    if (low) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] *= pow2(f);
+    }
+    to_terms<tok_f16x2, NP>(p, pf[u]);
+  }
+}
+
+// largest exponent of the four blocks' value scales
+__device__ inline int over_groups(int e) {
+  e = max(e, __shfl_xor(e, 16));
+  return max(e, __shfl_xor(e, 32));
+}
+
 // One workgroup: 16 columns (queries and heads that read one key/value head)
 // of one sequence and one split of its tokens; its 4 waves take every fourth
 // 64-token tile of the split and join their results in LDS.  Columns are
@@ -160,9 +289,7 @@ __global__ __launch_bounds__(256) void attend_few(AttendArgs a, int splits, int 
   const int G = static_cast<int>(a.q_heads) / heads;
   const Seq q = sequence(a, b);
   const int64_t columns = static_cast<int64_t>(q.n) * G;
-  const int nb = static_cast<int>(a.c.page) / 16;
-  const int pow = (nb & (nb - 1)) == 0 ? __builtin_ctz(nb) : -1;
-  const int32_t* table = a.b.table + b * a.b.cols;
+  const Find find = finder(a, b, hk);
   const float c = a.scale * kLog2e;
 
   for (int64_t col0 = static_cast<int64_t>(blockIdx.x / splits) * 16; col0 < columns; col0 += static_cast<int64_t>(coltiles) * 16) {
@@ -181,19 +308,7 @@ __global__ __launch_bounds__(256) void attend_few(AttendArgs a, int splits, int 
     if (split + 1 < splits && t0 + split_tiles < t1) t1 = t0 + split_tiles;
 
     tok_u32x4 qf[KS][NQ];
-    {
-      const S* qp = static_cast<const S*>(a.q) + (q.row0 + qi) * a.ld_q + static_cast<int64_t>(qh) * D;
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int d = (k >> 1) * 64 + g * 16 + (k & 1) * 8 + e;
-          f[e] = d < D ? E::widen(qp[d]) : 0.f;
-        }
-        to_terms<typename F::Q2, NQ>(f, qf[k]);
-      }
-    }
+    load_query<E, KS>(a, q.row0 + qi, qh, g, qf);
     tok_f32x4 acc[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -202,14 +317,7 @@ __global__ __launch_bounds__(256) void attend_few(AttendArgs a, int splits, int 
 
     for (int tile = t0 + wave; tile < t1; tile += 4) {
       const int blk0 = tile * 4, tok0 = tile * 64;
-      auto find = [&](int blk) __attribute__((always_inline)) {  // block index among the cache's, or -1
-        const int colp = pow >= 0 ? blk >> pow : blk / nb;
-        if (blk * 16 >= ue || colp >= a.b.cols) return static_cast<int64_t>(-1);
-        const int64_t page = table[colp];
-        if (page < 0 || page >= a.c.pages) return static_cast<int64_t>(-1);
-        return (page * heads + hk) * nb + (blk - colp * nb);
-      };
-      const int64_t kb = find(blk0 + (r >> 2)), vb = find(blk0 + g);
+      const int64_t kb = find(blk0 + (r >> 2), ue), vb = find(blk0 + g, ue);
       const uint8_t* kp = static_cast<const uint8_t*>(a.c.k) + (kb * 16 + (r & 3)) * D + g * 16;
       const uint8_t* vp = static_cast<const uint8_t*>(a.c.v) + (vb * D + r) * 16;
       // scales of block g; c times the key's, 0 kept off so that -inf stays -inf
@@ -244,25 +352,12 @@ __global__ __launch_bounds__(256) void attend_few(AttendArgs a, int splits, int 
       bool bad = false;
       if (edge) {
         const int base = tok0 + 16 * g;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int tok = base + 4 * t + i;
-            if (tok < mine.begin || tok >= mine.end || vb < 0) s[t][i] = -kInf;
-          }
+        hide(s, base, mine, vb >= 0);
         // values that no column sees become 0; NaN among the others are
         // taken out of the product and put back where they are seen
         uint32_t keep[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          keep[t] = 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int tok = base + 4 * t + i;
-            if (tok >= ub && tok < ue) keep[t] |= 255u << (8 * i);
-          }
-        }
+        for (int t = 0; t < 4; ++t) keep[t] = kept(base, t, ub, ue);
         bool any = false;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
@@ -279,47 +374,12 @@ __global__ __launch_bounds__(256) void attend_few(AttendArgs a, int splits, int 
             for (int t = 0; t < 4; ++t) vv[d][t] = no_nan(vv[d][t]);
         }
       }
-      float top = -kInf;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
-      top *= cg;
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      int ve4 = ve;
-      ve4 = max(ve4, __shfl_xor(ve4, 16));
-      ve4 = max(ve4, __shfl_xor(ve4, 32));
-      const float next = fmaxf(m, top);
-      const float ref = next == -kInf ? 0.f : next;
-      if (__ballot(next > m || ve4 > unit)) {
-        const float down = __builtin_amdgcn_exp2f(m - ref);
-        const int grown = max(ve4, unit);
-        l *= down;
-        const float all = down * pow2(unit - grown);
-#pragma unroll
-        for (int d = 0; d < DT; ++d) acc[d] *= all;
-        m = next;
-        unit = grown;
-      }
-      const int k = max(ve - unit, kDeep), f = ve - unit - k;
-      const float vk = pow2(k), lift = kLift - ref;
-      const bool low = __ballot(f < 0) != 0;
+      const int grown = max(unit, over_groups(ve));
+      const int k = max(ve - grown, kDeep), f = ve - grown - k;
+      const float vk = pow2(k);
       tok_u32x4 pf[2][NP];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float p[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * u + (e >> 2)][e & 3], cg, lift));
-          l += p[e];
-        }
-        if (low) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) p[e] *= pow2(f);
-        }
-        to_terms<tok_f16x2, NP>(p, pf[u]);
-      }
+      soften<DT, NP>(s, cg, f, __ballot(f < 0) != 0, pow2(unit - grown), m, l, acc, pf);
+      unit = grown;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -328,24 +388,7 @@ __global__ __launch_bounds__(256) void attend_few(AttendArgs a, int splits, int 
 #pragma unroll
           for (int n = 0; n < NP; ++n) acc[d] = mfma_f16(vf, pf[u][n], acc[d]);
         }
-      if (bad) {
-        for (int o = 0; o < 4; ++o) {
-          const int64_t ob = __shfl(vb, 16 * o);
-          if (ob < 0) continue;
-          for (int t = 0; t < 16; ++t) {
-            const int tok = tok0 + 16 * o + t;
-            if (tok < mine.begin || tok >= mine.end) continue;
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int ch = d * 16 + g * 4 + i;
-                if (ch < D && (static_cast<const uint8_t*>(a.c.v)[(ob * D + ch) * 16 + t] & 127) == 127)
-                  acc[d][i] = __builtin_nanf("");
-              }
-          }
-        }
-      }
+      if (bad) put_nan<DT>(a, vb, tok0, g, mine, acc);
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -399,6 +442,235 @@ __global__ __launch_bounds__(256) void attend_few(AttendArgs a, int splits, int 
   }
 }
 
+__device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(1))) const void global_void;
+
+// One workgroup: 4 waves of CT column tiles each, one sequence, one key/value
+// head, one split of the tokens.  The codes of a 64-token tile come straight
+// into LDS, fragment by fragment (1 KB each: a lane's 16 bytes side by side, so
+// reads have no bank conflicts), two tiles in turn; every wave converts the
+// fragments that it multiplies with its CT column tiles.
+template <class E, int DP, int CT>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(AttendArgs a, int splits, int split_tiles, int coltiles) {
+  typedef Form<E> F;
+  typedef typename E::store S;
+  constexpr int KS = DP / 32, DT = DP / 16, NJ = DP / 64, NQ = F::NQ, NP = F::NP;
+  constexpr int NF = 4 * NJ + DT;  // fragments of a tile
+  static_assert(NF % 4 == 0, "whole rounds of waves");
+  __shared__ __align__(16) uint8_t lds[2][NF * 1024];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  // workgroup i runs on L2 cache i % 8: each cache gets a run of consecutive
+  // units, so that one cache reads a head's codes; the last columns, which see
+  // most in a causal call, come first
+  const int heads = static_cast<int>(a.c.heads), D = static_cast<int>(a.c.dim);
+  int64_t id = blockIdx.x;
+  {
+    const int64_t total = gridDim.x, each = total / 8, rest = total % 8, c = id % 8;
+    id = c * each + (c < rest ? c : rest) + id / 8;
+  }
+  const int ct = coltiles - 1 - static_cast<int>(id % coltiles);
+  id /= coltiles;
+  const int split = static_cast<int>(id % splits);
+  id /= splits;
+  const int hk = static_cast<int>(id % heads);
+  const int64_t b = id / heads;
+  const int G = static_cast<int>(a.q_heads) / heads;
+  const Seq q = sequence(a, b);
+  const int64_t columns = static_cast<int64_t>(q.n) * G;
+  const Find find = finder(a, b, hk);
+  const float c = a.scale * kLog2e;
+  constexpr int WG = 64 * CT;  // columns
+
+  for (int64_t wg0 = static_cast<int64_t>(ct) * WG; wg0 < columns; wg0 += static_cast<int64_t>(coltiles) * WG) {
+    // what the workgroup's columns see together, and what this wave's do
+    auto sight_of = [&](int64_t col) { return sight(a, q.len, q.start + static_cast<int>((col < columns ? col : columns - 1) / G)); };
+    const int ub = sight_of(wg0).begin, ue = sight_of(wg0 + WG - 1).end;
+    const int64_t col0 = wg0 + wave * 16 * CT;
+    const Sight wlo = sight_of(col0), whi = sight_of(col0 + 16 * CT - 1);
+    const int t0 = ub / 64 + split * split_tiles;
+    int t1 = (ue + 63) / 64;
+    if (split + 1 < splits && t0 + split_tiles < t1) t1 = t0 + split_tiles;
+
+    tok_u32x4 qf[CT][KS][NQ];
+    Sight mine[CT];
+    tok_f32x4 acc[CT][DT];
+    float m[CT], l[CT];
+#pragma unroll
+    for (int x = 0; x < CT; ++x) {
+      const int64_t col = col0 + 16 * x + r < columns ? col0 + 16 * x + r : columns - 1;
+      const int qi = static_cast<int>(col / G), qh = hk * G + static_cast<int>(col % G);
+      mine[x] = sight(a, q.len, q.start + qi);
+      load_query<E, KS>(a, q.row0 + qi, qh, g, qf[x]);
+      m[x] = -kInf;
+      l[x] = 0.f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[x][d] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    int unit = -126;
+
+    // a tile on its way: this lane's blocks of K rows and of V
+    struct Ids {
+      int64_t kb, vb;
+    };
+    auto ids = [&](int tile) { return Ids{find(tile * 4 + (r >> 2), ue), find(tile * 4 + g, ue)}; };
+    auto fetch = [&](const Ids& i, int buf) __attribute__((always_inline)) {
+      const uint8_t* kp = static_cast<const uint8_t*>(a.c.k) + (i.kb * 16 + (r & 3)) * D + g * 16;
+      const uint8_t* vp = static_cast<const uint8_t*>(a.c.v) + (i.vb * D + r) * 16;
+#pragma unroll
+      for (int n = 0; n < NF / 4; ++n) {
+        const int f = n * 4 + wave;
+        const bool isk = f < 4 * NJ;
+        const int t = f / NJ, j = f % NJ, d = f - 4 * NJ;
+        const bool ok = isk ? i.kb >= 0 && j * 64 + g * 16 < D : i.vb >= 0 && d * 16 < D;
+        const uint8_t* p = isk ? kp + 4 * t * D + j * 64 : vp + d * 256;
+        __builtin_amdgcn_global_load_lds((global_void*)(ok ? p : reinterpret_cast<const uint8_t*>(kZeros)),
+                                         (lds_void*)(&lds[buf][f * 1024]), 16, 0, 0);
+      }
+    };
+
+    Ids cur{-1, -1}, nxt{-1, -1};
+    float ks = 1.f, vs = 1.f;
+    auto scales = [&](const Ids& i, float& k, float& v) {
+      k = i.vb >= 0 ? a.c.k_scale[i.vb] : 1.f;
+      v = i.vb >= 0 ? a.c.v_scale[i.vb] : 0x1p-126f;
+    };
+    if (t0 < t1) {
+      cur = ids(t0);
+      fetch(cur, 0);
+      scales(cur, ks, vs);
+      nxt = ids(t0 + 1);
+    }
+    for (int tile = t0; tile < t1; ++tile) {
+      const int buf = (tile - t0) & 1, tok0 = tile * 64;
+      __syncthreads();  // this tile is in LDS, and nobody reads the other buffer
+      float ks1 = 1.f, vs1 = 1.f;
+      Ids far = nxt;
+      if (tile + 1 < t1) {
+        fetch(nxt, buf ^ 1);
+        scales(nxt, ks1, vs1);
+        far = ids(tile + 2);
+      }
+      const uint8_t* frag = &lds[buf][lane * 16];
+      auto read = [&](int f) { return *reinterpret_cast<const tok_u32x4*>(frag + f * 1024); };
+      if (tok0 < whi.end && tok0 + 64 > wlo.begin) {
+        const float cg = fmaxf(c * ks, 0x1p-126f);
+        const int ve = exponent_of(vs);
+        tok_f32x4 s[CT][4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+          for (int x = 0; x < CT; ++x) s[x][t] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) {
+            const tok_u32x4 kv = read(t * NJ + j);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const tok_u32x4 kf = F::k(kv[2 * h], kv[2 * h + 1]);
+#pragma unroll
+              for (int x = 0; x < CT; ++x)
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) s[x][t] = F::mfma(kf, qf[x][2 * j + h][n], s[x][t]);
+            }
+          }
+        }
+        const bool edge = tok0 < whi.begin || tok0 + 64 > wlo.end || __ballot(cur.vb < 0) != 0;
+        const int base = tok0 + 16 * g;
+        uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
+        bool bad = false;
+        if (edge) {
+#pragma unroll
+          for (int x = 0; x < CT; ++x) hide(s[x], base, mine[x], cur.vb >= 0);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) keep[t] = kept(base, t, wlo.begin, whi.end);
+          bool any = false;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const tok_u32x4 v = read(4 * NJ + d);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) any |= nan_code(v[t] & keep[t]);
+          }
+          bad = __ballot(any) != 0;
+        }
+        const int grown = max(unit, over_groups(ve));
+        const int k = max(ve - grown, kDeep), f = ve - grown - k;
+        const float vk = pow2(k), shrink = pow2(unit - grown);
+        const bool low = __ballot(f < 0) != 0;
+        unit = grown;
+        tok_u32x4 pf[CT][2][NP];
+#pragma unroll
+        for (int x = 0; x < CT; ++x) soften<DT, NP>(s[x], cg, f, low, shrink, m[x], l[x], acc[x], pf[x]);
+        auto second = [&](bool clean) __attribute__((always_inline)) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            tok_u32x4 v = read(4 * NJ + d);
+            if (!clean) {
+#pragma unroll
+              for (int t = 0; t < 4; ++t) v[t] = no_nan(v[t] & keep[t]);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const tok_u32x4 vf = codes_f16(v[2 * u], v[2 * u + 1], vk);
+#pragma unroll
+              for (int x = 0; x < CT; ++x)
+#pragma unroll
+                for (int n = 0; n < NP; ++n) acc[x][d] = mfma_f16(vf, pf[x][u][n], acc[x][d]);
+            }
+          }
+        };
+        if (edge)
+          second(false);
+        else
+          second(true);
+        if (bad) {
+#pragma unroll
+          for (int x = 0; x < CT; ++x) put_nan<DT>(a, cur.vb, tok0, g, mine[x], acc[x]);
+        }
+      }
+      cur = nxt;
+      nxt = far;
+      ks = ks1;
+      vs = vs1;
+    }
+    __syncthreads();  // before another round's first tile
+
+#pragma unroll
+    for (int x = 0; x < CT; ++x) {
+      float sum = l[x];
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      sum *= pow2(-kLift);
+      const int64_t col = col0 + 16 * x + r;
+      if (col >= columns) continue;
+      const int64_t row = (q.row0 + col / G) * a.q_heads + hk * G + col % G;
+      float* part = splits > 1 ? a.part + (static_cast<int64_t>(split) * a.b.T * a.q_heads + row) * (D + 2) : nullptr;
+      const float inv = part ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        if (d * 16 >= D) continue;
+        float o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = ldexpf(acc[x][d][i], unit - kLift) * inv;
+        if (part) {
+          __builtin_memcpy(part + 2 + d * 16 + g * 4, o, 16);
+        } else {
+          S v[4] = {E::narrow(o[0]), E::narrow(o[1]), E::narrow(o[2]), E::narrow(o[3])};
+          __builtin_memcpy(static_cast<S*>(a.out) + row * D + d * 16 + g * 4, v, sizeof v);
+        }
+      }
+      if (g == 0) {
+        if (part) {
+          part[0] = m[x];
+          part[1] = sum;
+        } else if (a.lse) {
+          a.lse[row] = sum == 0.f ? -kInf : m[x] * kLn2 + logf(sum);
+        }
+      }
+    }
+  }
+}
+
 // out and lse from the partial results of a split call: one wave a row.
 template <class E>
 __global__ __launch_bounds__(256) void attend_join(AttendArgs a, int splits) {
@@ -436,18 +708,39 @@ int64_t tiles_seen(const c3c_kv_batch& b, int64_t page, int64_t window) {
   return up(tokens, 64);
 }
 
+// Column tiles a wave: two keep two waves on a SIMD, whose exponentials and
+// matrix products overlap; f32's three terms leave room for one.
+constexpr int column_tiles(int dp, int terms) { return dp > 192 || terms > 1 ? 1 : 2; }
+int64_t workgroup_columns(int64_t dim, int dtype) {
+  return 64 * column_tiles(static_cast<int>(dim), dtype == C3C_DTYPE_F32 ? 3 : 1);
+}
+
+// Calls of at most 16 columns a sequence and head take attend_few.
+bool few(int64_t columns) { return columns <= 16; }
+
 template <class E>
-hipError_t run(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  const int64_t G = a.q_heads / a.c.heads, coltiles = up(a.b.max_new * G, 16);
-  const int64_t tiles = tiles_seen(a.b, a.c.page, a.window);
-  const int64_t blocks = coltiles * p.splits;
-  if (a.b.B > 65535 || a.c.heads > 65535 || blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  auto k = a.c.dim <= 64    ? attend_few<E, 64>
-           : a.c.dim <= 128 ? attend_few<E, 128>
-           : a.c.dim <= 192 ? attend_few<E, 192>
-                            : attend_few<E, 256>;
-  hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(a.c.heads), static_cast<unsigned>(a.b.B)),
-                     dim3(256), 0, s, a, p.splits, static_cast<int>(up(tiles, p.splits)), static_cast<int>(coltiles));
+hipError_t run(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s) {
+  const int64_t columns = a.b.max_new * (a.q_heads / a.c.heads);
+  const int64_t split_tiles = up(tiles_seen(a.b, a.c.page, a.window), p.splits);
+  if (few(columns)) {
+    if (a.b.B > 65535 || a.c.heads > 65535) return hipErrorInvalidConfiguration;
+    auto k = a.c.dim <= 64    ? attend_few<E, 64>
+             : a.c.dim <= 128 ? attend_few<E, 128>
+             : a.c.dim <= 192 ? attend_few<E, 192>
+                              : attend_few<E, 256>;
+    hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(p.splits), static_cast<unsigned>(a.c.heads), static_cast<unsigned>(a.b.B)),
+                       dim3(256), 0, s, a, p.splits, static_cast<int>(split_tiles), 1);
+  } else {
+    const int64_t coltiles = up(columns, workgroup_columns(a.c.dim, dtype)), blocks = coltiles * p.splits * a.c.heads * a.b.B;
+    if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+    constexpr int NQ = Form<E>::NQ;
+    auto k = a.c.dim <= 64    ? attend_many<E, 64, column_tiles(64, NQ)>
+             : a.c.dim <= 128 ? attend_many<E, 128, column_tiles(128, NQ)>
+             : a.c.dim <= 192 ? attend_many<E, 192, column_tiles(192, NQ)>
+                              : attend_many<E, 256, column_tiles(256, NQ)>;
+    hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a, p.splits, static_cast<int>(split_tiles),
+                       static_cast<int>(coltiles));
+  }
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.splits > 1) {
     const int64_t jb = up(a.b.T * a.q_heads, 4);
@@ -463,12 +756,14 @@ hipError_t run(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 AttendPlan plan_attend(const c3c_kv_cache& c, const c3c_kv_batch& b, int dtype, int64_t q_heads,
                        int causal, int64_t window) {
   AttendPlan p;
-  const int64_t base = up(b.max_new * (q_heads / c.heads), 16) * c.heads * b.B;
-  const int64_t tiles = tiles_seen(b, c.page, window);
+  const int64_t columns = b.max_new * (q_heads / c.heads), tiles = tiles_seen(b, c.page, window);
+  const int64_t base = up(columns, few(columns) ? 16 : workgroup_columns(c.dim, dtype)) * c.heads * b.B;
   if (base == 0) return p;
-  // enough workgroups to fill the device several times (sequences are
-  // ragged), of at least one tile a wave
-  const int64_t want = up(8 * device_compute_units(), base), most = up(tiles, 4);
+  // few: enough workgroups to fill the device several times (sequences are
+  // ragged), of at least one tile a wave; many: one workgroup a compute unit,
+  // of at least 4 tiles
+  const int64_t cus = device_compute_units();
+  const int64_t want = few(columns) ? up(8 * cus, base) : cus / base, most = up(tiles, 4);
   const int64_t s = want < most ? want : most;
   if (s > 1) {
     p.splits = static_cast<int>(s);
@@ -479,9 +774,9 @@ AttendPlan plan_attend(const c3c_kv_cache& c, const c3c_kv_batch& b, int dtype, 
 
 hipError_t launch_attend(const AttendArgs& a, int dtype, const AttendPlan& plan, hipStream_t s) {
   if (a.b.B == 0 || a.b.T == 0 || a.b.max_new == 0) return hipSuccess;
-  return dtype == C3C_DTYPE_BF16  ? run<ElemBf16>(a, plan, s)
-         : dtype == C3C_DTYPE_F16 ? run<ElemF16>(a, plan, s)
-                                  : run<ElemF32>(a, plan, s);
+  return dtype == C3C_DTYPE_BF16  ? run<ElemBf16>(a, plan, dtype, s)
+         : dtype == C3C_DTYPE_F16 ? run<ElemF16>(a, plan, dtype, s)
+                                  : run<ElemF32>(a, plan, dtype, s);
 }
 
 }  // namespace c3c
