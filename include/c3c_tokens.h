@@ -135,9 +135,9 @@ typedef struct c3c_kv_cache {
 /* The sequences of a call, packed: sequence b has the rows cu[b] .. cu[b+1]
  * of q, k, v, which are the last tokens of its len[b].  Token p of sequence b
  * lies in page table[b][p / page].  Device memory: table [B][cols], cu [B+1]
- * ascending from 0 to T, len [B].  max_new: no sequence has more new tokens;
- * max_len: no sequence is longer (both shape the launch; they are not read
- * from the device).  What lies on the device is not trusted: rows outside
+ * ascending from 0 to T, len [B].  max_new: no sequence has more new tokens
+ * (attention leaves the output of rows past it undefined); max_len: no
+ * sequence is longer (it only plans the work).  What lies on the device is not trusted: rows outside
  * [0, T) are cut off, a token whose page is outside [0, pages) or past the
  * table's columns is not stored and not seen (so -1 marks an evicted page). */
 typedef struct c3c_kv_batch {
@@ -191,7 +191,7 @@ int c3c_kv_append(c3c_ctx* ctx, const c3c_kv_cache* cache, const c3c_kv_batch* b
  * dtype.  Rows of q that belong to no sequence leave theirs undefined.
  * Probabilities enter the matrix cores as sums of 1 (bf16), 2 (f16) or 3 (f32)
  * f16 terms; a value loses precision where its block's scale is more than
- * 2^30 below the largest value scale that the query's neighbours see.
+ * 2^24 below the largest value scale that the query's neighbours see.
  *
  * Workspace (c3c_paged_attention_workspace_bytes): the partial results of a
  * call whose sequences are split because there are too few queries for the

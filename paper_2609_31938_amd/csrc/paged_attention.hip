@@ -17,7 +17,7 @@
 //
 // K: e4m3 codes are exact in bf16 and f16; the scale joins c.
 // Q: in its own type, f32 as the sum of three bf16 terms.
-// P: 2^15 p as a sum of f16 terms (1 for bf16 calls, 2 for f16, 3 for f32):
+// P: 2^7 p as a sum of f16 terms (1 for bf16 calls, 2 for f16, 3 for f32):
 //   11 bits each, where a bf16 term would have 8 and its rounding would be
 //   seen in a bf16 output.
 // V: codes in f16 times 2^k.  The accumulator is kept in units of 2^E, E the
@@ -104,7 +104,10 @@ struct Form<ElemF32> : Form<ElemBf16> {
 __device__ inline float pow2(int e) { return e < -126 ? 0.f : __uint_as_float(static_cast<uint32_t>((e < 127 ? e : 127) + 127) << 23); }
 __device__ inline int exponent_of(float scale) { return static_cast<int>((__float_as_uint(scale) >> 23) & 255u) - 127; }
 
-constexpr int kLift = 15;  // P is 2^15 p: at most 2^15, and p keeps its bits down to 2^-29
+// P is 2^7 p.  The maximum that p is taken against may stay up to 2^8 behind
+// the true one, so P is at most 2^15, and p keeps its bits down to 2^-21.
+constexpr int kLift = 7;
+constexpr float kSlack = 8.f;
 constexpr int kDeep = -15; // least k: codes down to 2^-9 stay multiples of 2^-24
 
 // whether a dword holds the code of a NaN
@@ -115,67 +118,79 @@ __device__ inline uint32_t no_nan(uint32_t w) {
   return w & ~(at * 255u);
 }
 
+// The kernels' arguments: scalar registers are short beside two products and
+// a softmax, so sizes are 32 bits and what the host can work out is.
+struct Dev {
+  const uint8_t *k, *v;
+  const float *ks, *vs;
+  const int32_t *table, *cu, *len;
+  const void* q;
+  void* out;
+  float *lse, *part;
+  int64_t ld_q;
+  int T, q_heads, heads, G, D;
+  int pages, nb, pow, cols, cap;  // blocks of a page, their log2 or -1; tokens of a table row
+  int causal, window;
+  float c;                        // scale * log2 e
+  int splits, split_tiles, coltiles;
+};
+
 // What a column (a query) sees: tokens [begin, end) of its sequence.
 struct Sight {
   int begin, end;
 };
-__device__ inline Sight sight(const AttendArgs& a, int len, int p) {
+__device__ inline Sight sight(const Dev& a, int len, int p) {
   Sight s{0, len};
   if (a.causal && p + 1 < s.end) s.end = p + 1;
-  if (a.window > 0 && p - a.window + 1 > s.begin) s.begin = static_cast<int>(p - a.window + 1);
+  if (a.window > 0 && p - a.window + 1 > s.begin) s.begin = p - a.window + 1;
   return s;
 }
 
 // The sequence b as the kernels read it from the device: nothing of it is
 // trusted.
 struct Seq {
-  int64_t row0;
-  int n, len, start;  // new tokens, all tokens that the table can hold, place of the first new one
+  int row0, n, len, start;  // new tokens, all tokens that the table can hold, place of the first new one
 };
-__device__ inline Seq sequence(const AttendArgs& a, int64_t b) {
-  int64_t r0 = a.b.cu[b], r1 = a.b.cu[b + 1];
+__device__ inline Seq sequence(const Dev& a, int b) {
+  int r0 = a.cu[b], r1 = a.cu[b + 1];
   r0 = r0 < 0 ? 0 : r0;
-  r1 = r1 > a.b.T ? a.b.T : r1;
-  const int64_t all = a.b.cols * a.c.page, cap = all < 0x7fffff00 ? all : 0x7fffff00;
-  const int64_t len = a.b.len[b], n = r1 - r0;
-  return {r0, static_cast<int>(n > 0 ? n : 0), static_cast<int>(len < cap ? len : cap), static_cast<int>(len - n)};
+  r1 = r1 > a.T ? a.T : r1;
+  const int len = a.len[b], n = r1 > r0 ? r1 - r0 : 0;
+  // a negative length is one of nothing: its queries see nothing either way
+  return {r0, n, len < a.cap ? len : a.cap, (len < 0 ? 0 : len) - n};
 }
 
-// Index among the cache's 16-token blocks (of head hk) of block blk of a
-// sequence, or -1 where it has no page or begins at `end` or later.  pow: log2
-// of a page's blocks, or -1.
-struct Find {
-  const int32_t* table;
-  int cols, nb, pow, heads, hk;
-  int64_t pages;
-  __device__ int64_t operator()(int blk, int end) const {
-    const int col = pow >= 0 ? blk >> pow : blk / nb;
-    if (blk * 16 >= end || col >= cols) return -1;
-    const int64_t page = table[col];
-    if (page < 0 || page >= pages) return -1;
-    return (page * heads + hk) * nb + (blk - col * nb);
-  }
-};
-__device__ inline Find finder(const AttendArgs& a, int64_t b, int hk) {
-  const int nb = static_cast<int>(a.c.page) / 16;
-  return {a.b.table + b * a.b.cols, static_cast<int>(a.b.cols), nb, (nb & (nb - 1)) == 0 ? __builtin_ctz(nb) : -1,
-          static_cast<int>(a.c.heads), hk, a.c.pages};
+// Index among the cache's 16-token blocks (of head hk) of block blk of
+// sequence b, or -1 where it has no page or begins at `end` or later.
+__device__ inline int64_t find(const Dev& a, int b, int hk, int blk, int end) {
+  const int col = a.pow >= 0 ? blk >> a.pow : blk / a.nb;
+  if (blk * 16 >= end || col >= a.cols) return -1;
+  const int page = a.table[static_cast<int64_t>(b) * a.cols + col];
+  if (page < 0 || page >= a.pages) return -1;
+  return (static_cast<int64_t>(page) * a.heads + hk) * a.nb + (blk - col * a.nb);
+}
+
+// v, as a value that the compiler cannot compute with ahead of time: keeps
+// what rare or early code derives from it out of the main loop's registers
+__device__ inline int apart(int v) {
+  asm volatile("" : "+s"(v));
+  return v;
 }
 
 // The query of column (qi, qh), as terms, in the order of K's fragments:
 // element e of step k is channel 64 (k / 2) + 16 g + 8 (k % 2) + e.
 template <class E, int KS>
-__device__ inline void load_query(const AttendArgs& a, int64_t row, int qh, int g, tok_u32x4 (&qf)[KS][Form<E>::NQ]) {
-  const int D = static_cast<int>(a.c.dim);
-  const typename E::store* qp = static_cast<const typename E::store*>(a.q) + row * a.ld_q + static_cast<int64_t>(qh) * D;
+__device__ inline void load_query(const Dev& a, int64_t row, int qh, int g, tok_u32x4 (&qf)[KS][Form<E>::NQ]) {
+  typedef typename E::store S;
+  const int D = apart(a.D);
+  const S* qp = static_cast<const S*>(a.q) + row * a.ld_q + static_cast<int64_t>(qh) * D + g * 16;
 #pragma unroll
   for (int k = 0; k < KS; ++k) {
+    S v[8] = {};
+    if ((k >> 1) * 64 + g * 16 < D) __builtin_memcpy(v, qp + (k >> 1) * 64 + (k & 1) * 8, sizeof v);
     float f[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int d = (k >> 1) * 64 + g * 16 + (k & 1) * 8 + e;
-      f[e] = d < D ? E::widen(qp[d]) : 0.f;
-    }
+    for (int e = 0; e < 8; ++e) f[e] = E::widen(v[e]);
     to_terms<typename Form<E>::Q2, Form<E>::NQ>(f, qf[k]);
   }
 }
@@ -202,30 +217,35 @@ __device__ inline uint32_t kept(int base, int t, int ub, int ue) {
 // NaN that were taken out of an edge tile's values come back to the channels
 // of the columns that see them.  vb: this lane's block.
 template <int DT>
-__device__ inline void put_nan(const AttendArgs& a, int64_t vb, int tok0, int g, const Sight& mine, tok_f32x4 (&acc)[DT]) {
-  const int D = static_cast<int>(a.c.dim);
+__device__ inline void put_nan(const Dev& a, int64_t vb, int tok0, int g, const Sight& mine, tok_f32x4 (&acc)[DT]) {
+  const int D = apart(a.D);
   for (int o = 0; o < 4; ++o) {
     const int64_t ob = __shfl(vb, 16 * o);
     if (ob < 0) continue;
     for (int t = 0; t < 16; ++t) {
       const int tok = tok0 + 16 * o + t;
       if (tok < mine.begin || tok >= mine.end) continue;
+      const uint8_t* v = a.v + (ob * D + g * 4) * 16 + t;
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; ++d) {
+        if (d * 16 >= D) break;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int ch = d * 16 + g * 4 + i;
-          if (ch < D && (static_cast<const uint8_t*>(a.c.v)[(ob * D + ch) * 16 + t] & 127) == 127)
-            acc[d][i] = __builtin_nanf("");
-        }
+        for (int i = 0; i < 4; ++i)
+          if ((v[(d * 16 + i) * 16] & 127) == 127) acc[d][i] = __builtin_nanf("");
+      }
     }
   }
 }
 
-// The running softmax of one column tile over one 64-token tile: the new
-// maximum, the accumulator in its units, the probabilities as terms.
+// The running softmax of one column tile over one 64-token tile: the maximum,
+// the accumulators in its units, the probabilities as terms, their sum.
 // cg: c times the scale of this lane's block; f: what of its value exponent
 // goes to P; shrink: 2^(E before - E now).
+//   The maximum moves only when a score passes it by more than kSlack: the
+// exponentials' range allows it, and it then seldom costs a reduction over
+// lanes and a pass over the accumulators.
+//   The sum (l: this lane's part) is of the probabilities before their
+// rounding to terms, for lse is held to fp32.
 template <int DT, int NP>
 __device__ inline void soften(const tok_f32x4 (&s)[4], float cg, int f, bool low, float shrink, float& m, float& l,
                               tok_f32x4 (&acc)[DT], tok_u32x4 (&pf)[2][NP]) {
@@ -235,19 +255,18 @@ __device__ inline void soften(const tok_f32x4 (&s)[4], float cg, int f, bool low
 #pragma unroll
     for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
   top *= cg;
-  top = fmaxf(top, __shfl_xor(top, 16));
-  top = fmaxf(top, __shfl_xor(top, 32));
-  const float next = fmaxf(m, top);
-  const float ref = next == -kInf ? 0.f : next;
-  if (__ballot(next > m) || shrink != 1.f) {
-    const float down = __builtin_amdgcn_exp2f(m - ref);
+  if (__ballot(top > m + kSlack) || shrink != 1.f) {
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float next = top > m + kSlack ? top : m;
+    const float down = __builtin_amdgcn_exp2f(m - (next == -kInf ? 0.f : next));
     l *= down;
     const float all = down * shrink;
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] *= all;
     m = next;
   }
-  const float lift = kLift - ref;
+  const float lift = kLift - (m == -kInf ? 0.f : m);
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     float p[8];
@@ -275,7 +294,7 @@ __device__ inline int over_groups(int e) {
 // 64-token tile of the split and join their results in LDS.  Columns are
 // numbered token by token, the G heads of a token side by side.
 template <class E, int DP>  // DP: channels padded to 64
-__global__ __launch_bounds__(256) void attend_few(AttendArgs a, int splits, int split_tiles, int coltiles) {
+__global__ __launch_bounds__(256) void attend_few(Dev a) {
   typedef Form<E> F;
   constexpr int KS = DP / 32, DT = DP / 16, NQ = F::NQ, NP = F::NP;
   typedef typename E::store S;
@@ -283,162 +302,150 @@ __global__ __launch_bounds__(256) void attend_few(AttendArgs a, int splits, int 
   __shared__ __align__(16) float so[4][16][DP + 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
-  const int split = blockIdx.x % splits;
-  const int64_t b = blockIdx.z;
-  const int hk = blockIdx.y, heads = static_cast<int>(a.c.heads), D = static_cast<int>(a.c.dim);
-  const int G = static_cast<int>(a.q_heads) / heads;
+  const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+  const int D = a.D, G = a.G;
   const Seq q = sequence(a, b);
-  const int64_t columns = static_cast<int64_t>(q.n) * G;
-  const Find find = finder(a, b, hk);
-  const float c = a.scale * kLog2e;
+  const int columns = q.n * G < 16 ? q.n * G : 16;
+  if (columns == 0) return;
+  const int col = r < columns ? r : columns - 1;
+  const int qi = col / G, qh = hk * G + col % G;
+  const Sight mine = sight(a, q.len, q.start + qi);
+  // what all columns see together, and what each of them sees
+  const Sight lowest = sight(a, q.len, q.start), highest = sight(a, q.len, q.start + (columns - 1) / G);
+  const int ub = lowest.begin, ue = highest.end, cb = highest.begin, ce = lowest.end;
+  const int t0 = ub / 64 + split * a.split_tiles;
+  int t1 = (ue + 63) / 64;
+  // the last split takes what is left
+  if (split + 1 < a.splits && t0 + a.split_tiles < t1) t1 = t0 + a.split_tiles;
 
-  for (int64_t col0 = static_cast<int64_t>(blockIdx.x / splits) * 16; col0 < columns; col0 += static_cast<int64_t>(coltiles) * 16) {
-    const int64_t col = col0 + r < columns ? col0 + r : columns - 1;
-    const int qi = static_cast<int>(col / G), qh = hk * G + static_cast<int>(col % G);
-    const Sight mine = sight(a, q.len, q.start + qi);
-    // what all columns see together, and what each of them sees
-    const int i0 = static_cast<int>(col0 / G);
-    const int64_t lastcol = col0 + 15 < columns ? col0 + 15 : columns - 1;
-    const int i1 = static_cast<int>(lastcol / G);
-    const Sight lowest = sight(a, q.len, q.start + i0), highest = sight(a, q.len, q.start + i1);
-    const int ub = lowest.begin, ue = highest.end, cb = highest.begin, ce = lowest.end;
-    const int t0 = ub / 64 + split * split_tiles;
-    int t1 = (ue + 63) / 64;
-    // the last split takes what is left
-    if (split + 1 < splits && t0 + split_tiles < t1) t1 = t0 + split_tiles;
+  tok_u32x4 qf[KS][NQ];
+  load_query<E, KS>(a, q.row0 + qi, qh, g, qf);
+  tok_f32x4 acc[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d) acc[d] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -kInf, l = 0.f;  // l: this lane's part of 2^kLift times the sum
+  int unit = -126;           // E
 
-    tok_u32x4 qf[KS][NQ];
-    load_query<E, KS>(a, q.row0 + qi, qh, g, qf);
-    tok_f32x4 acc[DT];
+  for (int tile = t0 + wave; tile < t1; tile += 4) {
+    const int blk0 = tile * 4, tok0 = tile * 64;
+    const int64_t kb = find(a, b, hk, blk0 + (r >> 2), ue), vb = find(a, b, hk, blk0 + g, ue);
+    const uint8_t* kp = a.k + (kb * 16 + (r & 3)) * D + g * 16;
+    const uint8_t* vp = a.v + (vb * D + r) * 16;
+    // scales of block g; c times the key's, 0 kept off so that -inf stays -inf
+    const float cg = vb >= 0 ? fmaxf(a.c * a.ks[vb], 0x1p-126f) : 1.f;
+    const int ve = vb >= 0 ? exponent_of(a.vs[vb]) : -126;
+    tok_u32x4 kv[4][DP / 64], vv[DT];
 #pragma unroll
-    for (int d = 0; d < DT; ++d) acc[d] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -kInf, l = 0.f;  // l: this lane's part of 2^15 times the sum
-    int unit = -126;           // E
-
-    for (int tile = t0 + wave; tile < t1; tile += 4) {
-      const int blk0 = tile * 4, tok0 = tile * 64;
-      const int64_t kb = find(blk0 + (r >> 2), ue), vb = find(blk0 + g, ue);
-      const uint8_t* kp = static_cast<const uint8_t*>(a.c.k) + (kb * 16 + (r & 3)) * D + g * 16;
-      const uint8_t* vp = static_cast<const uint8_t*>(a.c.v) + (vb * D + r) * 16;
-      // scales of block g; c times the key's, 0 kept off so that -inf stays -inf
-      const float cg = vb >= 0 ? fmaxf(c * a.c.k_scale[vb], 0x1p-126f) : 1.f;
-      const int ve = vb >= 0 ? exponent_of(a.c.v_scale[vb]) : -126;
-      tok_u32x4 kv[4][DP / 64], vv[DT];
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int j = 0; j < DP / 64; ++j) {
-          kv[t][j] = tok_u32x4{0, 0, 0, 0};
-          if (kb >= 0 && j * 64 + g * 16 < D) kv[t][j] = *reinterpret_cast<const tok_u32x4*>(kp + 4 * t * D + j * 64);
-        }
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        vv[d] = tok_u32x4{0, 0, 0, 0};
-        if (vb >= 0 && d * 16 < D) vv[d] = *reinterpret_cast<const tok_u32x4*>(vp + d * 256);
+      for (int j = 0; j < DP / 64; ++j) {
+        kv[t][j] = tok_u32x4{0, 0, 0, 0};
+        if (kb >= 0 && j * 64 + g * 16 < D) kv[t][j] = *reinterpret_cast<const tok_u32x4*>(kp + 4 * t * D + j * 64);
       }
-      tok_f32x4 s[4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        s[t] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int d = 0; d < DT; ++d) {
+      vv[d] = tok_u32x4{0, 0, 0, 0};
+      if (vb >= 0 && d * 16 < D) vv[d] = *reinterpret_cast<const tok_u32x4*>(vp + d * 256);
+    }
+    tok_f32x4 s[4];
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const tok_u32x4 kf = F::k(kv[t][k >> 1][(k & 1) * 2], kv[t][k >> 1][(k & 1) * 2 + 1]);
+    for (int t = 0; t < 4; ++t) {
+      s[t] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int n = 0; n < NQ; ++n) s[t] = F::mfma(kf, qf[k][n], s[t]);
-        }
+      for (int k = 0; k < KS; ++k) {
+        const tok_u32x4 kf = F::k(kv[t][k >> 1][(k & 1) * 2], kv[t][k >> 1][(k & 1) * 2 + 1]);
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) s[t] = F::mfma(kf, qf[k][n], s[t]);
       }
-      // a tile that some column sees in part only, or with a page missing
-      const bool edge = tok0 < cb || tok0 + 64 > ce || __ballot(vb < 0) != 0;
-      bool bad = false;
-      if (edge) {
-        const int base = tok0 + 16 * g;
-        hide(s, base, mine, vb >= 0);
-        // values that no column sees become 0; NaN among the others are
-        // taken out of the product and put back where they are seen
-        uint32_t keep[4];
+    }
+    // a tile that some column sees in part only, or with a page missing
+    const bool edge = tok0 < cb || tok0 + 64 > ce || __ballot(vb < 0) != 0;
+    bool bad = false;
+    if (edge) {
+      const int base = tok0 + 16 * g;
+      hide(s, base, mine, vb >= 0);
+      // values that no column sees become 0; NaN among the others are
+      // taken out of the product and put back where they are seen
+      uint32_t keep[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) keep[t] = kept(base, t, ub, ue);
-        bool any = false;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            vv[d][t] &= keep[t];
-            any |= nan_code(vv[d][t]);
-          }
-        bad = __ballot(any) != 0;
-        if (bad) {
-#pragma unroll
-          for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) vv[d][t] = no_nan(vv[d][t]);
-        }
-      }
-      const int grown = max(unit, over_groups(ve));
-      const int k = max(ve - grown, kDeep), f = ve - grown - k;
-      const float vk = pow2(k);
-      tok_u32x4 pf[2][NP];
-      soften<DT, NP>(s, cg, f, __ballot(f < 0) != 0, pow2(unit - grown), m, l, acc, pf);
-      unit = grown;
+      for (int t = 0; t < 4; ++t) keep[t] = kept(base, t, ub, ue);
+      bool any = false;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const tok_u32x4 vf = codes_f16(vv[d][2 * u], vv[d][2 * u + 1], vk);
-#pragma unroll
-          for (int n = 0; n < NP; ++n) acc[d] = mfma_f16(vf, pf[u][n], acc[d]);
+        for (int t = 0; t < 4; ++t) {
+          vv[d][t] &= keep[t];
+          any |= nan_code(vv[d][t]);
         }
-      if (bad) put_nan<DT>(a, vb, tok0, g, mine, acc);
+      bad = __ballot(any) != 0;
+      if (bad) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) vv[d][t] = no_nan(vv[d][t]);
+      }
     }
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    l *= pow2(-kLift);
+    const int grown = max(unit, over_groups(ve));
+    const int k = max(ve - grown, kDeep), f = ve - grown - k;
+    const float vk = pow2(k);
+    tok_u32x4 pf[2][NP];
+    soften<DT, NP>(s, cg, f, __ballot(f < 0) != 0, pow2(unit - grown), m, l, acc, pf);
+    unit = grown;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[d][i] = ldexpf(acc[d][i], unit - kLift);
+      for (int u = 0; u < 2; ++u) {
+        const tok_u32x4 vf = codes_f16(vv[d][2 * u], vv[d][2 * u + 1], vk);
+#pragma unroll
+        for (int n = 0; n < NP; ++n) acc[d] = mfma_f16(vf, pf[u][n], acc[d]);
+      }
+    if (bad) put_nan<DT>(a, vb, tok0, g, mine, acc);
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  l *= pow2(-kLift);
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[d][i] = ldexpf(acc[d][i], unit - kLift);
 
-    // join the waves: the weights of their results, then 4 rows of sums
-    if (g == 0) {
-      sm[wave][r] = m;
-      sl[wave][r] = l;
-    }
+  // join the waves: the weights of their results, then 4 rows of sums
+  if (g == 0) {
+    sm[wave][r] = m;
+    sl[wave][r] = l;
+  }
 #pragma unroll
-    for (int d = 0; d < DT; ++d) *reinterpret_cast<tok_f32x4*>(&so[wave][r][d * 16 + g * 4]) = acc[d];
-    __syncthreads();
-    // 16 threads a column
-    const int oc = threadIdx.x >> 4, ol = threadIdx.x & 15;
-    float all = fmaxf(fmaxf(sm[0][oc], sm[1][oc]), fmaxf(sm[2][oc], sm[3][oc])), w[4], sum = 0.f;
-    const float ref = all == -kInf ? 0.f : all;
+  for (int d = 0; d < DT; ++d) *reinterpret_cast<tok_f32x4*>(&so[wave][r][d * 16 + g * 4]) = acc[d];
+  __syncthreads();
+  // 16 threads a column
+  const int oc = threadIdx.x >> 4, ol = threadIdx.x & 15;
+  float all = fmaxf(fmaxf(sm[0][oc], sm[1][oc]), fmaxf(sm[2][oc], sm[3][oc])), w[4], sum = 0.f;
+  const float ref = all == -kInf ? 0.f : all;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[i] = __builtin_amdgcn_exp2f(sm[i][oc] - ref);
-      sum += w[i] * sl[i][oc];
-    }
-    if (col0 + oc < columns) {
-      const int64_t oi = (col0 + oc) / G, oh = hk * G + (col0 + oc) % G;
-      const int64_t row = (q.row0 + oi) * a.q_heads + oh;
-      float* part = splits > 1 ? a.part + (static_cast<int64_t>(split) * a.b.T * a.q_heads + row) * (D + 2) : nullptr;
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      for (int d = ol; d < D; d += 16) {
-        float o = 0.f;
+  for (int i = 0; i < 4; ++i) {
+    w[i] = __builtin_amdgcn_exp2f(sm[i][oc] - ref);
+    sum += w[i] * sl[i][oc];
+  }
+  if (oc >= columns) return;
+  const int64_t row = static_cast<int64_t>(q.row0 + oc / G) * a.q_heads + hk * G + oc % G;
+  float* part = a.splits > 1 ? a.part + (static_cast<int64_t>(split) * a.T * a.q_heads + row) * (D + 2) : nullptr;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  for (int d = ol; d < D; d += 16) {
+    float o = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o += w[i] * so[i][oc][d];
-        if (part)
-          part[2 + d] = o;
-        else
-          static_cast<S*>(a.out)[row * D + d] = E::narrow(o * inv);
-      }
-      if (ol == 0) {
-        if (part) {
-          part[0] = all;
-          part[1] = sum;
-        } else if (a.lse) {
-          a.lse[row] = sum == 0.f ? -kInf : all * kLn2 + logf(sum);
-        }
-      }
+    for (int i = 0; i < 4; ++i) o += w[i] * so[i][oc][d];
+    if (part)
+      part[2 + d] = o;
+    else
+      static_cast<S*>(a.out)[row * D + d] = E::narrow(o * inv);
+  }
+  if (ol == 0) {
+    if (part) {
+      part[0] = all;
+      part[1] = sum;
+    } else if (a.lse) {
+      a.lse[row] = sum == 0.f ? -kInf : all * kLn2 + logf(sum);
     }
-    __syncthreads();
   }
 }
 
@@ -452,7 +459,7 @@ typedef __attribute__((address_space(1))) const void global_void;
 // reads have no bank conflicts), two tiles in turn; every wave converts the
 // fragments that it multiplies with its CT column tiles.
 template <class E, int DP, int CT>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(AttendArgs a, int splits, int split_tiles, int coltiles) {
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   typedef Form<E> F;
   typedef typename E::store S;
   constexpr int KS = DP / 32, DT = DP / 16, NJ = DP / 64, NQ = F::NQ, NP = F::NP;
@@ -464,208 +471,201 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(AttendArgs
   // workgroup i runs on L2 cache i % 8: each cache gets a run of consecutive
   // units, so that one cache reads a head's codes; the last columns, which see
   // most in a causal call, come first
-  const int heads = static_cast<int>(a.c.heads), D = static_cast<int>(a.c.dim);
-  int64_t id = blockIdx.x;
+  const int D = a.D, G = a.G;
+  uint32_t id = blockIdx.x;
   {
-    const int64_t total = gridDim.x, each = total / 8, rest = total % 8, c = id % 8;
+    const uint32_t total = gridDim.x, each = total / 8, rest = total % 8, c = id % 8;
     id = c * each + (c < rest ? c : rest) + id / 8;
   }
-  const int ct = coltiles - 1 - static_cast<int>(id % coltiles);
-  id /= coltiles;
-  const int split = static_cast<int>(id % splits);
-  id /= splits;
-  const int hk = static_cast<int>(id % heads);
-  const int64_t b = id / heads;
-  const int G = static_cast<int>(a.q_heads) / heads;
+  const int ct = a.coltiles - 1 - static_cast<int>(id % a.coltiles);
+  id /= a.coltiles;
+  const int split = static_cast<int>(id % a.splits);
+  id /= a.splits;
+  const int hk = static_cast<int>(id % a.heads), b = static_cast<int>(id / a.heads);
   const Seq q = sequence(a, b);
-  const int64_t columns = static_cast<int64_t>(q.n) * G;
-  const Find find = finder(a, b, hk);
-  const float c = a.scale * kLog2e;
   constexpr int WG = 64 * CT;  // columns
+  const int columns = q.n * G, wg0 = ct * WG;
+  if (wg0 >= columns) return;
+  // what the workgroup's columns see together, and what this wave's do
+  auto sight_of = [&](int col) { return sight(a, q.len, q.start + (col < columns ? col : columns - 1) / G); };
+  const int ub = sight_of(wg0).begin, ue = sight_of(wg0 + WG - 1).end;
+  const int col0 = wg0 + wave * 16 * CT;
+  const Sight wlo = sight_of(col0), whi = sight_of(col0 + 16 * CT - 1);
+  const int t0 = ub / 64 + split * a.split_tiles;
+  int t1 = (ue + 63) / 64;
+  if (split + 1 < a.splits && t0 + a.split_tiles < t1) t1 = t0 + a.split_tiles;
 
-  for (int64_t wg0 = static_cast<int64_t>(ct) * WG; wg0 < columns; wg0 += static_cast<int64_t>(coltiles) * WG) {
-    // what the workgroup's columns see together, and what this wave's do
-    auto sight_of = [&](int64_t col) { return sight(a, q.len, q.start + static_cast<int>((col < columns ? col : columns - 1) / G)); };
-    const int ub = sight_of(wg0).begin, ue = sight_of(wg0 + WG - 1).end;
-    const int64_t col0 = wg0 + wave * 16 * CT;
-    const Sight wlo = sight_of(col0), whi = sight_of(col0 + 16 * CT - 1);
-    const int t0 = ub / 64 + split * split_tiles;
-    int t1 = (ue + 63) / 64;
-    if (split + 1 < splits && t0 + split_tiles < t1) t1 = t0 + split_tiles;
+  tok_u32x4 qf[CT][KS][NQ];
+  Sight mine[CT];
+  tok_f32x4 acc[CT][DT];
+  float m[CT], l[CT];
+#pragma unroll
+  for (int x = 0; x < CT; ++x) {
+    const int col = col0 + 16 * x + r < columns ? col0 + 16 * x + r : columns - 1;
+    const int qi = col / G, qh = hk * G + col % G;
+    mine[x] = sight(a, q.len, q.start + qi);
+    load_query<E, KS>(a, q.row0 + qi, qh, g, qf[x]);
+    m[x] = -kInf;
+    l[x] = 0.f;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[x][d] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  int unit = -126;
 
-    tok_u32x4 qf[CT][KS][NQ];
-    Sight mine[CT];
-    tok_f32x4 acc[CT][DT];
-    float m[CT], l[CT];
+  // a tile on its way: this lane's blocks of K rows and of V
+  struct Ids {
+    int64_t kb, vb;
+  };
+  auto ids = [&](int tile) { return Ids{find(a, b, hk, tile * 4 + (r >> 2), ue), find(a, b, hk, tile * 4 + g, ue)}; };
+  auto fetch = [&](const Ids& i, int buf) __attribute__((always_inline)) {
+    const uint8_t* kp = a.k + (i.kb * 16 + (r & 3)) * D + g * 16;
+    const uint8_t* vp = a.v + (i.vb * D + r) * 16;
 #pragma unroll
-    for (int x = 0; x < CT; ++x) {
-      const int64_t col = col0 + 16 * x + r < columns ? col0 + 16 * x + r : columns - 1;
-      const int qi = static_cast<int>(col / G), qh = hk * G + static_cast<int>(col % G);
-      mine[x] = sight(a, q.len, q.start + qi);
-      load_query<E, KS>(a, q.row0 + qi, qh, g, qf[x]);
-      m[x] = -kInf;
-      l[x] = 0.f;
-#pragma unroll
-      for (int d = 0; d < DT; ++d) acc[x][d] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < NF / 4; ++n) {
+      const int f = n * 4 + wave;
+      const bool isk = n < NJ;
+      const int t = f / NJ, j = f - t * NJ, d = f - 4 * NJ;
+      const bool ok = isk ? i.kb >= 0 && j * 64 + g * 16 < D : i.vb >= 0 && d * 16 < D;
+      const uint8_t* p = isk ? kp + 4 * t * D + j * 64 : vp + d * 256;
+      __builtin_amdgcn_global_load_lds((global_void*)(ok ? p : reinterpret_cast<const uint8_t*>(kZeros)),
+                                       (lds_void*)(&lds[buf][f * 1024]), 16, 0, 0);
     }
-    int unit = -126;
+  };
 
-    // a tile on its way: this lane's blocks of K rows and of V
-    struct Ids {
-      int64_t kb, vb;
-    };
-    auto ids = [&](int tile) { return Ids{find(tile * 4 + (r >> 2), ue), find(tile * 4 + g, ue)}; };
-    auto fetch = [&](const Ids& i, int buf) __attribute__((always_inline)) {
-      const uint8_t* kp = static_cast<const uint8_t*>(a.c.k) + (i.kb * 16 + (r & 3)) * D + g * 16;
-      const uint8_t* vp = static_cast<const uint8_t*>(a.c.v) + (i.vb * D + r) * 16;
-#pragma unroll
-      for (int n = 0; n < NF / 4; ++n) {
-        const int f = n * 4 + wave;
-        const bool isk = f < 4 * NJ;
-        const int t = f / NJ, j = f % NJ, d = f - 4 * NJ;
-        const bool ok = isk ? i.kb >= 0 && j * 64 + g * 16 < D : i.vb >= 0 && d * 16 < D;
-        const uint8_t* p = isk ? kp + 4 * t * D + j * 64 : vp + d * 256;
-        __builtin_amdgcn_global_load_lds((global_void*)(ok ? p : reinterpret_cast<const uint8_t*>(kZeros)),
-                                         (lds_void*)(&lds[buf][f * 1024]), 16, 0, 0);
-      }
-    };
-
-    Ids cur{-1, -1}, nxt{-1, -1};
-    float ks = 1.f, vs = 1.f;
-    auto scales = [&](const Ids& i, float& k, float& v) {
-      k = i.vb >= 0 ? a.c.k_scale[i.vb] : 1.f;
-      v = i.vb >= 0 ? a.c.v_scale[i.vb] : 0x1p-126f;
-    };
-    if (t0 < t1) {
-      cur = ids(t0);
-      fetch(cur, 0);
-      scales(cur, ks, vs);
-      nxt = ids(t0 + 1);
+  Ids cur{-1, -1}, nxt{-1, -1};
+  float ks = 1.f, vs = 1.f;
+  auto scales = [&](const Ids& i, float& k, float& v) {
+    k = i.vb >= 0 ? a.ks[i.vb] : 1.f;
+    v = i.vb >= 0 ? a.vs[i.vb] : 0x1p-126f;
+  };
+  if (t0 < t1) {
+    cur = ids(t0);
+    fetch(cur, 0);
+    scales(cur, ks, vs);
+    nxt = ids(t0 + 1);
+  }
+  for (int tile = t0; tile < t1; ++tile) {
+    const int buf = (tile - t0) & 1, tok0 = tile * 64;
+    __syncthreads();  // this tile is in LDS, and nobody reads the other buffer
+    float ks1 = 1.f, vs1 = 1.f;
+    Ids far = nxt;
+    if (tile + 1 < t1) {
+      fetch(nxt, buf ^ 1);
+      scales(nxt, ks1, vs1);
+      far = ids(tile + 2);
     }
-    for (int tile = t0; tile < t1; ++tile) {
-      const int buf = (tile - t0) & 1, tok0 = tile * 64;
-      __syncthreads();  // this tile is in LDS, and nobody reads the other buffer
-      float ks1 = 1.f, vs1 = 1.f;
-      Ids far = nxt;
-      if (tile + 1 < t1) {
-        fetch(nxt, buf ^ 1);
-        scales(nxt, ks1, vs1);
-        far = ids(tile + 2);
-      }
-      const uint8_t* frag = &lds[buf][lane * 16];
-      auto read = [&](int f) { return *reinterpret_cast<const tok_u32x4*>(frag + f * 1024); };
-      if (tok0 < whi.end && tok0 + 64 > wlo.begin) {
-        const float cg = fmaxf(c * ks, 0x1p-126f);
-        const int ve = exponent_of(vs);
-        tok_f32x4 s[CT][4];
+    const uint8_t* frag = &lds[buf][lane * 16];
+    auto read = [&](int f) { return *reinterpret_cast<const tok_u32x4*>(frag + f * 1024); };
+    if (tok0 < whi.end && tok0 + 64 > wlo.begin) {
+      const float cg = fmaxf(a.c * ks, 0x1p-126f);
+      const int ve = exponent_of(vs);
+      tok_f32x4 s[CT][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+      for (int t = 0; t < 4; ++t) {
 #pragma unroll
-          for (int x = 0; x < CT; ++x) s[x][t] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < CT; ++x) s[x][t] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) {
-            const tok_u32x4 kv = read(t * NJ + j);
+        for (int j = 0; j < NJ; ++j) {
+          const tok_u32x4 kv = read(t * NJ + j);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const tok_u32x4 kf = F::k(kv[2 * h], kv[2 * h + 1]);
+          for (int h = 0; h < 2; ++h) {
+            const tok_u32x4 kf = F::k(kv[2 * h], kv[2 * h + 1]);
 #pragma unroll
-              for (int x = 0; x < CT; ++x)
+            for (int x = 0; x < CT; ++x)
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) s[x][t] = F::mfma(kf, qf[x][2 * j + h][n], s[x][t]);
-            }
+              for (int n = 0; n < NQ; ++n) s[x][t] = F::mfma(kf, qf[x][2 * j + h][n], s[x][t]);
           }
         }
-        const bool edge = tok0 < whi.begin || tok0 + 64 > wlo.end || __ballot(cur.vb < 0) != 0;
-        const int base = tok0 + 16 * g;
-        uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
-        bool bad = false;
-        if (edge) {
-#pragma unroll
-          for (int x = 0; x < CT; ++x) hide(s[x], base, mine[x], cur.vb >= 0);
-#pragma unroll
-          for (int t = 0; t < 4; ++t) keep[t] = kept(base, t, wlo.begin, whi.end);
-          bool any = false;
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const tok_u32x4 v = read(4 * NJ + d);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) any |= nan_code(v[t] & keep[t]);
-          }
-          bad = __ballot(any) != 0;
-        }
-        const int grown = max(unit, over_groups(ve));
-        const int k = max(ve - grown, kDeep), f = ve - grown - k;
-        const float vk = pow2(k), shrink = pow2(unit - grown);
-        const bool low = __ballot(f < 0) != 0;
-        unit = grown;
-        tok_u32x4 pf[CT][2][NP];
-#pragma unroll
-        for (int x = 0; x < CT; ++x) soften<DT, NP>(s[x], cg, f, low, shrink, m[x], l[x], acc[x], pf[x]);
-        auto second = [&](bool clean) __attribute__((always_inline)) {
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            tok_u32x4 v = read(4 * NJ + d);
-            if (!clean) {
-#pragma unroll
-              for (int t = 0; t < 4; ++t) v[t] = no_nan(v[t] & keep[t]);
-            }
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const tok_u32x4 vf = codes_f16(v[2 * u], v[2 * u + 1], vk);
-#pragma unroll
-              for (int x = 0; x < CT; ++x)
-#pragma unroll
-                for (int n = 0; n < NP; ++n) acc[x][d] = mfma_f16(vf, pf[x][u][n], acc[x][d]);
-            }
-          }
-        };
-        if (edge)
-          second(false);
-        else
-          second(true);
-        if (bad) {
-#pragma unroll
-          for (int x = 0; x < CT; ++x) put_nan<DT>(a, cur.vb, tok0, g, mine[x], acc[x]);
-        }
       }
-      cur = nxt;
-      nxt = far;
-      ks = ks1;
-      vs = vs1;
+      const bool edge = tok0 < whi.begin || tok0 + 64 > wlo.end || __ballot(cur.vb < 0) != 0;
+      const int base = tok0 + 16 * g;
+      uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
+      bool bad = false;
+      if (edge) {
+#pragma unroll
+        for (int x = 0; x < CT; ++x) hide(s[x], base, mine[x], cur.vb >= 0);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) keep[t] = kept(base, t, wlo.begin, whi.end);
+        bool any = false;
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          const tok_u32x4 v = read(4 * NJ + d);
+#pragma unroll
+          for (int t = 0; t < 4; ++t) any |= nan_code(v[t] & keep[t]);
+        }
+        bad = __ballot(any) != 0;
+      }
+      const int grown = max(unit, over_groups(ve));
+      const int k = max(ve - grown, kDeep), f = ve - grown - k;
+      const float vk = pow2(k), shrink = pow2(unit - grown);
+      const bool low = __ballot(f < 0) != 0;
+      unit = grown;
+      tok_u32x4 pf[CT][2][NP];
+#pragma unroll
+      for (int x = 0; x < CT; ++x) soften<DT, NP>(s[x], cg, f, low, shrink, m[x], l[x], acc[x], pf[x]);
+      auto second = [&](bool clean) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          tok_u32x4 v = read(4 * NJ + d);
+          if (!clean) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) v[t] = no_nan(v[t] & keep[t]);
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const tok_u32x4 vf = codes_f16(v[2 * u], v[2 * u + 1], vk);
+#pragma unroll
+            for (int x = 0; x < CT; ++x)
+#pragma unroll
+              for (int n = 0; n < NP; ++n) acc[x][d] = mfma_f16(vf, pf[x][u][n], acc[x][d]);
+          }
+        }
+      };
+      if (edge)
+        second(false);
+      else
+        second(true);
+      if (bad) {
+#pragma unroll
+        for (int x = 0; x < CT; ++x) put_nan<DT>(a, cur.vb, tok0, g, mine[x], acc[x]);
+      }
     }
-    __syncthreads();  // before another round's first tile
+    cur = nxt;
+    nxt = far;
+    ks = ks1;
+    vs = vs1;
+  }
 
 #pragma unroll
-    for (int x = 0; x < CT; ++x) {
-      float sum = l[x];
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
-      sum *= pow2(-kLift);
-      const int64_t col = col0 + 16 * x + r;
-      if (col >= columns) continue;
-      const int64_t row = (q.row0 + col / G) * a.q_heads + hk * G + col % G;
-      float* part = splits > 1 ? a.part + (static_cast<int64_t>(split) * a.b.T * a.q_heads + row) * (D + 2) : nullptr;
-      const float inv = part ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+  for (int x = 0; x < CT; ++x) {
+    float sum = l[x];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    sum *= pow2(-kLift);
+    const int col = col0 + 16 * x + r;
+    if (col >= columns) continue;
+    const int64_t row = static_cast<int64_t>(q.row0 + col / G) * a.q_heads + hk * G + col % G;
+    float* part = a.splits > 1 ? a.part + (static_cast<int64_t>(split) * a.T * a.q_heads + row) * (D + 2) : nullptr;
+    const float inv = part ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        if (d * 16 >= D) continue;
-        float o[4];
+    for (int d = 0; d < DT; ++d) {
+      if (d * 16 >= D) continue;
+      float o[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = ldexpf(acc[x][d][i], unit - kLift) * inv;
-        if (part) {
-          __builtin_memcpy(part + 2 + d * 16 + g * 4, o, 16);
-        } else {
-          S v[4] = {E::narrow(o[0]), E::narrow(o[1]), E::narrow(o[2]), E::narrow(o[3])};
-          __builtin_memcpy(static_cast<S*>(a.out) + row * D + d * 16 + g * 4, v, sizeof v);
-        }
+      for (int i = 0; i < 4; ++i) o[i] = ldexpf(acc[x][d][i], unit - kLift) * inv;
+      if (part) {
+        __builtin_memcpy(part + 2 + d * 16 + g * 4, o, 16);
+      } else {
+        S v[4] = {E::narrow(o[0]), E::narrow(o[1]), E::narrow(o[2]), E::narrow(o[3])};
+        __builtin_memcpy(static_cast<S*>(a.out) + row * D + d * 16 + g * 4, v, sizeof v);
       }
-      if (g == 0) {
-        if (part) {
-          part[0] = m[x];
-          part[1] = sum;
-        } else if (a.lse) {
-          a.lse[row] = sum == 0.f ? -kInf : m[x] * kLn2 + logf(sum);
-        }
+    }
+    if (g == 0) {
+      if (part) {
+        part[0] = m[x];
+        part[1] = sum;
+      } else if (a.lse) {
+        a.lse[row] = sum == 0.f ? -kInf : m[x] * kLn2 + logf(sum);
       }
     }
   }
@@ -673,17 +673,17 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(AttendArgs
 
 // out and lse from the partial results of a split call: one wave a row.
 template <class E>
-__global__ __launch_bounds__(256) void attend_join(AttendArgs a, int splits) {
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6), rows = a.b.T * a.q_heads;
+__global__ __launch_bounds__(256) void attend_join(Dev a) {
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6), rows = static_cast<int64_t>(a.T) * a.q_heads;
   if (row >= rows) return;
-  const int lane = threadIdx.x & 63, D = static_cast<int>(a.c.dim);
+  const int lane = threadIdx.x & 63, D = a.D;
   const float* part = a.part + row * (D + 2);
   const int64_t step = rows * (D + 2);
   float m = -kInf;
-  for (int s = 0; s < splits; ++s) m = fmaxf(m, part[s * step]);
+  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, part[s * step]);
   const float ref = m == -kInf ? 0.f : m;
   float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
+  for (int s = 0; s < a.splits; ++s) {
     const float part_l = part[s * step + 1];
     if (part_l == 0.f) continue;  // nothing seen
     const float w = __builtin_amdgcn_exp2f(part[s * step] - ref);
@@ -719,33 +719,37 @@ int64_t workgroup_columns(int64_t dim, int dtype) {
 bool few(int64_t columns) { return columns <= 16; }
 
 template <class E>
-hipError_t run(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s) {
-  const int64_t columns = a.b.max_new * (a.q_heads / a.c.heads);
-  const int64_t split_tiles = up(tiles_seen(a.b, a.c.page, a.window), p.splits);
+hipError_t run(const AttendArgs& h, const AttendPlan& p, int dtype, hipStream_t s) {
+  const int64_t G = h.q_heads / h.c.heads, columns = h.b.max_new * G, nb = h.c.page / 16;
+  const int64_t cap = h.b.cols * h.c.page, coltiles = up(columns, workgroup_columns(h.c.dim, dtype));
+  const int64_t blocks = coltiles * p.splits * h.c.heads * h.b.B, joins = up(h.b.T * h.q_heads, 4);
+  // 32-bit numbering of columns (of T rows at most), workgroups and grids
+  if (up(h.b.T * G, 16) * 16 + 1024 > 0x7fffffff || columns > 0x7fffffff - 1024 || joins > 0x7fffffff ||
+      (few(columns) ? h.b.B > 65535 || h.c.heads > 65535 : blocks > 0x7fffffff))
+    return hipErrorInvalidConfiguration;
+  const Dev a{static_cast<const uint8_t*>(h.c.k), static_cast<const uint8_t*>(h.c.v), h.c.k_scale, h.c.v_scale,
+              h.b.table, h.b.cu, h.b.len, h.q, h.out, h.lse, h.part, h.ld_q,
+              static_cast<int>(h.b.T), static_cast<int>(h.q_heads), static_cast<int>(h.c.heads), static_cast<int>(G),
+              static_cast<int>(h.c.dim), static_cast<int>(h.c.pages), static_cast<int>(nb),
+              (nb & (nb - 1)) == 0 ? __builtin_ctzll(nb) : -1, static_cast<int>(h.b.cols),
+              // room for the tile arithmetic past the last token
+              static_cast<int>(cap < 0x7fff0000 ? cap : 0x7fff0000), h.causal, static_cast<int>(h.window),
+              h.scale * kLog2e, p.splits, static_cast<int>(up(tiles_seen(h.b, h.c.page, h.window), p.splits)),
+              static_cast<int>(coltiles)};
   if (few(columns)) {
-    if (a.b.B > 65535 || a.c.heads > 65535) return hipErrorInvalidConfiguration;
-    auto k = a.c.dim <= 64    ? attend_few<E, 64>
-             : a.c.dim <= 128 ? attend_few<E, 128>
-             : a.c.dim <= 192 ? attend_few<E, 192>
-                              : attend_few<E, 256>;
-    hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(p.splits), static_cast<unsigned>(a.c.heads), static_cast<unsigned>(a.b.B)),
-                       dim3(256), 0, s, a, p.splits, static_cast<int>(split_tiles), 1);
+    auto k = a.D <= 64 ? attend_few<E, 64> : a.D <= 128 ? attend_few<E, 128> : a.D <= 192 ? attend_few<E, 192> : attend_few<E, 256>;
+    hipLaunchKernelGGL(k, dim3(p.splits, a.heads, static_cast<unsigned>(h.b.B)), dim3(256), 0, s, a);
   } else {
-    const int64_t coltiles = up(columns, workgroup_columns(a.c.dim, dtype)), blocks = coltiles * p.splits * a.c.heads * a.b.B;
-    if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
     constexpr int NQ = Form<E>::NQ;
-    auto k = a.c.dim <= 64    ? attend_many<E, 64, column_tiles(64, NQ)>
-             : a.c.dim <= 128 ? attend_many<E, 128, column_tiles(128, NQ)>
-             : a.c.dim <= 192 ? attend_many<E, 192, column_tiles(192, NQ)>
-                              : attend_many<E, 256, column_tiles(256, NQ)>;
-    hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a, p.splits, static_cast<int>(split_tiles),
-                       static_cast<int>(coltiles));
+    auto k = a.D <= 64    ? attend_many<E, 64, column_tiles(64, NQ)>
+             : a.D <= 128 ? attend_many<E, 128, column_tiles(128, NQ)>
+             : a.D <= 192 ? attend_many<E, 192, column_tiles(192, NQ)>
+                          : attend_many<E, 256, column_tiles(256, NQ)>;
+    hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
   }
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.splits > 1) {
-    const int64_t jb = up(a.b.T * a.q_heads, 4);
-    if (jb > 0x7fffffff) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(attend_join<E>, dim3(static_cast<unsigned>(jb)), dim3(256), 0, s, a, p.splits);
+    hipLaunchKernelGGL(attend_join<E>, dim3(static_cast<unsigned>(joins)), dim3(256), 0, s, a);
     e = hipGetLastError();
   }
   return e;
