@@ -161,13 +161,14 @@ __device__ inline Seq sequence(const Dev& a, int b) {
 }
 
 // Index among the cache's 16-token blocks (of head hk) of block blk of
-// sequence b, or -1 where it has no page or begins at `end` or later.
-__device__ inline int64_t find(const Dev& a, int b, int hk, int blk, int end) {
+// sequence b, or kNone where it has no page or begins at `end` or later.
+constexpr uint32_t kNone = 0xffffffffu;
+__device__ inline uint32_t find(const Dev& a, int b, int hk, int blk, int end) {
   const int col = a.pow >= 0 ? blk >> a.pow : blk / a.nb;
-  if (blk * 16 >= end || col >= a.cols) return -1;
-  const int page = a.table[static_cast<int64_t>(b) * a.cols + col];
-  if (page < 0 || page >= a.pages) return -1;
-  return (static_cast<int64_t>(page) * a.heads + hk) * a.nb + (blk - col * a.nb);
+  if (blk * 16 >= end || col >= a.cols) return kNone;
+  const uint32_t page = a.table[static_cast<int64_t>(b) * a.cols + col];
+  if (page >= static_cast<uint32_t>(a.pages)) return kNone;
+  return (page * a.heads + hk) * a.nb + (blk - col * a.nb);
 }
 
 // v, as a value that the compiler cannot compute with ahead of time: keeps
@@ -217,15 +218,15 @@ __device__ inline uint32_t kept(int base, int t, int ub, int ue) {
 // NaN that were taken out of an edge tile's values come back to the channels
 // of the columns that see them.  vb: this lane's block.
 template <int DT>
-__device__ inline void put_nan(const Dev& a, int64_t vb, int tok0, int g, const Sight& mine, tok_f32x4 (&acc)[DT]) {
+__device__ inline void put_nan(const Dev& a, uint32_t vb, int tok0, int g, const Sight& mine, tok_f32x4 (&acc)[DT]) {
   const int D = apart(a.D);
   for (int o = 0; o < 4; ++o) {
-    const int64_t ob = __shfl(vb, 16 * o);
-    if (ob < 0) continue;
+    const uint32_t ob = __shfl(vb, 16 * o);
+    if (ob == kNone) continue;
     for (int t = 0; t < 16; ++t) {
       const int tok = tok0 + 16 * o + t;
       if (tok < mine.begin || tok >= mine.end) continue;
-      const uint8_t* v = a.v + (ob * D + g * 4) * 16 + t;
+      const uint8_t* v = a.v + (static_cast<int64_t>(ob) * D + g * 4) * 16 + t;
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         if (d * 16 >= D) break;
@@ -328,24 +329,25 @@ __global__ __launch_bounds__(256) void attend_few(Dev a) {
 
   for (int tile = t0 + wave; tile < t1; tile += 4) {
     const int blk0 = tile * 4, tok0 = tile * 64;
-    const int64_t kb = find(a, b, hk, blk0 + (r >> 2), ue), vb = find(a, b, hk, blk0 + g, ue);
-    const uint8_t* kp = a.k + (kb * 16 + (r & 3)) * D + g * 16;
-    const uint8_t* vp = a.v + (vb * D + r) * 16;
+    const uint32_t vb = find(a, b, hk, blk0 + g, ue), kb = __shfl(vb, (r >> 2) * 16);
+    const bool kok = kb != kNone, vok = vb != kNone;
+    const uint8_t* kp = a.k + (static_cast<int64_t>(kb) * 16 + (r & 3)) * D + g * 16;
+    const uint8_t* vp = a.v + (static_cast<int64_t>(vb) * D + r) * 16;
     // scales of block g; c times the key's, 0 kept off so that -inf stays -inf
-    const float cg = vb >= 0 ? fmaxf(a.c * a.ks[vb], 0x1p-126f) : 1.f;
-    const int ve = vb >= 0 ? exponent_of(a.vs[vb]) : -126;
+    const float cg = vok ? fmaxf(a.c * a.ks[vb], 0x1p-126f) : 1.f;
+    const int ve = vok ? exponent_of(a.vs[vb]) : -126;
     tok_u32x4 kv[4][DP / 64], vv[DT];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int j = 0; j < DP / 64; ++j) {
         kv[t][j] = tok_u32x4{0, 0, 0, 0};
-        if (kb >= 0 && j * 64 + g * 16 < D) kv[t][j] = *reinterpret_cast<const tok_u32x4*>(kp + 4 * t * D + j * 64);
+        if (kok && j * 64 + g * 16 < D) kv[t][j] = *reinterpret_cast<const tok_u32x4*>(kp + 4 * t * D + j * 64);
       }
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
       vv[d] = tok_u32x4{0, 0, 0, 0};
-      if (vb >= 0 && d * 16 < D) vv[d] = *reinterpret_cast<const tok_u32x4*>(vp + d * 256);
+      if (vok && d * 16 < D) vv[d] = *reinterpret_cast<const tok_u32x4*>(vp + d * 256);
     }
     tok_f32x4 s[4];
 #pragma unroll
@@ -359,11 +361,11 @@ __global__ __launch_bounds__(256) void attend_few(Dev a) {
       }
     }
     // a tile that some column sees in part only, or with a page missing
-    const bool edge = tok0 < cb || tok0 + 64 > ce || __ballot(vb < 0) != 0;
+    const bool edge = tok0 < cb || tok0 + 64 > ce || __ballot(!vok) != 0;
     bool bad = false;
     if (edge) {
       const int base = tok0 + 16 * g;
-      hide(s, base, mine, vb >= 0);
+      hide(s, base, mine, vok);
       // values that no column sees become 0; NaN among the others are
       // taken out of the product and put back where they are seen
       uint32_t keep[4];
@@ -454,18 +456,22 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
 // One workgroup: 4 waves of CT column tiles each, one sequence, one key/value
-// head, one split of the tokens.  The codes of a 64-token tile come straight
+// head, one split of the tokens.  K's codes of a 64-token tile come straight
 // into LDS, fragment by fragment (1 KB each: a lane's 16 bytes side by side, so
-// reads have no bank conflicts), two tiles in turn; every wave converts the
-// fragments that it multiplies with its CT column tiles.
+// reads have no bank conflicts), and every wave converts the fragments that
+// it multiplies.  V's go through registers: each wave converts a quarter of
+// them to f16 for all.  Two tiles in turn.  What bounds it is the vector
+// units: conversions and exponentials beside the products; that is why V is
+// converted once (K too would make LDS reads the bound).
 template <class E, int DP, int CT>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   typedef Form<E> F;
   typedef typename E::store S;
   constexpr int KS = DP / 32, DT = DP / 16, NJ = DP / 64, NQ = F::NQ, NP = F::NP;
-  constexpr int NF = 4 * NJ + DT;  // fragments of a tile
-  static_assert(NF % 4 == 0, "whole rounds of waves");
-  __shared__ __align__(16) uint8_t lds[2][NF * 1024];
+  constexpr int VW = DT / 4;  // V fragments that a wave converts
+  __shared__ __align__(16) uint8_t kbuf[2][4 * NJ * 1024];
+  __shared__ __align__(16) uint8_t vbuf[2][DT * 2048];
+  __shared__ int nan_seen[2][4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, g = lane >> 4;
   // workgroup i runs on L2 cache i % 8: each cache gets a run of consecutive
@@ -488,7 +494,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   if (wg0 >= columns) return;
   // what the workgroup's columns see together, and what this wave's do
   auto sight_of = [&](int col) { return sight(a, q.len, q.start + (col < columns ? col : columns - 1) / G); };
-  const int ub = sight_of(wg0).begin, ue = sight_of(wg0 + WG - 1).end;
+  const Sight lo = sight_of(wg0), hi = sight_of(wg0 + WG - 1);
+  const int ub = lo.begin, ue = hi.end;
   const int col0 = wg0 + wave * 16 * CT;
   const Sight wlo = sight_of(col0), whi = sight_of(col0 + 16 * CT - 1);
   const int t0 = ub / 64 + split * a.split_tiles;
@@ -510,130 +517,133 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[x][d] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  int unit = -126;
-
-  // a tile on its way: this lane's blocks of K rows and of V
-  struct Ids {
-    int64_t kb, vb;
-  };
-  auto ids = [&](int tile) { return Ids{find(a, b, hk, tile * 4 + (r >> 2), ue), find(a, b, hk, tile * 4 + g, ue)}; };
-  auto fetch = [&](const Ids& i, int buf) __attribute__((always_inline)) {
-    const uint8_t* kp = a.k + (i.kb * 16 + (r & 3)) * D + g * 16;
-    const uint8_t* vp = a.v + (i.vb * D + r) * 16;
+  // Tiles on their way: block g of the tile of this lane, its scales, K in
+  // LDS, this wave's part of V in registers.
+  auto block = [&](int tile) { return find(a, b, hk, tile * 4 + g, ue); };
+  tok_u32x4 vr[VW];
+  auto fetch = [&](uint32_t vb, int buf) __attribute__((always_inline)) {
+    const uint32_t kb = __shfl(vb, (r >> 2) * 16);
+    const uint8_t* zeros = reinterpret_cast<const uint8_t*>(kZeros);
+    const uint8_t* kp = a.k + (static_cast<int64_t>(kb) * 16 + (r & 3)) * D + g * 16;
+    const uint8_t* vp = a.v + (static_cast<int64_t>(vb) * D + r) * 16;
 #pragma unroll
-    for (int n = 0; n < NF / 4; ++n) {
-      const int f = n * 4 + wave;
-      const bool isk = n < NJ;
-      const int t = f / NJ, j = f - t * NJ, d = f - 4 * NJ;
-      const bool ok = isk ? i.kb >= 0 && j * 64 + g * 16 < D : i.vb >= 0 && d * 16 < D;
-      const uint8_t* p = isk ? kp + 4 * t * D + j * 64 : vp + d * 256;
-      __builtin_amdgcn_global_load_lds((global_void*)(ok ? p : reinterpret_cast<const uint8_t*>(kZeros)),
-                                       (lds_void*)(&lds[buf][f * 1024]), 16, 0, 0);
+    for (int n = 0; n < NJ; ++n) {
+      const int f = n * 4 + wave, t = f / NJ, j = f - t * NJ;
+      const bool ok = kb != kNone && j * 64 + g * 16 < D;
+      __builtin_amdgcn_global_load_lds((global_void*)(ok ? kp + 4 * t * D + j * 64 : zeros), (lds_void*)(&kbuf[buf][f * 1024]),
+                                       16, 0, 0);
+    }
+#pragma unroll
+    for (int n = 0; n < VW; ++n) {
+      const int d = n * 4 + wave;
+      vr[n] = *reinterpret_cast<const tok_u32x4*>(vb != kNone && d * 16 < D ? vp + d * 256 : zeros);
     }
   };
-
-  Ids cur{-1, -1}, nxt{-1, -1};
-  float ks = 1.f, vs = 1.f;
-  auto scales = [&](const Ids& i, float& k, float& v) {
-    k = i.vb >= 0 ? a.ks[i.vb] : 1.f;
-    v = i.vb >= 0 ? a.vs[i.vb] : 0x1p-126f;
+  // a tile that some column of the workgroup does not see whole
+  auto partial = [&](int tok0, uint32_t vb) { return tok0 < hi.begin || tok0 + 64 > lo.end || __ballot(vb == kNone) != 0; };
+  int unit = -126, grown = -126, rest = 0;  // E, E after the next tile, what of its exponents goes to P
+  auto convert = [&](int tile, uint32_t vb, float vs, int buf) __attribute__((always_inline)) {
+    const int ve = exponent_of(vs);
+    grown = max(unit, over_groups(ve));
+    const int k = max(ve - grown, kDeep);
+    rest = ve - grown - k;
+    const float vk = pow2(k);
+    if (partial(tile * 64, vb)) {
+      // values that no column sees become 0; NaN among the others are taken
+      // out of the product and put back where they are seen
+      bool any = false;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const uint32_t keep = kept(tile * 64 + 16 * g, t, ub, ue);
+#pragma unroll
+        for (int n = 0; n < VW; ++n) {
+          vr[n][t] &= keep;
+          any |= nan_code(vr[n][t]);
+          vr[n][t] = no_nan(vr[n][t]);
+        }
+      }
+      const bool seen = __ballot(any) != 0;
+      if (lane == 0) nan_seen[buf][wave] = seen;
+    }
+#pragma unroll
+    for (int n = 0; n < VW; ++n)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        *reinterpret_cast<tok_u32x4*>(&vbuf[buf][((n * 4 + wave) * 2 + u) * 1024 + lane * 16]) =
+            codes_f16(vr[n][2 * u], vr[n][2 * u + 1], vk);
   };
+  auto scales = [&](uint32_t vb, float& k, float& v) {
+    k = vb != kNone ? a.ks[vb] : 1.f;
+    v = vb != kNone ? a.vs[vb] : 0x1p-126f;
+  };
+
+  uint32_t cur = kNone, nxt = kNone;
+  float ks = 1.f, vs = 1.f;
   if (t0 < t1) {
-    cur = ids(t0);
+    cur = block(t0);
     fetch(cur, 0);
     scales(cur, ks, vs);
-    nxt = ids(t0 + 1);
+    nxt = block(t0 + 1);
+    convert(t0, cur, vs, 0);
   }
   for (int tile = t0; tile < t1; ++tile) {
     const int buf = (tile - t0) & 1, tok0 = tile * 64;
-    __syncthreads();  // this tile is in LDS, and nobody reads the other buffer
+    __syncthreads();  // this tile is in LDS, and nobody reads the other buffers
     float ks1 = 1.f, vs1 = 1.f;
-    Ids far = nxt;
+    uint32_t far = kNone;
     if (tile + 1 < t1) {
       fetch(nxt, buf ^ 1);
       scales(nxt, ks1, vs1);
-      far = ids(tile + 2);
+      far = block(tile + 2);
     }
-    const uint8_t* frag = &lds[buf][lane * 16];
-    auto read = [&](int f) { return *reinterpret_cast<const tok_u32x4*>(frag + f * 1024); };
-    if (tok0 < whi.end && tok0 + 64 > wlo.begin) {
-      const float cg = fmaxf(a.c * ks, 0x1p-126f);
-      const int ve = exponent_of(vs);
-      tok_f32x4 s[CT][4];
+    const float cg = fmaxf(a.c * ks, 0x1p-126f), shrink = pow2(unit - grown);
+    const int f = rest;
+    const bool low = __ballot(f < 0) != 0;
+    unit = grown;
+    tok_f32x4 s[CT][4];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < 4; ++t) {
 #pragma unroll
-        for (int x = 0; x < CT; ++x) s[x][t] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int x = 0; x < CT; ++x) s[x][t] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          const tok_u32x4 kv = read(t * NJ + j);
+      for (int j = 0; j < NJ; ++j) {
+        const tok_u32x4 kv = *reinterpret_cast<const tok_u32x4*>(&kbuf[buf][(t * NJ + j) * 1024 + lane * 16]);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const tok_u32x4 kf = F::k(kv[2 * h], kv[2 * h + 1]);
+        for (int h = 0; h < 2; ++h) {
+          const tok_u32x4 kf = F::k(kv[2 * h], kv[2 * h + 1]);
 #pragma unroll
-            for (int x = 0; x < CT; ++x)
+          for (int x = 0; x < CT; ++x)
 #pragma unroll
-              for (int n = 0; n < NQ; ++n) s[x][t] = F::mfma(kf, qf[x][2 * j + h][n], s[x][t]);
-          }
+            for (int n = 0; n < NQ; ++n) s[x][t] = F::mfma(kf, qf[x][2 * j + h][n], s[x][t]);
         }
-      }
-      const bool edge = tok0 < whi.begin || tok0 + 64 > wlo.end || __ballot(cur.vb < 0) != 0;
-      const int base = tok0 + 16 * g;
-      uint32_t keep[4] = {~0u, ~0u, ~0u, ~0u};
-      bool bad = false;
-      if (edge) {
-#pragma unroll
-        for (int x = 0; x < CT; ++x) hide(s[x], base, mine[x], cur.vb >= 0);
-#pragma unroll
-        for (int t = 0; t < 4; ++t) keep[t] = kept(base, t, wlo.begin, whi.end);
-        bool any = false;
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const tok_u32x4 v = read(4 * NJ + d);
-#pragma unroll
-          for (int t = 0; t < 4; ++t) any |= nan_code(v[t] & keep[t]);
-        }
-        bad = __ballot(any) != 0;
-      }
-      const int grown = max(unit, over_groups(ve));
-      const int k = max(ve - grown, kDeep), f = ve - grown - k;
-      const float vk = pow2(k), shrink = pow2(unit - grown);
-      const bool low = __ballot(f < 0) != 0;
-      unit = grown;
-      tok_u32x4 pf[CT][2][NP];
-#pragma unroll
-      for (int x = 0; x < CT; ++x) soften<DT, NP>(s[x], cg, f, low, shrink, m[x], l[x], acc[x], pf[x]);
-      auto second = [&](bool clean) __attribute__((always_inline)) {
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          tok_u32x4 v = read(4 * NJ + d);
-          if (!clean) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t) v[t] = no_nan(v[t] & keep[t]);
-          }
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const tok_u32x4 vf = codes_f16(v[2 * u], v[2 * u + 1], vk);
-#pragma unroll
-            for (int x = 0; x < CT; ++x)
-#pragma unroll
-              for (int n = 0; n < NP; ++n) acc[x][d] = mfma_f16(vf, pf[x][u][n], acc[x][d]);
-          }
-        }
-      };
-      if (edge)
-        second(false);
-      else
-        second(true);
-      if (bad) {
-#pragma unroll
-        for (int x = 0; x < CT; ++x) put_nan<DT>(a, cur.vb, tok0, g, mine[x], acc[x]);
       }
     }
+    if (tok0 < whi.begin || tok0 + 64 > wlo.end || __ballot(cur == kNone) != 0) {
+#pragma unroll
+      for (int x = 0; x < CT; ++x) hide(s[x], tok0 + 16 * g, mine[x], cur != kNone);
+    }
+    tok_u32x4 pf[CT][2][NP];
+#pragma unroll
+    for (int x = 0; x < CT; ++x) soften<DT, NP>(s[x], cg, f, low, shrink, m[x], l[x], acc[x], pf[x]);
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const tok_u32x4 vf = *reinterpret_cast<const tok_u32x4*>(&vbuf[buf][(d * 2 + u) * 1024 + lane * 16]);
+#pragma unroll
+        for (int x = 0; x < CT; ++x)
+#pragma unroll
+          for (int n = 0; n < NP; ++n) acc[x][d] = mfma_f16(vf, pf[x][u][n], acc[x][d]);
+      }
+    }
+    if (partial(tok0, cur) && (nan_seen[buf][0] | nan_seen[buf][1] | nan_seen[buf][2] | nan_seen[buf][3])) {
+#pragma unroll
+      for (int x = 0; x < CT; ++x) put_nan<DT>(a, cur, tok0, g, mine[x], acc[x]);
+    }
+    if (tile + 1 < t1) convert(tile + 1, nxt, vs1, buf ^ 1);
     cur = nxt;
     nxt = far;
     ks = ks1;
-    vs = vs1;
   }
 
 #pragma unroll
@@ -723,9 +733,9 @@ hipError_t run(const AttendArgs& h, const AttendPlan& p, int dtype, hipStream_t 
   const int64_t G = h.q_heads / h.c.heads, columns = h.b.max_new * G, nb = h.c.page / 16;
   const int64_t cap = h.b.cols * h.c.page, coltiles = up(columns, workgroup_columns(h.c.dim, dtype));
   const int64_t blocks = coltiles * p.splits * h.c.heads * h.b.B, joins = up(h.b.T * h.q_heads, 4);
-  // 32-bit numbering of columns (of T rows at most), workgroups and grids
+  // 32-bit numbering of columns (of T rows at most), blocks, workgroups and grids
   if (up(h.b.T * G, 16) * 16 + 1024 > 0x7fffffff || columns > 0x7fffffff - 1024 || joins > 0x7fffffff ||
-      (few(columns) ? h.b.B > 65535 || h.c.heads > 65535 : blocks > 0x7fffffff))
+      h.c.pages * h.c.heads * nb >= 0xffffffffll || (few(columns) ? h.b.B > 65535 || h.c.heads > 65535 : blocks > 0x7fffffff))
     return hipErrorInvalidConfiguration;
   const Dev a{static_cast<const uint8_t*>(h.c.k), static_cast<const uint8_t*>(h.c.v), h.c.k_scale, h.c.v_scale,
               h.b.table, h.b.cu, h.b.len, h.q, h.out, h.lse, h.part, h.ld_q,
