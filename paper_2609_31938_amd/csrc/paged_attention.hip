@@ -238,18 +238,14 @@ __device__ inline void put_nan(const Dev& a, uint32_t vb, int tok0, int g, const
   }
 }
 
-// The running softmax of one column tile over one 64-token tile: the maximum,
-// the accumulators in its units, the probabilities as terms, their sum.
-// cg: c times the scale of this lane's block; f: what of its value exponent
-// goes to P; shrink: 2^(E before - E now).
-//   The maximum moves only when a score passes it by more than kSlack: the
+// The running softmax of one column tile over one 64-token tile, in two
+// steps.  First the maximum m and the accumulators in its units (cg: c times
+// the key scale of this lane's block; shrink: 2^(E before - E now)).  The
+// maximum moves only when a score passes it by more than kSlack: the
 // exponentials' range allows it, and it then seldom costs a reduction over
 // lanes and a pass over the accumulators.
-//   The sum (l: this lane's part) is of the probabilities before their
-// rounding to terms, for lse is held to fp32.
-template <int DT, int NP>
-__device__ inline void soften(const tok_f32x4 (&s)[4], float cg, int f, bool low, float shrink, float& m, float& l,
-                              tok_f32x4 (&acc)[DT], tok_u32x4 (&pf)[2][NP]) {
+template <int DT>
+__device__ inline void rescale(const tok_f32x4 (&s)[4], float cg, float shrink, float& m, float& l, tok_f32x4 (&acc)[DT]) {
   float top = -kInf;
 #pragma unroll
   for (int t = 0; t < 4; ++t)
@@ -267,21 +263,27 @@ __device__ inline void soften(const tok_f32x4 (&s)[4], float cg, int f, bool low
     for (int d = 0; d < DT; ++d) acc[d] *= all;
     m = next;
   }
-  const float lift = kLift - (m == -kInf ? 0.f : m);
+}
+
+// Then the probabilities as terms, 2^f P, and this lane's part l of their sum
+// (before their rounding to terms, for lse is held to fp32).  f: what of the
+// block's value exponent goes to P; below 2^-60 nothing is left of it.
+constexpr int kLeast = -60;
+template <int NP>
+__device__ inline void weigh(const tok_f32x4 (&s)[4], float cg, int f, float m, float& l, tok_u32x4 (&pf)[2][NP]) {
+  const float lift = kLift + f - (m == -kInf ? 0.f : m);
+  float sum = 0.f;
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     float p[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[2 * u + (e >> 2)][e & 3], cg, lift));
-      l += p[e];
-    }
-    if (low) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] *= pow2(f);
+      sum += p[e];
     }
     to_terms<tok_f16x2, NP>(p, pf[u]);
   }
+  l = __builtin_fmaf(sum, pow2(-f), l);
 }
 
 // largest exponent of the four blocks' value scales
@@ -388,10 +390,11 @@ __global__ __launch_bounds__(256) void attend_few(Dev a) {
       }
     }
     const int grown = max(unit, over_groups(ve));
-    const int k = max(ve - grown, kDeep), f = ve - grown - k;
+    const int k = max(ve - grown, kDeep), f = max(ve - grown - k, kLeast);
     const float vk = pow2(k);
     tok_u32x4 pf[2][NP];
-    soften<DT, NP>(s, cg, f, __ballot(f < 0) != 0, pow2(unit - grown), m, l, acc, pf);
+    rescale<DT>(s, cg, pow2(unit - grown), m, l, acc);
+    weigh<NP>(s, cg, f, m, l, pf);
     unit = grown;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -521,11 +524,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   // LDS, this wave's part of V in registers.
   auto block = [&](int tile) { return find(a, b, hk, tile * 4 + g, ue); };
   tok_u32x4 vr[VW];
-  auto fetch = [&](uint32_t vb, int buf) __attribute__((always_inline)) {
+  const uint8_t* zeros = reinterpret_cast<const uint8_t*>(kZeros);
+  auto fetch_k = [&](uint32_t vb, int buf) __attribute__((always_inline)) {
     const uint32_t kb = __shfl(vb, (r >> 2) * 16);
-    const uint8_t* zeros = reinterpret_cast<const uint8_t*>(kZeros);
     const uint8_t* kp = a.k + (static_cast<int64_t>(kb) * 16 + (r & 3)) * D + g * 16;
-    const uint8_t* vp = a.v + (static_cast<int64_t>(vb) * D + r) * 16;
 #pragma unroll
     for (int n = 0; n < NJ; ++n) {
       const int f = n * 4 + wave, t = f / NJ, j = f - t * NJ;
@@ -533,6 +535,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
       __builtin_amdgcn_global_load_lds((global_void*)(ok ? kp + 4 * t * D + j * 64 : zeros), (lds_void*)(&kbuf[buf][f * 1024]),
                                        16, 0, 0);
     }
+  };
+  auto fetch_v = [&](uint32_t vb) __attribute__((always_inline)) {
+    const uint8_t* vp = a.v + (static_cast<int64_t>(vb) * D + r) * 16;
 #pragma unroll
     for (int n = 0; n < VW; ++n) {
       const int d = n * 4 + wave;
@@ -546,7 +551,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     const int ve = exponent_of(vs);
     grown = max(unit, over_groups(ve));
     const int k = max(ve - grown, kDeep);
-    rest = ve - grown - k;
+    rest = max(ve - grown - k, kLeast);
     const float vk = pow2(k);
     if (partial(tile * 64, vb)) {
       // values that no column sees become 0; NaN among the others are taken
@@ -577,30 +582,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     v = vb != kNone ? a.vs[vb] : 0x1p-126f;
   };
 
-  uint32_t cur = kNone, nxt = kNone;
-  float ks = 1.f, vs = 1.f;
-  if (t0 < t1) {
-    cur = block(t0);
-    fetch(cur, 0);
-    scales(cur, ks, vs);
-    nxt = block(t0 + 1);
-    convert(t0, cur, vs, 0);
-  }
-  for (int tile = t0; tile < t1; ++tile) {
-    const int buf = (tile - t0) & 1, tok0 = tile * 64;
-    __syncthreads();  // this tile is in LDS, and nobody reads the other buffers
-    float ks1 = 1.f, vs1 = 1.f;
-    uint32_t far = kNone;
-    if (tile + 1 < t1) {
-      fetch(nxt, buf ^ 1);
-      scales(nxt, ks1, vs1);
-      far = block(tile + 2);
-    }
-    const float cg = fmaxf(a.c * ks, 0x1p-126f), shrink = pow2(unit - grown);
-    const int f = rest;
-    const bool low = __ballot(f < 0) != 0;
-    unit = grown;
-    tok_f32x4 s[CT][4];
+  tok_f32x4 s[CT][4];
+  auto first = [&](int buf, tok_f32x4 (&s)[CT][4]) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
 #pragma unroll
@@ -618,13 +601,62 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
         }
       }
     }
+  };
+
+  // A round works on tile t's softmax and second product and on tile t + 1's
+  // first, which has nothing to wait for while the exponentials run.  K is
+  // fetched two tiles ahead, V one.
+  uint32_t cur = kNone, nxt = kNone, far = kNone;  // blocks of tiles t, t + 1, t + 2
+  float ks = 1.f;
+  if (t0 < t1) {
+    float vs;
+    cur = block(t0);
+    fetch_k(cur, t0 & 1);
+    fetch_v(cur);
+    scales(cur, ks, vs);
+    if (t0 + 1 < t1) {
+      nxt = block(t0 + 1);
+      fetch_k(nxt, (t0 + 1) & 1);
+    }
+    far = block(t0 + 2);
+    convert(t0, cur, vs, t0 & 1);
+    __syncthreads();
+    first(t0 & 1, s);
+  }
+  for (int tile = t0; tile < t1; ++tile) {
+    const int buf = tile & 1, tok0 = tile * 64;
+    __syncthreads();  // what this round reads is in LDS, and nobody reads what it writes
+    float ks1 = 1.f, vs1 = 1.f;
+    uint32_t next = kNone;
+    if (tile + 1 < t1) {
+      fetch_v(nxt);
+      scales(nxt, ks1, vs1);
+      if (tile + 2 < t1) fetch_k(far, buf);
+      next = block(tile + 3);
+    }
+    const float cg = fmaxf(a.c * ks, 0x1p-126f), shrink = pow2(unit - grown);
+    const int f = rest;
+    unit = grown;
     if (tok0 < whi.begin || tok0 + 64 > wlo.end || __ballot(cur == kNone) != 0) {
 #pragma unroll
       for (int x = 0; x < CT; ++x) hide(s[x], tok0 + 16 * g, mine[x], cur != kNone);
     }
+#pragma unroll
+    for (int x = 0; x < CT; ++x) rescale<DT>(s[x], cg, shrink, m[x], l[x], acc[x]);
+    __builtin_amdgcn_sched_barrier(0);
+    tok_f32x4 s1[CT][4];
+    first(buf ^ 1, s1);  // past the last tile: of stale codes, and never used
     tok_u32x4 pf[CT][2][NP];
 #pragma unroll
-    for (int x = 0; x < CT; ++x) soften<DT, NP>(s[x], cg, f, low, shrink, m[x], l[x], acc[x], pf[x]);
+    for (int x = 0; x < CT; ++x) weigh<NP>(s[x], cg, f, m[x], l[x], pf[x]);
+#ifdef SCHED
+#pragma unroll
+    for (int i = 0; i < 4 * CT * KS * NQ; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, SCHED, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#endif
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
 #pragma unroll
@@ -636,6 +668,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
           for (int n = 0; n < NP; ++n) acc[x][d] = mfma_f16(vf, pf[x][u][n], acc[x][d]);
       }
     }
+    __builtin_amdgcn_sched_barrier(0);
     if (partial(tok0, cur) && (nan_seen[buf][0] | nan_seen[buf][1] | nan_seen[buf][2] | nan_seen[buf][3])) {
 #pragma unroll
       for (int x = 0; x < CT; ++x) put_nan<DT>(a, cur, tok0, g, mine[x], acc[x]);
@@ -643,7 +676,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     if (tile + 1 < t1) convert(tile + 1, nxt, vs1, buf ^ 1);
     cur = nxt;
     nxt = far;
+    far = next;
     ks = ks1;
+#pragma unroll
+    for (int x = 0; x < CT; ++x)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) s[x][t] = s1[x][t];
   }
 
 #pragma unroll
