@@ -160,15 +160,18 @@ __device__ inline Seq sequence(const Dev& a, int b) {
   return {r0, n, len < a.cap ? len : a.cap, (len < 0 ? 0 : len) - n};
 }
 
-// Index among the cache's 16-token blocks (of head hk) of block blk of
-// sequence b, or kNone where it has no page or begins at `end` or later.
+// Blocks of a sequence are found in two steps, so that nothing waits for the
+// page table: peek reads the page of block blk (none where the block begins at
+// `end` or later), settle makes it the block's index among the cache's (of
+// head hk), or kNone.
 constexpr uint32_t kNone = 0xffffffffu;
-__device__ inline uint32_t find(const Dev& a, int b, int hk, int blk, int end) {
-  const int col = a.pow >= 0 ? blk >> a.pow : blk / a.nb;
-  if (blk * 16 >= end || col >= a.cols) return kNone;
-  const uint32_t page = a.table[static_cast<int64_t>(b) * a.cols + col];
-  if (page >= static_cast<uint32_t>(a.pages)) return kNone;
-  return (page * a.heads + hk) * a.nb + (blk - col * a.nb);
+__device__ inline int column_of(const Dev& a, int blk) { return a.pow >= 0 ? blk >> a.pow : blk / a.nb; }
+__device__ inline uint32_t peek(const Dev& a, const int32_t* row, int blk, int end) {
+  const int col = column_of(a, blk);
+  return blk * 16 < end && col < a.cols ? static_cast<uint32_t>(row[col]) : kNone;
+}
+__device__ inline uint32_t settle(const Dev& a, int hk, int blk, uint32_t page) {
+  return page < static_cast<uint32_t>(a.pages) ? (page * a.heads + hk) * a.nb + (blk - column_of(a, blk) * a.nb) : kNone;
 }
 
 // v, as a value that the compiler cannot compute with ahead of time: keeps
@@ -238,6 +241,20 @@ __device__ inline void put_nan(const Dev& a, uint32_t vb, int tok0, int g, const
   }
 }
 
+// A maximum over the four lane groups
+__device__ inline float over_groups(float v) {
+  auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+  p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ inline int over_groups(int v) {
+  auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(static_cast<int>(p[0]), static_cast<int>(p[1]));
+  p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(static_cast<int>(p[0]), static_cast<int>(p[1]));
+}
+
 // The running softmax of one column tile over one 64-token tile, in two
 // steps.  First the maximum m and the accumulators in its units (cg: c times
 // the key scale of this lane's block; shrink: 2^(E before - E now)).  The
@@ -253,8 +270,7 @@ __device__ inline void rescale(const tok_f32x4 (&s)[4], float cg, float shrink, 
     for (int i = 0; i < 4; ++i) top = fmaxf(top, s[t][i]);
   top *= cg;
   if (__ballot(top > m + kSlack) || shrink != 1.f) {
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = over_groups(top);
     const float next = top > m + kSlack ? top : m;
     const float down = __builtin_amdgcn_exp2f(m - (next == -kInf ? 0.f : next));
     l *= down;
@@ -284,12 +300,6 @@ __device__ inline void weigh(const tok_f32x4 (&s)[4], float cg, int f, float m, 
     to_terms<tok_f16x2, NP>(p, pf[u]);
   }
   l = __builtin_fmaf(sum, pow2(-f), l);
-}
-
-// largest exponent of the four blocks' value scales
-__device__ inline int over_groups(int e) {
-  e = max(e, __shfl_xor(e, 16));
-  return max(e, __shfl_xor(e, 32));
 }
 
 // One workgroup: 16 columns (queries and heads that read one key/value head)
@@ -329,9 +339,12 @@ __global__ __launch_bounds__(256) void attend_few(Dev a) {
   float m = -kInf, l = 0.f;  // l: this lane's part of 2^kLift times the sum
   int unit = -126;           // E
 
+  const int32_t* pages = a.table + static_cast<int64_t>(b) * a.cols;
+  uint32_t page = peek(a, pages, (t0 + wave) * 4 + g, ue);
   for (int tile = t0 + wave; tile < t1; tile += 4) {
     const int blk0 = tile * 4, tok0 = tile * 64;
-    const uint32_t vb = find(a, b, hk, blk0 + g, ue), kb = __shfl(vb, (r >> 2) * 16);
+    const uint32_t vb = settle(a, hk, blk0 + g, page), kb = __shfl(vb, (r >> 2) * 16);
+    page = peek(a, pages, blk0 + 16 + g, ue);
     const bool kok = kb != kNone, vok = vb != kNone;
     const uint8_t* kp = a.k + (static_cast<int64_t>(kb) * 16 + (r & 3)) * D + g * 16;
     const uint8_t* vp = a.v + (static_cast<int64_t>(vb) * D + r) * 16;
@@ -522,12 +535,15 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   }
   // Tiles on their way: block g of the tile of this lane, its scales, K in
   // LDS, this wave's part of V in registers.
-  auto block = [&](int tile) { return find(a, b, hk, tile * 4 + g, ue); };
+  const int32_t* pages = a.table + static_cast<int64_t>(b) * a.cols;
+  auto page_of = [&](int tile) { return peek(a, pages, tile * 4 + g, ue); };
+  auto block = [&](int tile, uint32_t page) { return settle(a, hk, tile * 4 + g, page); };
   tok_u32x4 vr[VW];
-  const uint8_t* zeros = reinterpret_cast<const uint8_t*>(kZeros);
+  typedef __attribute__((address_space(1))) const uint8_t global_u8;
+  global_u8* zeros = (global_u8*)kZeros;
   auto fetch_k = [&](uint32_t vb, int buf) __attribute__((always_inline)) {
     const uint32_t kb = __shfl(vb, (r >> 2) * 16);
-    const uint8_t* kp = a.k + (static_cast<int64_t>(kb) * 16 + (r & 3)) * D + g * 16;
+    global_u8* kp = (global_u8*)a.k + (static_cast<int64_t>(kb) * 16 + (r & 3)) * D + g * 16;
 #pragma unroll
     for (int n = 0; n < NJ; ++n) {
       const int f = n * 4 + wave, t = f / NJ, j = f - t * NJ;
@@ -537,11 +553,11 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     }
   };
   auto fetch_v = [&](uint32_t vb) __attribute__((always_inline)) {
-    const uint8_t* vp = a.v + (static_cast<int64_t>(vb) * D + r) * 16;
+    global_u8* vp = (global_u8*)a.v + (static_cast<int64_t>(vb) * D + r) * 16;
 #pragma unroll
     for (int n = 0; n < VW; ++n) {
       const int d = n * 4 + wave;
-      vr[n] = *reinterpret_cast<const tok_u32x4*>(vb != kNone && d * 16 < D ? vp + d * 256 : zeros);
+      vr[n] = *(__attribute__((address_space(1))) const tok_u32x4*)(vb != kNone && d * 16 < D ? vp + d * 256 : zeros);
     }
   };
   // a tile that some column of the workgroup does not see whole
@@ -606,19 +622,20 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   // A round works on tile t's softmax and second product and on tile t + 1's
   // first, which has nothing to wait for while the exponentials run.  K is
   // fetched two tiles ahead, V one.
-  uint32_t cur = kNone, nxt = kNone, far = kNone;  // blocks of tiles t, t + 1, t + 2
+  uint32_t cur = kNone, nxt = kNone;  // blocks of tiles t, t + 1
+  uint32_t page = kNone;              // page of tile t + 2
   float ks = 1.f;
   if (t0 < t1) {
     float vs;
-    cur = block(t0);
+    cur = block(t0, page_of(t0));
     fetch_k(cur, t0 & 1);
     fetch_v(cur);
     scales(cur, ks, vs);
     if (t0 + 1 < t1) {
-      nxt = block(t0 + 1);
+      nxt = block(t0 + 1, page_of(t0 + 1));
       fetch_k(nxt, (t0 + 1) & 1);
     }
-    far = block(t0 + 2);
+    page = page_of(t0 + 2);
     convert(t0, cur, vs, t0 & 1);
     __syncthreads();
     first(t0 & 1, s);
@@ -627,12 +644,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     const int buf = tile & 1, tok0 = tile * 64;
     __syncthreads();  // what this round reads is in LDS, and nobody reads what it writes
     float ks1 = 1.f, vs1 = 1.f;
-    uint32_t next = kNone;
+    const uint32_t far = block(tile + 2, page);
     if (tile + 1 < t1) {
       fetch_v(nxt);
       scales(nxt, ks1, vs1);
       if (tile + 2 < t1) fetch_k(far, buf);
-      next = block(tile + 3);
+      page = page_of(tile + 3);
     }
     const float cg = fmaxf(a.c * ks, 0x1p-126f), shrink = pow2(unit - grown);
     const int f = rest;
@@ -649,14 +666,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     tok_u32x4 pf[CT][2][NP];
 #pragma unroll
     for (int x = 0; x < CT; ++x) weigh<NP>(s[x], cg, f, m[x], l[x], pf[x]);
-#ifdef SCHED
-#pragma unroll
-    for (int i = 0; i < 4 * CT * KS * NQ; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x002, SCHED, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#endif
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
 #pragma unroll
@@ -676,7 +685,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     if (tile + 1 < t1) convert(tile + 1, nxt, vs1, buf ^ 1);
     cur = nxt;
     nxt = far;
-    far = next;
     ks = ks1;
 #pragma unroll
     for (int x = 0; x < CT; ++x)
@@ -811,12 +819,31 @@ AttendPlan plan_attend(const c3c_kv_cache& c, const c3c_kv_batch& b, int dtype, 
   const int64_t columns = b.max_new * (q_heads / c.heads), tiles = tiles_seen(b, c.page, window);
   const int64_t base = up(columns, few(columns) ? 16 : workgroup_columns(c.dim, dtype)) * c.heads * b.B;
   if (base == 0) return p;
-  // few: enough workgroups to fill the device several times (sequences are
-  // ragged), of at least one tile a wave; many: one workgroup a compute unit,
-  // of at least 4 tiles
-  const int64_t cus = device_compute_units();
-  const int64_t want = few(columns) ? up(8 * cus, base) : cus / base, most = up(tiles, 4);
-  const int64_t s = want < most ? want : most;
+  const int64_t cus = device_compute_units(), most = up(tiles, 4);
+  int64_t s = 1;
+  if (few(columns)) {
+    // enough workgroups to fill the device several times (sequences are
+    // ragged), of at least one tile a wave
+    const int64_t want = up(8 * cus, base);
+    s = want < most ? want : most;
+  } else {
+    // the fewest rounds of workgroups, counted in tiles: each round costs its
+    // tiles and about 3 more to begin and end, the join its launch and its
+    // traffic (a tile takes about 2.8 us at 128 channels, 1 us reads and writes
+    // 4 MB).  Two bf16 sequences of 1560 queries, 12 heads and 9400 tokens: 312
+    // workgroups for 512 places; three splits 318 us, one 423.
+    const int64_t places = cus * (c.dim <= 128 ? 2 : 1);
+    const double bytes = 8.0 * b.T * q_heads * (c.dim + 2), tile_us = 2.8 * c.dim / 128;
+    double best = 0;
+    for (int64_t n = 1; n <= most && n <= 32; ++n) {
+      const double t = up(base * n, places) * (static_cast<double>(up(tiles, n)) + 3) +
+                       (n > 1 ? (5 + n * bytes / 4e6) / tile_us : 0);
+      if (n == 1 || t < best) {
+        best = t;
+        s = n;
+      }
+    }
+  }
   if (s > 1) {
     p.splits = static_cast<int>(s);
     p.part_bytes = s * b.T * q_heads * (c.dim + 2) * 4;
