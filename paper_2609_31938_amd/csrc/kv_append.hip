@@ -4,13 +4,16 @@
 //   block of 16 tokens and head: scale 2^e, e least with max|x| <= 448 2^e;
 //   codes e4m3(x 2^-e)
 //
-// One wave owns one block of 16 tokens of one head (of k, v or q): it holds
-// the block's new values in registers, a pair of channels a lane and token,
-// so the block's maximum is one reduction over the wave and every element is
-// read once and written once.  Nobody else writes the block, so the scale
-// needs no atomics, and an append of many tokens and many appends of one give
-// the same scales.  Bound by memory traffic for frames of tokens and by
-// latency for single ones.
+// One wave owns one block of 16 tokens of one head (of k, v or q): lane l holds
+// 8 channels from 8 (l % 16) on (and the same past 128) of the 4 tokens from
+// 4 (l / 16) on, 16 bytes a load.  So the block's maximum is one reduction over
+// the wave and every element is read once and written once.  Nobody else
+// writes the block, so the scale needs no atomics, and an append of many tokens
+// and many appends of one give the same scales.  V's 4 x 4 (lane groups x
+// pairs of channels) dwords of 4 tokens are transposed between the lane groups,
+// so that a lane stores whole 16-byte rows.  Everything that an address needs
+// is read before the values are worked on: a single token's time is a chain of
+// memory latencies.
 //
 // The products and sums of a rotation are rounded one by one (no fused
 // multiply-add), so that a code is decided by the formula's own fp32 value.
@@ -41,211 +44,290 @@ __device__ inline uint32_t codes2(float a, float b) {
   return r;
 }
 
-// Two elements of a row at channel c (even).
-template <class E, bool AL>
-__device__ inline void load2(const typename E::store* p, float& a, float& b) {
-  typename E::store v[2];
-  if (AL) {
-    __builtin_memcpy(v, __builtin_assume_aligned(p, 2 * sizeof(v[0])), sizeof v);
-  } else {
-    v[0] = p[0];
-    v[1] = p[1];
-  }
-  a = E::widen(v[0]);
-  b = E::widen(v[1]);
+// 8 elements of a row, at any alignment
+template <class E>
+__device__ inline void load8(const typename E::store* p, float (&f)[8]) {
+  typename E::store v[8];
+  __builtin_memcpy(v, p, sizeof v);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = E::widen(v[e]);
+}
+template <int N>
+__device__ inline void load_f(const float* p, float (&f)[N]) {
+  __builtin_memcpy(f, p, 4 * N);
 }
 
-// NP pairs of channels a lane: lane l holds channels 2 (l + 64 i) and the next.
-template <class E, int NP, bool AL>
+// Rotates 8 channels from c on; src: the row (for the other half of a pair),
+// cs and sn: the angle's rows.
+template <class E>
+__device__ inline void rotate(const typename E::store* src, const float* cs, const float* sn, int c, int rot, int pairs,
+                              float (&x)[8]) {
+  const int half = rot >> 1;
+  if (c >= rot) return;
+  if (pairs) {
+    float co[4], si[4];
+    if (c + 8 <= rot) {
+      load_f(cs + (c >> 1), co);
+      load_f(sn + (c >> 1), si);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = c + 2 * e < rot ? (c >> 1) + e : 0;
+        co[e] = cs[i];
+        si[e] = sn[i];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float u = x[2 * e], v = x[2 * e + 1];
+      if (c + 2 * e < rot) {
+        x[2 * e] = u * co[e] - v * si[e];
+        x[2 * e + 1] = v * co[e] + u * si[e];
+      }
+    }
+  } else if ((half & 7) == 0) {  // all 8 in the same half
+    const bool low = c < half;
+    const int j = low ? c : c - half;
+    float o[8], co[8], si[8];
+    load8<E>(src + (low ? c + half : j), o);
+    load_f(cs + j, co);
+    load_f(sn + j, si);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float a = x[e] * co[e], b = o[e] * si[e];
+      x[e] = low ? a - b : a + b;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int ch = c + e;
+      if (ch < rot) {
+        const bool low = ch < half;
+        const int j = low ? ch : ch - half;
+        const float a = x[e] * cs[j], b = E::widen(src[low ? ch + half : j]) * sn[j];
+        x[e] = low ? a - b : a + b;
+      }
+    }
+  }
+}
+
+// d[j] of lane group g: 4 tokens (from 4 g on) of channel j.  Afterwards
+// d[4 * i + t] of lane group g: tokens 4 t .. of channel 2 g + i.
+__device__ inline void transpose(uint32_t (&d)[8]) {
+  uint32_t e[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {  // lanes below 32 keep channels 0-3, the others 4-7
+    const auto p = __builtin_amdgcn_permlane32_swap(d[j], d[j + 4], false, false);
+    e[j] = p[0];      // of groups 0 and 1 (this lane's g % 2)
+    e[4 + j] = p[1];  // of groups 2 and 3
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h)    // token groups 2 h, 2 h + 1
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {  // even groups keep channels 0, 1, odd ones 2, 3
+      const auto p = __builtin_amdgcn_permlane16_swap(e[4 * h + i], e[4 * h + i + 2], false, false);
+      d[4 * i + 2 * h] = p[0];
+      d[4 * i + 2 * h + 1] = p[1];
+    }
+}
+
+// four codes, as many multiplied by 2^-shrink
+__device__ inline uint32_t shrunk(uint32_t w, float less) {
+  const tok_f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+  return codes2(a[0] * less, a[1] * less) | codes2(b[0] * less, b[1] * less) << 16;
+}
+
+template <class E, int NP>  // NP: 1, or 2 beyond 128 channels
 __global__ __launch_bounds__(256) void kv_append_k(AppendArgs a) {
   typedef typename E::store S;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, g = lane >> 4, c0 = (lane & 15) * 8;
   const int64_t b = blockIdx.z;
   const int heads = static_cast<int>(a.c.heads), D = static_cast<int>(a.c.dim);
   // one wave a head: keys, values, then queries
-  int unit = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.y) * 4 + (threadIdx.x >> 6));
+  const int unit = __builtin_amdgcn_readfirstlane(static_cast<int>(blockIdx.y) * 4 + (threadIdx.x >> 6));
   if (unit >= 2 * heads + static_cast<int>(a.q_out ? a.q_heads : 0)) return;
   const int what = unit < heads ? 0 : unit < 2 * heads ? 1 : 2;
   const int head = unit - what * heads;
 
   // this sequence's rows and places
   int64_t row0 = a.b.cu[b], row1 = a.b.cu[b + 1];
+  const int64_t len = a.b.len[b];
   row0 = row0 < 0 ? 0 : row0;
   row1 = row1 > a.b.T ? a.b.T : row1;
   const int64_t n = row1 - row0;
   if (n <= 0) return;
-  const int64_t len = a.b.len[b];
   const int64_t start = len - n;  // place of the first new token; negative if len is too short
-  const int64_t first = start >= 0 ? start / 16 : -((15 - start) / 16);
-  const int64_t last = (len - 1 >= 0) ? (len - 1) / 16 : -((16 - len) / 16);
+  // floor of the first and last place over 16
+  const int64_t first = start >> 4, last = (len - 1) >> 4;
 
   const S* src = static_cast<const S*>(what == 0 ? a.k : what == 1 ? a.v : a.q) + static_cast<int64_t>(head) * D;
   const int64_t ld = what == 0 ? a.ld_k : what == 1 ? a.ld_v : a.ld_q;
   const int rot = (what != 1 && a.r.cos) ? static_cast<int>(a.r.rot) : 0;
+  const int nb = static_cast<int>(a.c.page) >> 4;
 
   for (int64_t blk = first + blockIdx.x; blk <= last; blk += gridDim.x) {
     const int64_t p0 = blk * 16;
     const int lo = start > p0 ? static_cast<int>(start - p0) : 0;
     const int hi = len - p0 < 16 ? static_cast<int>(len - p0) : 16;
     const int64_t r0 = row0 + (p0 - start);  // row of place 0 of the block (valid from lo to hi)
-    float x[16][NP][2];
+    // the block's page; tokens without a valid one are not stored
+    int64_t at = -1;  // of the block among the cache's
+    if (what < 2 && blk >= 0) {
+      const int64_t col = blk / nb;
+      if (col < a.b.cols) {
+        const int64_t page = a.b.table[b * a.b.cols + col];
+        if (page >= 0 && page < a.c.pages) at = (page * heads + head) * nb + (blk - col * nb);
+      }
+    }
+    float x[4][NP][8];
 #pragma unroll
-    for (int t = 0; t < 16; ++t)
+    for (int t = 0; t < 4; ++t) {
+      const int place = 4 * g + t;
+      const bool in = place >= lo && place < hi;
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        const int c = 2 * (lane + 64 * i);
-        x[t][i][0] = x[t][i][1] = 0.f;
-        if (t >= lo && t < hi && c < D) load2<E, AL>(src + (r0 + t) * ld + c, x[t][i][0], x[t][i][1]);
-      }
-    if (rot) {
-      const int half = rot >> 1;
 #pragma unroll
-      for (int t = 0; t < 16; ++t) {
-        if (t < lo || t >= hi) continue;
-        const int64_t at = a.r.pos ? a.r.pos[r0 + t] : p0 + t;
-        const bool ok = at >= 0 && at < a.r.rows;
-        const float* cs = a.r.cos + (ok ? at : 0) * half;
-        const float* sn = a.r.sin + (ok ? at : 0) * half;
+        for (int e = 0; e < 8; ++e) x[t][i][e] = 0.f;
+        if (in && c0 + 128 * i < D) load8<E>(src + (r0 + place) * ld + c0 + 128 * i, x[t][i]);
+      }
+    }
+    float* scale = nullptr;
+    uint8_t* codes = nullptr;
+    int old = -126;
+    tok_u32x4 was[NP][2];  // v: this lane's two rows of earlier and later tokens
+    if (at >= 0) {
+      scale = (what == 0 ? a.c.k_scale : a.c.v_scale) + at;
+      codes = static_cast<uint8_t*>(what == 0 ? a.c.k : a.c.v) + at * D * 16;
+      if (lo > 0) old = static_cast<int>((__float_as_uint(*scale) >> 23) & 255u) - 127;
+      if (what == 1 && (lo > 0 || hi < 16)) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (c0 + 128 * i < D) was[i][e] = *reinterpret_cast<const tok_u32x4*>(codes + (c0 + 128 * i + 2 * g + e) * 16);
+      }
+    }
+    if (rot) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        __builtin_amdgcn_sched_barrier(0);  // one token's angles at a time: registers for more waves
+        const int place = 4 * g + t;
+        if (place < lo || place >= hi) continue;
+        const int64_t row = a.r.pos ? a.r.pos[r0 + place] : p0 + place;
+        const bool ok = row >= 0 && row < a.r.rows;
+        const float* cs = a.r.cos + (ok ? row : 0) * (rot >> 1);
+        const float* sn = a.r.sin + (ok ? row : 0) * (rot >> 1);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-          const int c = 2 * (lane + 64 * i);
-          if (a.r.pairs) {
-            if (c < rot) {
-              const float co = cs[c >> 1], si = sn[c >> 1], u = x[t][i][0], v = x[t][i][1];
-              x[t][i][0] = u * co - v * si;
-              x[t][i][1] = v * co + u * si;
-            }
-          } else {
+          if (c0 + 128 * i < D) rotate<E>(src + (r0 + place) * ld, cs, sn, c0 + 128 * i, rot, a.r.pairs, x[t][i]);
+          if (!ok) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int ch = c + e;
-              if (ch < rot) {
-                const bool low = ch < half;
-                const int j = low ? ch : ch - half;
-                const float other = E::widen(src[(r0 + t) * ld + (low ? ch + half : j)]);
-                const float co = cs[j], si = sn[j], u = x[t][i][e];
-                x[t][i][e] = low ? u * co - other * si : u * co + other * si;
-              }
-            }
+            for (int e = 0; e < 8; ++e) x[t][i][e] = __builtin_nanf("");
           }
-          if (!ok) x[t][i][0] = x[t][i][1] = __builtin_nanf("");
         }
       }
     }
     if (what == 2) {
       S* out = static_cast<S*>(a.q_out) + static_cast<int64_t>(head) * D;
 #pragma unroll
-      for (int t = 0; t < 16; ++t) {
-        if (t < lo || t >= hi) continue;
+      for (int t = 0; t < 4; ++t) {
+        const int place = 4 * g + t;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-          const int c = 2 * (lane + 64 * i);
-          if (c >= D) continue;
-          S* o = out + (r0 + t) * (a.q_heads * D) + c;
-          S v[2] = {E::narrow(x[t][i][0]), E::narrow(x[t][i][1])};
-          if (AL) {
-            __builtin_memcpy(__builtin_assume_aligned(o, 2 * sizeof(S)), v, sizeof v);
-          } else {
-            o[0] = v[0];
-            o[1] = v[1];
-          }
+          const int c = c0 + 128 * i;
+          if (place < lo || place >= hi || c >= D) continue;
+          S v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = E::narrow(x[t][i][e]);
+          __builtin_memcpy(out + (r0 + place) * (a.q_heads * D) + c, v, sizeof v);
         }
       }
       continue;
     }
-    // the block's page; tokens without a valid one are not stored
-    if (p0 + 16 <= 0 || blk < 0) continue;
-    const int64_t col = p0 / a.c.page;
-    if (col >= a.b.cols) continue;
-    const int64_t page = a.b.table[b * a.b.cols + col];
-    if (page < 0 || page >= a.c.pages) continue;
-    const int64_t nb = a.c.page / 16, pb = blk - col * nb;  // block of the page
-    float* scale = (what == 0 ? a.c.k_scale : a.c.v_scale) + (page * heads + head) * nb + pb;
+    if (at < 0) continue;
 
     float top = 0.f;
 #pragma unroll
-    for (int t = 0; t < 16; ++t)
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int i = 0; i < NP; ++i)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < 8; ++e) {
           const float m = fabsf(x[t][i][e]);
           top = fmaxf(top, m < kInf ? m : 0.f);
         }
     int ex = exponent_for(wave_max(top));
-    int shrink = 0;  // earlier codes are multiplied by 2^-shrink
-    if (lo > 0) {
-      int old = static_cast<int>((__float_as_uint(*scale) >> 23) & 255u) - 127;
-      old = old < -126 ? -126 : old > 127 ? 127 : old;
-      ex = ex > old ? ex : old;
-      shrink = ex - old;
-    }
-    const float inv = pow2(-ex < -126 ? -126 : -ex);
-    const float fix = ex > 126 ? 0.5f : 1.f;  // 2^-127 is no normal number
+    old = old < -126 ? -126 : old > 127 ? 127 : old;
+    ex = ex > old ? ex : old;
+    const int shrink = lo > 0 ? ex - old : 0;  // earlier codes are multiplied by 2^-shrink
+    // 2^-ex as two factors: 2^-127 is no normal number
+    const float inv = pow2(-ex < -126 ? -126 : -ex), fix = ex > 126 ? 0.5f : 1.f;
     const float less = shrink > 126 ? 0.f : pow2(-shrink);
     if (lane == 0) *scale = pow2(ex);
 
     if (what == 0) {
-      uint8_t* k = static_cast<uint8_t*>(a.c.k) + ((page * heads + head) * a.c.page + pb * 16) * D;
 #pragma unroll
-      for (int t = 0; t < 16; ++t)
+      for (int t = 0; t < 4; ++t) {
+        const int place = 4 * g + t;
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-          const int c = 2 * (lane + 64 * i);
-          if (c >= D || t >= hi) continue;
-          uint16_t* p = reinterpret_cast<uint16_t*>(k + static_cast<int64_t>(t) * D + c);
-          if (t >= lo) {
-            *p = static_cast<uint16_t>(codes2(x[t][i][0] * inv * fix, x[t][i][1] * inv * fix));
+          const int c = c0 + 128 * i;
+          if (c >= D || place >= hi) continue;
+          tok_u32x2* p = reinterpret_cast<tok_u32x2*>(codes + static_cast<int64_t>(place) * D + c);
+          if (place >= lo) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = x[t][i][e] * inv * fix;
+            *p = tok_u32x2{codes2(v[0], v[1]) | codes2(v[2], v[3]) << 16, codes2(v[4], v[5]) | codes2(v[6], v[7]) << 16};
           } else if (shrink) {
-            const tok_f32x2 f = __builtin_amdgcn_cvt_pk_f32_fp8(*p, false);
-            *p = static_cast<uint16_t>(codes2(f[0] * less, f[1] * less));
+            const tok_u32x2 w = *p;
+            *p = tok_u32x2{shrunk(w[0], less), shrunk(w[1], less)};
           }
         }
+      }
     } else {
-      uint8_t* v = static_cast<uint8_t*>(a.c.v) + ((page * heads + head) * nb + pb) * D * 16;
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
-        const int c = 2 * (lane + 64 * i);
-        if (c >= D) continue;
+        uint32_t d[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float v[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) v[t] = x[t][i][e] * inv * fix;
+          d[e] = codes2(v[0], v[1]) | codes2(v[2], v[3]) << 16;
+        }
+        transpose(d);
+        if (c0 + 128 * i >= D) continue;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          tok_u32x4* p = reinterpret_cast<tok_u32x4*>(v + (c + e) * 16);
-          tok_u32x4 w = {0, 0, 0, 0};
-          if (lo > 0 || hi < 16) w = *p;
+          tok_u32x4 w;
 #pragma unroll
-          for (int t = 0; t < 16; t += 2) {
-            const int sh = 8 * (t & 3);
-            uint32_t old = (w[t >> 2] >> sh) & 0xffffu;
-            if (shrink && t < lo) {
-              const tok_f32x2 f = __builtin_amdgcn_cvt_pk_f32_fp8(old, false);
-              old = codes2(f[0] * less, f[1] * less);
+          for (int q = 0; q < 4; ++q) {
+            w[q] = d[4 * e + q];
+            if (lo > 0 || hi < 16) {
+              uint32_t before = 0, now = 0;  // bytes of earlier and of new tokens
+#pragma unroll
+              for (int t = 0; t < 4; ++t) {
+                if (4 * q + t < lo) before |= 255u << (8 * t);
+                if (4 * q + t >= lo && 4 * q + t < hi) now |= 255u << (8 * t);
+              }
+              uint32_t o = was[i][e][q];
+              if (shrink) o = (o & ~before) | (shrunk(o, less) & before);
+              w[q] = (w[q] & now) | (o & ~now);
             }
-            const uint32_t now = codes2(x[t][i][e] * inv * fix, x[t + 1][i][e] * inv * fix);
-            const uint32_t keep = (t >= lo && t < hi ? 0u : 0xffu) | (t + 1 >= lo && t + 1 < hi ? 0u : 0xff00u);
-            w[t >> 2] = (w[t >> 2] & ~(0xffffu << sh)) | (((old & keep) | (now & ~keep)) << sh);
           }
-          *p = w;
+          *reinterpret_cast<tok_u32x4*>(codes + (c0 + 128 * i + 2 * g + e) * 16) = w;
         }
       }
     }
   }
 }
 
-template <class E, bool AL>
-hipError_t run(const AppendArgs& a, dim3 grid, hipStream_t s) {
-  auto k = a.c.dim <= 128 ? kv_append_k<E, 1, AL> : kv_append_k<E, 2, AL>;
-  hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
-  return hipGetLastError();
-}
-
 template <class E>
 hipError_t typed(const AppendArgs& a, dim3 grid, hipStream_t s) {
-  const int64_t two = 2 * static_cast<int64_t>(sizeof(typename E::store));
-  auto even = [&](const void* p, int64_t ld) {
-    return reinterpret_cast<uintptr_t>(p) % two == 0 && ld % 2 == 0;
-  };
-  const bool al = even(a.k, a.ld_k) && even(a.v, a.ld_v) && (!a.q_out || (even(a.q, a.ld_q) && even(a.q_out, 0)));
-  return al ? run<E, true>(a, grid, s) : run<E, false>(a, grid, s);
+  auto k = a.c.dim <= 128 ? kv_append_k<E, 1> : kv_append_k<E, 2>;
+  hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace

@@ -307,7 +307,7 @@ __device__ inline void weigh(const tok_f32x4 (&s)[4], float cg, int f, float m, 
 // 64-token tile of the split and join their results in LDS.  Columns are
 // numbered token by token, the G heads of a token side by side.
 template <class E, int DP>  // DP: channels padded to 64
-__global__ __launch_bounds__(256) void attend_few(Dev a) {
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few(Dev a) {
   typedef Form<E> F;
   constexpr int KS = DP / 32, DT = DP / 16, NQ = F::NQ, NP = F::NP;
   typedef typename E::store S;
@@ -340,30 +340,57 @@ __global__ __launch_bounds__(256) void attend_few(Dev a) {
   int unit = -126;           // E
 
   const int32_t* pages = a.table + static_cast<int64_t>(b) * a.cols;
-  uint32_t page = peek(a, pages, (t0 + wave) * 4 + g, ue);
-  for (int tile = t0 + wave; tile < t1; tile += 4) {
-    const int blk0 = tile * 4, tok0 = tile * 64;
-    const uint32_t vb = settle(a, hk, blk0 + g, page), kb = __shfl(vb, (r >> 2) * 16);
-    page = peek(a, pages, blk0 + 16 + g, ue);
-    const bool kok = kb != kNone, vok = vb != kNone;
-    const uint8_t* kp = a.k + (static_cast<int64_t>(kb) * 16 + (r & 3)) * D + g * 16;
-    const uint8_t* vp = a.v + (static_cast<int64_t>(vb) * D + r) * 16;
-    // scales of block g; c times the key's, 0 kept off so that -inf stays -inf
-    const float cg = vok ? fmaxf(a.c * a.ks[vb], 0x1p-126f) : 1.f;
-    const int ve = vok ? exponent_of(a.vs[vb]) : -126;
+  // A tile's codes and scales are loaded while the tile before is worked on,
+  // where the registers hold both.
+  constexpr bool AHEAD = DP <= 128;
+  struct Tile {
+    uint32_t vb;  // block g, or kNone
+    float ks, vs;
     tok_u32x4 kv[4][DP / 64], vv[DT];
+  };
+  auto load = [&](int tile, uint32_t page, Tile& x) __attribute__((always_inline)) {
+    x.vb = settle(a, hk, tile * 4 + g, page);
+    const uint32_t kb = __shfl(x.vb, (r >> 2) * 16);
+    const bool kok = kb != kNone, vok = x.vb != kNone;
+    const uint8_t* kp = a.k + (static_cast<int64_t>(kb) * 16 + (r & 3)) * D + g * 16;
+    const uint8_t* vp = a.v + (static_cast<int64_t>(x.vb) * D + r) * 16;
+    x.ks = vok ? a.ks[x.vb] : 1.f;
+    x.vs = vok ? a.vs[x.vb] : 0x1p-126f;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int j = 0; j < DP / 64; ++j) {
-        kv[t][j] = tok_u32x4{0, 0, 0, 0};
-        if (kok && j * 64 + g * 16 < D) kv[t][j] = *reinterpret_cast<const tok_u32x4*>(kp + 4 * t * D + j * 64);
+        x.kv[t][j] = tok_u32x4{0, 0, 0, 0};
+        if (kok && j * 64 + g * 16 < D) x.kv[t][j] = *reinterpret_cast<const tok_u32x4*>(kp + 4 * t * D + j * 64);
       }
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      vv[d] = tok_u32x4{0, 0, 0, 0};
-      if (vok && d * 16 < D) vv[d] = *reinterpret_cast<const tok_u32x4*>(vp + d * 256);
+      x.vv[d] = tok_u32x4{0, 0, 0, 0};
+      if (vok && d * 16 < D) x.vv[d] = *reinterpret_cast<const tok_u32x4*>(vp + d * 256);
     }
+  };
+  Tile next;
+  uint32_t page = peek(a, pages, (t0 + wave) * 4 + g, ue);
+  if (AHEAD && t0 + wave < t1) load(t0 + wave, page, next);
+  page = peek(a, pages, (t0 + wave + (AHEAD ? 4 : 0)) * 4 + g, ue);
+  for (int tile = t0 + wave; tile < t1; tile += 4) {
+    const int tok0 = tile * 64;
+    Tile now;
+    if (AHEAD) {
+      now = next;
+      if (tile + 4 < t1) load(tile + 4, page, next);
+      page = peek(a, pages, (tile + 8) * 4 + g, ue);
+    } else {
+      load(tile, page, now);
+      page = peek(a, pages, (tile + 4) * 4 + g, ue);
+    }
+    const uint32_t vb = now.vb;
+    const bool vok = vb != kNone;
+    auto& kv = now.kv;
+    auto& vv = now.vv;
+    // c times the key scale of block g; 0 kept off so that -inf stays -inf
+    const float cg = fmaxf(a.c * now.ks, 0x1p-126f);
+    const int ve = exponent_of(now.vs);
     tok_f32x4 s[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
@@ -728,29 +755,47 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
 }
 
 // out and lse from the partial results of a split call: one wave a row.
-template <class E>
+// Everything of U splits is read at once: a chain of reads was most of a single
+// token's time.
+template <class E, int NV>  // NV: channels a lane
 __global__ __launch_bounds__(256) void attend_join(Dev a) {
+  constexpr int U = 8;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6), rows = static_cast<int64_t>(a.T) * a.q_heads;
   if (row >= rows) return;
   const int lane = threadIdx.x & 63, D = a.D;
   const float* part = a.part + row * (D + 2);
   const int64_t step = rows * (D + 2);
-  float m = -kInf;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, part[s * step]);
-  const float ref = m == -kInf ? 0.f : m;
-  float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.splits; ++s) {
-    const float part_l = part[s * step + 1];
-    if (part_l == 0.f) continue;  // nothing seen
-    const float w = __builtin_amdgcn_exp2f(part[s * step] - ref);
-    l += w * part_l;
+  int ch[NV];  // lanes past the last channel work on it again and store nothing
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < D) o[i] += w * part[s * step + 2 + lane + 64 * i];
+  for (int i = 0; i < NV; ++i) ch[i] = lane + 64 * i < D ? lane + 64 * i : D - 1;
+  float m = -kInf, l = 0.f, o[NV] = {};
+  for (int s0 = 0; s0 < a.splits; s0 += U) {
+    const int n = a.splits - s0 < U ? a.splits - s0 : U;
+    const float* p = part + (s0 + (lane < n ? lane : n - 1)) * step;
+    const float pm = p[0], pl = p[1];
+    float v[U][NV];
+#pragma unroll
+    for (int s = 0; s < U; ++s)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) v[s][i] = part[(s0 + (s < n ? s : n - 1)) * step + 2 + ch[i]];
+    const float next = fmaxf(m, wave_max(pm)), ref = next == -kInf ? 0.f : next;
+    const float down = __builtin_amdgcn_exp2f(m - ref);
+    const float w = lane < n && pl != 0.f ? __builtin_amdgcn_exp2f(pm - ref) : 0.f;  // 0: nothing seen
+    m = next;
+    l = l * down + (lane < n ? w * pl : 0.f);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) o[i] *= down;
+#pragma unroll
+    for (int s = 0; s < U; ++s) {
+      const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
+#pragma unroll
+      for (int i = 0; i < NV; ++i) o[i] += s < n ? ws * v[s][i] : 0.f;
+    }
   }
+  l = wave_sum(l);
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < NV; ++i)
     if (lane + 64 * i < D) static_cast<typename E::store*>(a.out)[row * D + lane + 64 * i] = E::narrow(o[i] * inv);
   if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -kInf : m * kLn2 + logf(l);
 }
@@ -805,7 +850,8 @@ hipError_t run(const AttendArgs& h, const AttendPlan& p, int dtype, hipStream_t 
   }
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.splits > 1) {
-    hipLaunchKernelGGL(attend_join<E>, dim3(static_cast<unsigned>(joins)), dim3(256), 0, s, a);
+    auto join = a.D <= 64 ? attend_join<E, 1> : a.D <= 128 ? attend_join<E, 2> : attend_join<E, 4>;
+    hipLaunchKernelGGL(join, dim3(static_cast<unsigned>(joins)), dim3(256), 0, s, a);
     e = hipGetLastError();
   }
   return e;
@@ -822,10 +868,13 @@ AttendPlan plan_attend(const c3c_kv_cache& c, const c3c_kv_batch& b, int dtype, 
   const int64_t cus = device_compute_units(), most = up(tiles, 4);
   int64_t s = 1;
   if (few(columns)) {
-    // enough workgroups to fill the device several times (sequences are
-    // ragged), of at least one tile a wave
-    const int64_t want = up(8 * cus, base);
-    s = want < most ? want : most;
+    // two workgroups a compute unit, of at least one tile a wave and at most
+    // 256 tiles: a split more costs its start (64 sequences of 1000 to 32768
+    // tokens, 8 heads of 128: one split 452 us, four 494), but a sequence far
+    // longer than the others would be waited for
+    s = up(2 * cus, base);
+    if (s < up(tiles, 256)) s = up(tiles, 256);
+    if (s > most) s = most;
   } else {
     // the fewest rounds of workgroups, counted in tiles: each round costs its
     // tiles and about 3 more to begin and end, the join its launch and its

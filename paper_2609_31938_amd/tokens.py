@@ -25,10 +25,12 @@ import ctypes as C
 import torch
 
 from . import c3c
-from .c3c import _addr, _raise, _stream, dtype_of, lib
+from .c3c import _raise, lib
 
 BLOCK = 16  # C3C_KV_BLOCK: tokens that share a scale
 DTYPES = dict(c3c.DTYPES, i8=16)
+_NAMES = {torch.bfloat16: "bf16", torch.float16: "f16", torch.float32: "f32"}
+_TORCH = {n: d for d, n in _NAMES.items()}
 PAIRS = {"half": 0, "next": 1}
 
 _vp, _i64, _int, _f32, _P = C.c_void_p, C.c_int64, C.c_int, C.c_float, C.POINTER
@@ -70,21 +72,42 @@ lib.c3c_paged_attention.argtypes = [_vp, _P(_CacheDesc), _P(_BatchDesc), _int, _
                                     _vp, _vp]
 
 
+# A call of a single token takes a few microseconds on the device: what the
+# host does for it is kept short.  torch.cuda.current_stream() alone takes 2.8
+# us, the raw handle 0.1.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _stream(stream, t):
+    """The HIP stream of a call: the given one, or the current one of t's device."""
+    return _raw_stream(t.get_device()) if stream is None else getattr(stream, "cuda_stream", stream)
+
+
+def _addr(t, name):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    return t.data_ptr() or None
+
+
 def _check(t, name, dtype, shape):
     """The device address of a contiguous tensor of this dtype and shape."""
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    return _addr(t, name)
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    return t.data_ptr() or None
 
 
 def _float_dtype(t, name):
-    if t.dtype not in (torch.bfloat16, torch.float16, torch.float32):
+    n = _NAMES.get(t.dtype)
+    if n is None:
         raise ValueError(f"{name} has dtype {t.dtype}, expected bf16, f16 or f32")
-    return dtype_of(t)
+    return n
 
 
 def _rows(t, name):
@@ -101,10 +124,10 @@ def quantize_rows(ctx, x, q=None, scale=None, stream=None):
     max|x[t]| / 127.  Rows of x may be strided."""
     dtype, ld = _float_dtype(x, "x"), _rows(x, "x")
     T, n = x.shape
-    q = torch.empty((T, n), dtype=torch.int8, device=x.device) if q is None else q
-    scale = torch.empty(T, dtype=torch.float32, device=x.device) if scale is None else scale
+    q = x.new_empty((T, n), dtype=torch.int8) if q is None else q
+    scale = x.new_empty(T, dtype=torch.float32) if scale is None else scale
     _raise(lib.c3c_quantize_rows(ctx._h, T, n, ld, DTYPES[dtype], _addr(x, "x"), _check(q, "q", torch.int8, (T, n)),
-                                 _check(scale, "scale", torch.float32, (T,)), _stream(stream)), ctx, "c3c_quantize_rows")
+                                 _check(scale, "scale", torch.float32, (T,)), _stream(stream, x)), ctx, "c3c_quantize_rows")
     return q, scale
 
 
@@ -128,16 +151,17 @@ def linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=N
     M, K = x.shape
     N = w.shape[0]
     yd = out_dtype or (_float_dtype(out, "out") if out is not None else "bf16" if i8 else xd)
-    ydt = c3c._torch_dtype(yd)
+    ydt = _TORCH[yd]
     if out is None:
-        out = torch.empty((M, N), dtype=ydt, device=x.device)
+        out = x.new_empty((M, N), dtype=ydt)
     d = LinearDesc(M, N, K, ld, DTYPES[xd], DTYPES[yd])
     st = lib.c3c_linear_i8(
         ctx._h, C.byref(d), _addr(x, "x"), None if x_scale is None else _check(x_scale, "x_scale", torch.float32, (M,)),
         _check(w, "w", torch.int8, (N, K)), _check(w_scale, "w_scale", torch.float32, (N,)),
         None if bias is None else _check(bias, "bias", torch.float32, (N,)), _check(out, "out", ydt, (M, N)),
-        _stream(stream))
-    _raise(st, ctx, "c3c_linear_i8")
+        _stream(stream, x))
+    if st:
+        _raise(st, ctx, "c3c_linear_i8")
     return out
 
 
@@ -155,14 +179,14 @@ def norm_gate(ctx, h, y=None, gate=None, *, post=None, pre=None, alpha=1.0, eps=
     if h.dim() != 2:
         raise ValueError("h must be 2-d")
     T, n = h.shape
-    dt, dev, shape = h.dtype, h.device, h.shape
+    dt, shape = h.dtype, h.shape
     if h_out is None:
-        h_out = torch.empty(shape, dtype=dt, device=dev)
+        h_out = torch.empty_like(h)
     if quantize:
-        u_q = torch.empty(shape, dtype=torch.int8, device=dev) if u_q is None else u_q
-        u_scale = torch.empty(T, dtype=torch.float32, device=dev) if u_scale is None else u_scale
+        u_q = torch.empty_like(h, dtype=torch.int8) if u_q is None else u_q
+        u_scale = h.new_empty(T, dtype=torch.float32) if u_scale is None else u_scale
     elif pre is not None and u is None:
-        u = torch.empty(shape, dtype=dt, device=dev)
+        u = torch.empty_like(h)
     groups = -(-T // rows_per_gate) if rows_per_gate > 0 else 0
     d = NormDesc(T, n, rows_per_gate, alpha, eps, DTYPES[dtype], 0)
     st = lib.c3c_norm_gate(
@@ -171,8 +195,9 @@ def norm_gate(ctx, h, y=None, gate=None, *, post=None, pre=None, alpha=1.0, eps=
         None if post is None else _check(post, "post", torch.float32, (n,)),
         None if pre is None else _check(pre, "pre", torch.float32, (n,)), _check(h_out, "h_out", dt, shape),
         None if u is None else _check(u, "u", dt, shape), None if u_q is None else _check(u_q, "u_q", torch.int8, shape),
-        None if u_scale is None else _check(u_scale, "u_scale", torch.float32, (T,)), _stream(stream))
-    _raise(st, ctx, "c3c_norm_gate")
+        None if u_scale is None else _check(u_scale, "u_scale", torch.float32, (T,)), _stream(stream, h))
+    if st:
+        _raise(st, ctx, "c3c_norm_gate")
     return (h_out, u_q, u_scale) if quantize else (h_out, u)
 
 
@@ -234,9 +259,10 @@ def _heads(t, name, dtype, T, heads, dim):
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
     if t.shape != (T, heads, dim):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {(T, heads, dim)}")
-    if (dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim):
+    by_token, by_head, by_channel = t.stride()
+    if by_channel != 1 or (heads > 1 and by_head != dim):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return _addr(t, name), t.stride(0) if T > 1 else heads * dim
+    return _addr(t, name), by_token if T > 1 else heads * dim
 
 
 def kv_append(ctx, cache: KVCache, batch: Batch, k, v, *, q=None, cos=None, sin=None, pos=None, pairs="half",
@@ -255,7 +281,7 @@ def kv_append(ctx, cache: KVCache, batch: Batch, k, v, *, q=None, cos=None, sin=
         qh = q.shape[1]
         pq, ldq = _heads(q, "q", dt, T, qh, cache.dim)
         if q_out is None:
-            q_out = torch.empty((T, qh, cache.dim), dtype=dt, device=k.device)
+            q_out = k.new_empty((T, qh, cache.dim))
         po = _check(q_out, "q_out", dt, (T, qh, cache.dim))
     elif q_out is not None:
         raise ValueError("q_out goes with q")
@@ -267,8 +293,9 @@ def kv_append(ctx, cache: KVCache, batch: Batch, k, v, *, q=None, cos=None, sin=
                                  None if pos is None else _check(pos, "pos", torch.int32, (T,)), rows, 2 * half,
                                  PAIRS[pairs], 0))
     st = lib.c3c_kv_append(ctx._h, C.byref(cache._d), batch._of(T), rope, DTYPES[dtype], qh, pq or None, ldq, pk, ldk,
-                           pv, ldv, po or None, _stream(stream))
-    _raise(st, ctx, "c3c_kv_append")
+                           pv, ldv, po or None, _stream(stream, k))
+    if st:
+        _raise(st, ctx, "c3c_kv_append")
     return q_out
 
 
@@ -293,10 +320,11 @@ def paged_attention(ctx, cache: KVCache, batch: Batch, q, *, scale=None, causal:
     T, qh, dim = q.shape
     pq, ldq = _heads(q, "q", q.dtype, T, qh, cache.dim)
     if out is None:
-        out = torch.empty((T, qh, dim), dtype=q.dtype, device=q.device)
+        out = q.new_empty((T, qh, dim))
     st = lib.c3c_paged_attention(
         ctx._h, C.byref(cache._d), batch._of(T), DTYPES[dtype], qh, pq, ldq, dim ** -0.5 if scale is None else scale,
         int(causal), window, _check(out, "out", q.dtype, (T, qh, dim)),
-        None if lse is None else _check(lse, "lse", torch.float32, (T, qh)), _stream(stream))
-    _raise(st, ctx, "c3c_paged_attention")
+        None if lse is None else _check(lse, "lse", torch.float32, (T, qh)), _stream(stream, q))
+    if st:
+        _raise(st, ctx, "c3c_paged_attention")
     return out
