@@ -8,14 +8,21 @@
 // skinny: at most 64 tokens.  The weights are read once, straight into
 //   registers (no tile of them is used twice), by 4 waves that share 16 rows
 //   and take every fourth 128-byte piece of K; their sums meet in LDS.
-// tiled: BM x BN tiles, 128 bytes of K a stage, two stages in LDS.  With
-//   16-byte rows the stages are loaded straight into LDS (the buffer's bounds
-//   make rows past M or N and pieces past K zero); rows of any other length go
-//   through registers.  A 16-byte piece c of row r lies at place c ^ (r & 7):
-//   the 16 rows that a fragment read touches then spread over all banks.
+// tiled: BM x BN tiles.  64 bytes of K a stage, NS stages in an LDS ring; the
+//   fragments of the next stage are read while the products of this one run.
+//   What a stage costs is little beside what its bytes wait for (L2 and, for
+//   one line of five, the memory side cache), so the ring is as deep as LDS
+//   allows.  With 16-byte rows the stages are loaded straight into LDS (the
+//   buffer's bounds make rows past M or N and pieces past K zero); rows of any
+//   other length go through registers.  A 16-byte piece c of row r lies at
+//   place c ^ (r / 4 & 3): the 16 rows that a fragment read touches then
+//   spread over all banks.
 #include "token_dev.h"
 #include "tokens_internal.h"
 
+#ifndef NSBIG
+#define NSBIG 4
+#endif
 namespace c3c {
 namespace {
 
@@ -32,14 +39,33 @@ struct LinArgs {
   int y_dtype;
 };
 
-__device__ inline void put4(const LinArgs& a, int64_t m, int64_t n, tok_i32x4 v) {
-  const float s = a.x_scale[m];
+// w_scale and bias of four consecutive channels (the last one's past N)
+struct Channels {
+  float s[4], b[4];
+};
+__device__ inline Channels channels(const LinArgs& a, int64_t n) {
+  Channels c;
+  if (n + 4 <= a.N) {
+    __builtin_memcpy(c.s, a.w_scale + n, 16);
+    if (a.bias) __builtin_memcpy(c.b, a.bias + n, 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t at = n + i < a.N ? n + i : a.N - 1;
+      c.s[i] = a.w_scale[at];
+      if (a.bias) c.b[i] = a.bias[at];
+    }
+  }
+  return c;
+}
+
+// four results of token m, of which those below N are stored
+__device__ inline void put4(const LinArgs& a, int64_t m, int64_t n, tok_i32x4 v, float s, const Channels& c) {
   float f[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int64_t nn = n + i < a.N ? n + i : a.N - 1;
-    f[i] = static_cast<float>(v[i]) * s * a.w_scale[nn];
-    if (a.bias) f[i] += a.bias[nn];
+    f[i] = static_cast<float>(v[i]) * s * c.s[i];
+    if (a.bias) f[i] += c.b[i];
   }
   const int64_t at = m * a.N + n;
   if (a.y_dtype == C3C_DTYPE_F32) {
@@ -130,21 +156,24 @@ __global__ __launch_bounds__(256) void linear_skinny(LinArgs a) {
 #pragma unroll
     for (int w = 0; w < 3; ++w) acc[t] += sums[w][t][lane];
     const int64_t m = t * 16 + r, n = n0 + g * 4;
-    if (m < a.M && n < a.N) put4(a, m, n, acc[t]);
+    if (m < a.M && n < a.N) put4(a, m, n, acc[t], a.x_scale[m], channels(a, n));
   }
 }
 
-constexpr int BK = 128;  // bytes of K a stage
+constexpr int BK = 64;  // bytes of K a stage
 
-// NW waves, each with a WM x WN part of the tile.
-template <int BM, int BN, int WM, int WN, bool AL>
+// vmcnt(n), with the other counters left alone
+#define C3C_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | (((n) >> 4) << 14) | (7 << 4) | (15 << 8))
+
+// (BM / WM) * (BN / WN) waves, each with a WM x WN part of the tile.
+template <int BM, int BN, int WM, int WN, int NS, bool AL>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinArgs a) {
   constexpr int NW = (BM / WM) * (BN / WN);
   constexpr int MT = WM / 16, NT = WN / 16;
   constexpr int ROWS = BM + BN;              // rows of w, then rows of x
-  constexpr int LOADS = ROWS / 8 / NW;       // 1024-byte loads a wave and stage
-  static_assert(ROWS % (8 * NW) == 0 && BN % 8 == 0, "whole loads");
-  __shared__ __align__(16) int8_t lds[2 * ROWS * BK];
+  constexpr int LOADS = ROWS / 16 / NW;      // 1024-byte loads a wave and stage
+  static_assert(ROWS % (16 * NW) == 0 && BN % 16 == 0, "whole loads");
+  __shared__ __align__(16) int8_t lds[NS * ROWS * BK];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
 
@@ -167,94 +196,122 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
 
   const int stages = static_cast<int>((a.K + BK - 1) / BK);
   const int s0 = static_cast<int>(static_cast<int64_t>(stages) * split / a.splits);
-  const int s1 = static_cast<int>(static_cast<int64_t>(stages) * (split + 1) / a.splits);
+  const int count = static_cast<int>(static_cast<int64_t>(stages) * (split + 1) / a.splits) - s0;
 
   const int64_t nrows = a.N - n0 < BN ? a.N - n0 : BN, mrows = a.M - m0 < BM ? a.M - m0 : BM;
   const int8_t* wb = a.w + n0 * a.K;
   const int8_t* xb = a.x + m0 * a.ldx;
-  // the part of a 1024-byte load (8 rows) that this lane brings: row lane / 8,
-  // place lane % 8, hence piece (lane % 8) ^ (lane / 8)
-  const int lrow = lane >> 3, lpiece = (lane & 7) ^ lrow;
-  tok_i32x4 staged[LOADS];  // !AL
+  // the part of a 1024-byte load (16 rows) that this lane brings: row lane / 4,
+  // place lane % 4
+  const int lrow = lane >> 2, lpiece = (lane & 3) ^ (lane >> 4);
   const __amdgpu_buffer_rsrc_t wrs = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<int8_t*>(wb), 0, static_cast<int>(nrows * a.K), 0x00020000);
   const __amdgpu_buffer_rsrc_t xrs = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<int8_t*>(xb), 0, static_cast<int>((mrows - 1) * a.ldx + a.K), 0x00020000);
-  auto load = [&](int st, int buf) __attribute__((always_inline)) {
-    const int k = st * BK + lpiece * 16;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int row = (i * NW + wave) * 8;  // of ROWS, uniform; whole loads are of w or of x
-      const bool isw = row < BN;
-      const int rr = (isw ? row : row - BN) + lrow;
-      if (AL) {
-        const int ld = static_cast<int>(isw ? a.K : a.ldx);
-        const int off = k < a.K ? rr * ld + k : 0x7fffffff;
-        lds_void* to = (lds_void*)(lds + buf * ROWS * BK + row * BK);
-        if (isw)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(wrs, to, 16, off, 0, 0, 0);
-        else
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(xrs, to, 16, off, 0, 0, 0);
-      } else {
-        const int64_t ld = isw ? a.K : a.ldx;
-        const bool ok = rr < (isw ? nrows : mrows);
-        staged[i] = piece<false>((isw ? wb : xb) + (ok ? rr * ld + k : 0), ok ? a.K - k : 0);
-      }
+  tok_i32x4 staged[LOADS];  // !AL
+  // load i of stage st of this split
+  auto load = [&](int st, int i) __attribute__((always_inline)) {
+    const int k = (s0 + st) * BK + lpiece * 16, buf = st % NS;
+    const int row = (i * NW + wave) * 16;  // of ROWS, uniform; whole loads are of w or of x
+    const bool isw = row < BN;
+    const int rr = (isw ? row : row - BN) + lrow;
+    if (AL) {
+      const int ld = static_cast<int>(isw ? a.K : a.ldx);
+      // past K: a sign bit takes the offset out of every buffer
+      const int off = (rr * ld + k) | ((static_cast<int>(a.K) - 1 - k) & static_cast<int>(0x80000000u));
+      lds_void* to = (lds_void*)(lds + buf * ROWS * BK + row * BK);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(isw ? wrs : xrs, to, 16, off, 0, 0, 0);
+    } else {
+      const int64_t ld = isw ? a.K : a.ldx;
+      const bool ok = rr < (isw ? nrows : mrows);
+      staged[i] = piece<false>((isw ? wb : xb) + (ok ? rr * ld + k : 0), ok ? a.K - k : 0);
     }
   };
-  auto settle = [&](int buf) __attribute__((always_inline)) {
-    if (!AL) {
+  auto settle = [&](int st) __attribute__((always_inline)) {  // !AL
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        *reinterpret_cast<tok_i32x4*>(lds + buf * ROWS * BK + (i * NW + wave) * 8 * BK + lane * 16) = staged[i];
-    }
+    for (int i = 0; i < LOADS; ++i)
+      *reinterpret_cast<tok_i32x4*>(lds + (st % NS) * ROWS * BK + (i * NW + wave) * 16 * BK + lane * 16) = staged[i];
   };
 
   const int wm = wave % (BM / WM) * WM, wn = wave / (BM / WM) * WN;
+  // every fragment row is congruent to r modulo 16
+  const int at = r * BK + ((g ^ (r >> 2)) & 3) * 16;
+  struct Frags {
+    tok_i32x4 w[NT], x[MT];
+  };
+  // fragment n of NT + MT
+  auto read = [&](int st, int n, Frags& f) __attribute__((always_inline)) {
+    const int8_t* base = lds + (st % NS) * ROWS * BK + at;
+    if (n < NT)
+      f.w[n] = *reinterpret_cast<const tok_i32x4*>(base + (wn + n * 16) * BK);
+    else
+      f.x[n - NT] = *reinterpret_cast<const tok_i32x4*>(base + (BN + wm + (n - NT) * 16) * BK);
+  };
   tok_i32x4 acc[NT][MT];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int j = 0; j < MT; ++j) acc[i][j] = tok_i32x4{0, 0, 0, 0};
 
-  if (s0 < s1) {
-    load(s0, 0);
-    settle(0);
-  }
-  __syncthreads();
-  for (int st = s0; st < s1; ++st) {
-    const int cur = (st - s0) & 1;
-    if (st + 1 < s1) load(st + 1, cur ^ 1);
-    const int8_t* base = lds + cur * ROWS * BK;
+  // One round: stage st's products, stage st + 1's fragments, stage st + NS's
+  // loads into the place of stage st, whose fragments every wave has read
+  // when it comes to the barrier.  Reads and products take turns: reads all at
+  // once would keep LDS and the matrix cores busy one after the other (a
+  // stage's reads and writes take LDS about as long as its products take the
+  // matrix cores).  What is read and loaded past the last stage is never used.
+  auto round = [&](int st, const Frags& cur, Frags& nxt) __attribute__((always_inline)) {
+    if (AL) C3C_VMCNT((NS - 2) * LOADS);  // stage st + 1 has landed: the loads behind it may be on their way
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    constexpr int STEPS = NT + MT;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      // every fragment row is congruent to r modulo 8
-      const int place = ((ks * 4 + g) ^ (r & 7)) * 16;
-      tok_i32x4 av[NT], bv[MT];
+    for (int n = 0; n < STEPS; ++n) {
+      __builtin_amdgcn_sched_barrier(0);
+      read(st + 1, n, nxt);
 #pragma unroll
-      for (int i = 0; i < NT; ++i)
-        av[i] = *reinterpret_cast<const tok_i32x4*>(base + (wn + i * 16 + r) * BK + place);
+      for (int i = 0; i < LOADS; ++i)
+        if (i * STEPS / LOADS == n) load(st + (AL ? NS : 2), i);
 #pragma unroll
-      for (int j = 0; j < MT; ++j)
-        bv[j] = *reinterpret_cast<const tok_i32x4*>(base + (BN + wm + j * 16 + r) * BK + place);
-#pragma unroll
-      for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(av[i], bv[j], acc[i][j], 0, 0, 0);
+      for (int e = n * NT * MT / STEPS; e < (n + 1) * NT * MT / STEPS; ++e)
+        acc[e / MT][e % MT] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cur.w[e / MT], cur.x[e % MT], acc[e / MT][e % MT], 0, 0, 0);
     }
-    if (st + 1 < s1) settle(cur ^ 1);
-    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);
+    if (!AL) settle(st + 2);
+  };
+  Frags fa, fb;
+#pragma unroll
+  for (int s = 0; s < (AL ? NS : 2); ++s) {
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load(s, i);
+    if (!AL) settle(s);
   }
+  if (AL) C3C_VMCNT((NS - 1) * LOADS);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+  for (int n = 0; n < NT + MT; ++n) read(0, n, fa);
+  for (int st = 0; st < count; st += 2) {
+    round(st, fa, fb);
+    if (st + 1 < count) round(st + 1, fb, fa);
+  }
+  C3C_VMCNT(0);  // nothing is on its way into LDS when the workgroup ends
 
+  float xs[MT];
+  if (!a.part) {
 #pragma unroll
-  for (int j = 0; j < MT; ++j) {
-    const int64_t m = m0 + wm + j * 16 + r;
-    if (m >= a.M) continue;
+    for (int j = 0; j < MT; ++j) {
+      const int64_t m = m0 + wm + j * 16 + r;
+      xs[j] = a.x_scale[m < a.M ? m : a.M - 1];
+    }
+  }
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      const int64_t n = n0 + wn + i * 16 + g * 4;
-      if (n >= a.N) continue;
+  for (int i = 0; i < NT; ++i) {
+    const int64_t n = n0 + wn + i * 16 + g * 4;
+    if (n >= a.N) continue;
+    Channels c;
+    if (!a.part) c = channels(a, n);
+#pragma unroll
+    for (int j = 0; j < MT; ++j) {
+      const int64_t m = m0 + wm + j * 16 + r;
+      if (m >= a.M) continue;
       if (a.part) {
         int32_t* p = a.part + (split * a.M + m) * a.N + n;
         if (n + 4 <= a.N) {
@@ -264,7 +321,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
             if (n + e < a.N) p[e] = acc[i][j][e];
         }
       } else {
-        put4(a, m, n, acc[i][j]);
+        put4(a, m, n, acc[i][j], xs[j], c);
       }
     }
   }
@@ -288,7 +345,7 @@ __global__ __launch_bounds__(256) void linear_join(LinArgs a) {
         if (n + e < a.N) v[e] += p[e];
     }
   }
-  put4(a, m, n, v);
+  put4(a, m, n, v, a.x_scale[m], channels(a, n));
 }
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -305,10 +362,10 @@ Tile tile_of(int64_t M, int64_t N) {
   return {64, 64};
 }
 
-template <int BM, int BN, int WM, int WN, bool AL>
+template <int BM, int BN, int WM, int WN, int NS, bool AL>
 hipError_t run_tiled(LinArgs a, hipStream_t s) {
   constexpr int threads = (BM / WM) * (BN / WN) * 64;
-  auto k = linear_tiled<BM, BN, WM, WN, AL>;
+  auto k = linear_tiled<BM, BN, WM, WN, NS, AL>;
   a.tiles_m = static_cast<int>(up(a.M, BM));
   a.tiles_n = static_cast<int>(up(a.N, BN));
   const int64_t blocks = static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.splits;
@@ -326,8 +383,8 @@ LinearPlan plan_linear_i8(int64_t M, int64_t N, int64_t K) {
   if (M <= kSkinny) return p;
   const Tile t = tile_of(M, N);
   const int64_t tiles = up(M, t.bm) * up(N, t.bn), stages = up(K, BK), cus = device_compute_units();
-  // at least 8 stages a split: fewer cost more in partial sums than they save
-  const int64_t s = cus / tiles < stages / 8 ? cus / tiles : stages / 8;
+  // at least 16 stages a split: fewer cost more in partial sums than they save
+  const int64_t s = cus / tiles < stages / 16 ? cus / tiles : stages / 16;
   if (s > 1) {
     p.splits = static_cast<int>(s);
     p.part_bytes = s * M * N * 4;
@@ -353,9 +410,9 @@ hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, in
     return hipGetLastError();
   }
   const Tile t = tile_of(M, N);
-  hipError_t e = t.bm == 256   ? (al ? run_tiled<256, 256, 128, 64, true>(a, s) : run_tiled<256, 256, 128, 64, false>(a, s))
-                 : t.bm == 128 ? (al ? run_tiled<128, 128, 64, 64, true>(a, s) : run_tiled<128, 128, 64, 64, false>(a, s))
-                               : (al ? run_tiled<64, 64, 32, 32, true>(a, s) : run_tiled<64, 64, 32, 32, false>(a, s));
+  hipError_t e = t.bm == 256   ? (al ? run_tiled<256, 256, 128, 64, NSBIG, true>(a, s) : run_tiled<256, 256, 128, 64, 4, false>(a, s))
+                 : t.bm == 128 ? (al ? run_tiled<128, 128, 64, 64, 4, true>(a, s) : run_tiled<128, 128, 64, 64, 4, false>(a, s))
+                               : (al ? run_tiled<64, 64, 32, 32, 4, true>(a, s) : run_tiled<64, 64, 32, 32, 4, false>(a, s));
   if (e == hipSuccess && part) {
     const int64_t blocks = up(M * up(N, 4), 256);
     if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
