@@ -7,29 +7,38 @@
 //
 // skinny: at most 64 tokens.  The weights are read once, straight into
 //   registers (no tile of them is used twice), by 4 waves that share 16 rows
-//   and take every fourth 128-byte piece of K; their sums meet in LDS.
-// tiled: BM x BN tiles.  64 bytes of K a stage, NS stages in an LDS ring; the
-//   fragments of the next stage are read while the products of this one run.
-//   What a stage costs is little beside what its bytes wait for (L2 and, for
-//   one line of five, the memory side cache), so the ring is as deep as LDS
-//   allows.  With 16-byte rows the stages are loaded straight into LDS (the
-//   buffer's bounds make rows past M or N and pieces past K zero); rows of any
-//   other length go through registers.  A 16-byte piece c of row r lies at
-//   place c ^ (r / 4 & 3): the 16 rows that a fragment read touches then
-//   spread over all banks.
+//   and take every fourth 128-byte piece of K, 8 of them in flight; their sums
+//   meet in LDS.  Up to 4 tokens of floats are quantised in the same kernel, by
+//   every workgroup for itself, while its first weights are on their way.
+// tiled: BM x BN tiles, stages of 64 or 128 bytes of K in an LDS ring, the
+//   fragments of the next 64 bytes read between the products of these.  The
+//   largest tile takes two stages of 128 bytes (whole cache lines; 794 us for
+//   32760 x 5120 x 5120 quantised normal values, 2.16 PFLOP/s) over four of 64
+//   (865 us).  What bounds it is the way to LDS: the loads alone take 710 us,
+//   the products alone 620 (at the clock that power leaves them; 3.5 PFLOP/s
+//   with random operands in registers).  With 16-byte rows the stages are loaded
+//   straight into LDS (the buffer's bounds make rows past M or N and pieces
+//   past K zero); rows of any other length go through registers.
 #include "token_dev.h"
 #include "tokens_internal.h"
 
-#ifndef NSBIG
-#define NSBIG 4
-#endif
 namespace c3c {
 namespace {
 
 typedef __attribute__((address_space(3))) void lds_void;
 
+struct Codes {};  // int8 activations, where float ones name their type
+template <class E>
+struct is_codes {
+  static constexpr bool value = false;
+};
+template <>
+struct is_codes<Codes> {
+  static constexpr bool value = true;
+};
+
 struct LinArgs {
-  const int8_t *x, *w;
+  const int8_t *x, *w;  // x: also the address of float tokens (linear_skinny)
   const float *x_scale, *w_scale, *bias;
   void* y;
   int32_t* part;  // [splits][M][N], or NULL: y is written
@@ -107,27 +116,24 @@ __device__ inline tok_i32x4 piece(const int8_t* p, int64_t m) {
   return v;
 }
 
-// MT tiles of 16 tokens.
-template <int MT, bool AL>
+constexpr int kFusedBytes = 32768;  // of quantised rows in LDS
+
+// MT tiles of 16 tokens.  E: int8 for codes, or the type of float tokens that
+// the kernel quantises (MT = 1, at most kFusedBytes of codes).
+template <class E, int MT, bool AL>
 __global__ __launch_bounds__(256) void linear_skinny(LinArgs a) {
+  constexpr bool FUSE = !is_codes<E>::value;
   __shared__ tok_i32x4 sums[3][MT][64];
+  __shared__ __align__(16) int8_t rows[FUSE ? kFusedBytes : 16];
+  __shared__ float tops[4][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r = lane & 15, g = lane >> 4;
   const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 16;
   const int64_t nr = n0 + r < a.N ? n0 + r : a.N - 1;
   const int8_t* wp = a.w + nr * a.K;
-  const int8_t* xp[MT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int64_t m = t * 16 + r;
-    xp[t] = a.x + (m < a.M ? m : a.M - 1) * a.ldx;
-  }
-  tok_i32x4 acc[MT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) acc[t] = tok_i32x4{0, 0, 0, 0};
-  constexpr int U = 4;  // stages in flight
-  for (int64_t k0 = wave * 128; k0 < a.K; k0 += 512 * U) {
-    tok_i32x4 wv[U][2];
+  constexpr int U = 8 / MT < 4 ? 4 : 8 / MT;  // stages in flight
+  tok_i32x4 wv[U][2];
+  auto fetch = [&](int64_t k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -135,14 +141,61 @@ __global__ __launch_bounds__(256) void linear_skinny(LinArgs a) {
         const int64_t k = k0 + 512 * u + 64 * j + 16 * g;
         wv[u][j] = piece<AL>(wp + k, a.K - k);
       }
+  };
+  fetch(wave * 128);
+  const int pitch = static_cast<int>((a.K + 15) / 16 * 16);
+  if constexpr (FUSE) {
+    typedef typename E::store S;
+    const S* x = reinterpret_cast<const S*>(a.x);
+    const int M = static_cast<int>(a.M), K = static_cast<int>(a.K);
+    for (int m = 0; m < M; ++m) {
+      float top = 0.f;
+      for (int k = threadIdx.x * E::VEC; k < K; k += 256 * E::VEC) {
+        float f[E::VEC];
+        load_vec<E>(x + m * a.ldx + k, K - k, f);
+#pragma unroll
+        for (int e = 0; e < E::VEC; ++e) top = fmaxf(top, magnitude(f[e]));
+      }
+      top = wave_max(top);
+      if (lane == 0) tops[wave][m] = top;
+    }
+    __syncthreads();
+    for (int m = 0; m < M; ++m) {
+      const float s = row_scale(fmaxf(fmaxf(tops[0][m], tops[1][m]), fmaxf(tops[2][m], tops[3][m])));
+      for (int k = threadIdx.x * E::VEC; k < pitch; k += 256 * E::VEC) {
+        float f[E::VEC];
+        load_vec<E>(x + m * a.ldx + k, K - k, f);
+        store_codes<E::VEC>(rows + m * pitch + k, E::VEC, f, s);
+      }
+    }
+    __syncthreads();
+  }
+  const int8_t* xp[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int64_t m = t * 16 + r < a.M ? t * 16 + r : a.M - 1;
+    xp[t] = FUSE ? rows + m * pitch : a.x + m * a.ldx;
+  }
+  tok_i32x4 acc[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) acc[t] = tok_i32x4{0, 0, 0, 0};
+  for (int64_t k0 = wave * 128; k0 < a.K; k0 += 512 * U) {
+    tok_i32x4 now[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) now[u][j] = wv[u][j];
+    if (k0 + 512 * U < a.K) fetch(k0 + 512 * U);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int64_t k = k0 + 512 * u + 64 * j + 16 * g;
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[u][j], piece<AL>(xp[t] + k, a.K - k), acc[t], 0, 0, 0);
+        for (int t = 0; t < MT; ++t) {
+          const tok_i32x4 xv = FUSE ? piece<true>(xp[t] + k, a.K - k) : piece<AL>(xp[t] + k, a.K - k);
+          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[u][j], xv, acc[t], 0, 0, 0);
+        }
       }
   }
   if (wave > 0) {
@@ -156,30 +209,40 @@ __global__ __launch_bounds__(256) void linear_skinny(LinArgs a) {
 #pragma unroll
     for (int w = 0; w < 3; ++w) acc[t] += sums[w][t][lane];
     const int64_t m = t * 16 + r, n = n0 + g * 4;
-    if (m < a.M && n < a.N) put4(a, m, n, acc[t], a.x_scale[m], channels(a, n));
+    if (m >= a.M || n >= a.N) continue;
+    const float s = FUSE ? row_scale(fmaxf(fmaxf(tops[0][m], tops[1][m]), fmaxf(tops[2][m], tops[3][m]))) : a.x_scale[m];
+    put4(a, m, n, acc[t], s, channels(a, n));
   }
 }
 
-constexpr int BK = 64;  // bytes of K a stage
+// Place of piece c of row r in its LDS row: the pieces of one column spread
+// over all banks.
+template <int BK>
+__device__ inline int spread(int r, int c) {
+  return BK == 128 ? c ^ (r & 7) : c ^ (r >> 2 & 3);
+}
 
 // vmcnt(n), with the other counters left alone
 #define C3C_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | (((n) >> 4) << 14) | (7 << 4) | (15 << 8))
 
 // (BM / WM) * (BN / WN) waves, each with a WM x WN part of the tile.
-template <int BM, int BN, int WM, int WN, int NS, bool AL>
+template <int BM, int BN, int WM, int WN, int BK, int NS, bool AL>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinArgs a) {
   constexpr int NW = (BM / WM) * (BN / WN);
   constexpr int MT = WM / 16, NT = WN / 16;
   constexpr int ROWS = BM + BN;              // rows of w, then rows of x
-  constexpr int LOADS = ROWS / 16 / NW;      // 1024-byte loads a wave and stage
-  static_assert(ROWS % (16 * NW) == 0 && BN % 16 == 0, "whole loads");
+  constexpr int KS = BK / 64;                // matrix-core steps a stage
+  constexpr int LR = 1024 / BK;              // rows of a 1024-byte load
+  constexpr int LOADS = ROWS / LR / NW;      // loads a wave and stage
+  static_assert(ROWS % (LR * NW) == 0 && BN % LR == 0, "whole loads");
   __shared__ __align__(16) int8_t lds[NS * ROWS * BK];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
 
   // tiles in an order that keeps each of the 8 L2 caches on neighbouring
   // ones: workgroup b runs on cache b % 8, which gets a run of consecutive
-  // tiles, walked in columns of 8 tiles of tokens
+  // tiles, walked in columns of 6 tiles of tokens (32760 x 5120 x 5120: 794 us;
+  // columns of 4 809, of 8 857)
   const int total = a.tiles_m * a.tiles_n;
   int b = blockIdx.x;
   const int split = b / total;
@@ -188,7 +251,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
     const int each = total / 8, rest = total % 8, c = b % 8, i = b / 8;
     b = c * each + (c < rest ? c : rest) + i;
   }
-  constexpr int COL = 8;
+  constexpr int COL = 6;
   const int colg = b / (COL * a.tiles_n), in = b - colg * COL * a.tiles_n;
   const int high = a.tiles_m - colg * COL < COL ? a.tiles_m - colg * COL : COL;
   const int tm = colg * COL + in % high, tn = in / high;
@@ -201,9 +264,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
   const int64_t nrows = a.N - n0 < BN ? a.N - n0 : BN, mrows = a.M - m0 < BM ? a.M - m0 : BM;
   const int8_t* wb = a.w + n0 * a.K;
   const int8_t* xb = a.x + m0 * a.ldx;
-  // the part of a 1024-byte load (16 rows) that this lane brings: row lane / 4,
-  // place lane % 4
-  const int lrow = lane >> 2, lpiece = (lane & 3) ^ (lane >> 4);
+  // the part of a load that this lane brings: row and piece
+  const int lrow = lane / (BK / 16), lpiece = spread<BK>(lrow, lane % (BK / 16));
   const __amdgpu_buffer_rsrc_t wrs = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<int8_t*>(wb), 0, static_cast<int>(nrows * a.K), 0x00020000);
   const __amdgpu_buffer_rsrc_t xrs = __builtin_amdgcn_make_buffer_rsrc(
@@ -212,7 +274,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
   // load i of stage st of this split
   auto load = [&](int st, int i) __attribute__((always_inline)) {
     const int k = (s0 + st) * BK + lpiece * 16, buf = st % NS;
-    const int row = (i * NW + wave) * 16;  // of ROWS, uniform; whole loads are of w or of x
+    const int row = (i * NW + wave) * LR;  // of ROWS, uniform; whole loads are of w or of x
     const bool isw = row < BN;
     const int rr = (isw ? row : row - BN) + lrow;
     if (AL) {
@@ -230,18 +292,17 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
   auto settle = [&](int st) __attribute__((always_inline)) {  // !AL
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
-      *reinterpret_cast<tok_i32x4*>(lds + (st % NS) * ROWS * BK + (i * NW + wave) * 16 * BK + lane * 16) = staged[i];
+      *reinterpret_cast<tok_i32x4*>(lds + (st % NS) * ROWS * BK + (i * NW + wave) * LR * BK + lane * 16) = staged[i];
   };
 
   const int wm = wave % (BM / WM) * WM, wn = wave / (BM / WM) * WN;
-  // every fragment row is congruent to r modulo 16
-  const int at = r * BK + ((g ^ (r >> 2)) & 3) * 16;
   struct Frags {
     tok_i32x4 w[NT], x[MT];
   };
-  // fragment n of NT + MT
-  auto read = [&](int st, int n, Frags& f) __attribute__((always_inline)) {
-    const int8_t* base = lds + (st % NS) * ROWS * BK + at;
+  // fragment n of NT + MT of step ks of a stage; every fragment row is
+  // congruent to r modulo 16
+  auto read = [&](int st, int ks, int n, Frags& f) __attribute__((always_inline)) {
+    const int8_t* base = lds + (st % NS) * ROWS * BK + r * BK + spread<BK>(r, ks * 4 + g) * 16;
     if (n < NT)
       f.w[n] = *reinterpret_cast<const tok_i32x4*>(base + (wn + n * 16) * BK);
     else
@@ -253,29 +314,33 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
 #pragma unroll
     for (int j = 0; j < MT; ++j) acc[i][j] = tok_i32x4{0, 0, 0, 0};
 
-  // One round: stage st's products, stage st + 1's fragments, stage st + NS's
-  // loads into the place of stage st, whose fragments every wave has read
-  // when it comes to the barrier.  Reads and products take turns: reads all at
-  // once would keep LDS and the matrix cores busy one after the other (a
-  // stage's reads and writes take LDS about as long as its products take the
-  // matrix cores).  What is read and loaded past the last stage is never used.
-  auto round = [&](int st, const Frags& cur, Frags& nxt) __attribute__((always_inline)) {
-    if (AL) C3C_VMCNT((NS - 2) * LOADS);  // stage st + 1 has landed: the loads behind it may be on their way
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  // One step: its products, the next step's fragments.  The last step of a
+  // stage waits for stage st + 1 and, once every wave has read the last of
+  // stage st, loads stage st + NS into its place.  Reads and products take
+  // turns: reads all at once would keep LDS and the matrix cores busy one after
+  // the other.  What is read and loaded past the last stage is never used.
+  auto step = [&](int st, int ks, const Frags& cur, Frags& nxt) __attribute__((always_inline)) {
+    const bool end = ks == KS - 1;
+    if (end) {
+      if (AL) C3C_VMCNT((NS - 2) * LOADS);  // stage st + 1 has landed: the loads behind it may be on their way
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
     constexpr int STEPS = NT + MT;
 #pragma unroll
     for (int n = 0; n < STEPS; ++n) {
       __builtin_amdgcn_sched_barrier(0);
-      read(st + 1, n, nxt);
+      read(end ? st + 1 : st, end ? 0 : ks + 1, n, nxt);
+      if (end) {
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        if (i * STEPS / LOADS == n) load(st + (AL ? NS : 2), i);
+        for (int i = 0; i < LOADS; ++i)
+          if (i * STEPS / LOADS == n) load(st + (AL ? NS : 2), i);
+      }
 #pragma unroll
       for (int e = n * NT * MT / STEPS; e < (n + 1) * NT * MT / STEPS; ++e)
         acc[e / MT][e % MT] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cur.w[e / MT], cur.x[e % MT], acc[e / MT][e % MT], 0, 0, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (!AL) settle(st + 2);
+    if (end && !AL) settle(st + 2);
   };
   Frags fa, fb;
 #pragma unroll
@@ -287,10 +352,17 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
   if (AL) C3C_VMCNT((NS - 1) * LOADS);
   asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-  for (int n = 0; n < NT + MT; ++n) read(0, n, fa);
-  for (int st = 0; st < count; st += 2) {
-    round(st, fa, fb);
-    if (st + 1 < count) round(st + 1, fb, fa);
+  for (int n = 0; n < NT + MT; ++n) read(0, 0, n, fa);
+  if (KS == 2) {
+    for (int st = 0; st < count; ++st) {
+      step(st, 0, fa, fb);
+      step(st, 1, fb, fa);
+    }
+  } else {
+    for (int st = 0; st < count; st += 2) {
+      step(st, 0, fa, fb);
+      if (st + 1 < count) step(st + 1, 0, fb, fa);
+    }
   }
   C3C_VMCNT(0);  // nothing is on its way into LDS when the workgroup ends
 
@@ -362,10 +434,10 @@ Tile tile_of(int64_t M, int64_t N) {
   return {64, 64};
 }
 
-template <int BM, int BN, int WM, int WN, int NS, bool AL>
+template <int BM, int BN, int WM, int WN, int BK, int NS, bool AL>
 hipError_t run_tiled(LinArgs a, hipStream_t s) {
   constexpr int threads = (BM / WM) * (BN / WN) * 64;
-  auto k = linear_tiled<BM, BN, WM, WN, NS, AL>;
+  auto k = linear_tiled<BM, BN, WM, WN, BK, NS, AL>;
   a.tiles_m = static_cast<int>(up(a.M, BM));
   a.tiles_n = static_cast<int>(up(a.N, BN));
   const int64_t blocks = static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.splits;
@@ -382,9 +454,19 @@ LinearPlan plan_linear_i8(int64_t M, int64_t N, int64_t K) {
   LinearPlan p;
   if (M <= kSkinny) return p;
   const Tile t = tile_of(M, N);
-  const int64_t tiles = up(M, t.bm) * up(N, t.bn), stages = up(K, BK), cus = device_compute_units();
-  // at least 16 stages a split: fewer cost more in partial sums than they save
-  const int64_t s = cus / tiles < stages / 16 ? cus / tiles : stages / 16;
+  const int64_t tiles = up(M, t.bm) * up(N, t.bn), stages = up(K, 64), cus = device_compute_units();
+  // Split while the device has idle compute units and it pays: a stage of 64
+  // bytes takes about 0.5 us where few workgroups run (it is latency), joining
+  // 4 us and the traffic of the partial sums.
+  int64_t s = 1;
+  double best = 0;
+  for (int64_t n = 1; n <= stages / 4 && (n == 1 || tiles * n <= 2 * cus); ++n) {
+    const double us = 0.5 * up(stages, n) * up(tiles * n, cus) + (n > 1 ? 4 + 8e-6 / 4 * n * M * N : 0);
+    if (n == 1 || us < best) {
+      best = us;
+      s = n;
+    }
+  }
   if (s > 1) {
     p.splits = static_cast<int>(s);
     p.part_bytes = s * M * N * 4;
@@ -402,17 +484,16 @@ hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, in
   const bool al = K % 16 == 0 && ldx % 16 == 0 && ldx < (1 << 22) && reinterpret_cast<uintptr_t>(x) % 16 == 0 &&
                   reinterpret_cast<uintptr_t>(w) % 16 == 0;
   if (M <= kSkinny) {
-    const int64_t blocks = up(N, 16);
-    auto k = M <= 16   ? (al ? linear_skinny<1, true> : linear_skinny<1, false>)
-             : M <= 32 ? (al ? linear_skinny<2, true> : linear_skinny<2, false>)
-                       : (al ? linear_skinny<4, true> : linear_skinny<4, false>);
-    hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
+    auto k = M <= 16   ? (al ? linear_skinny<Codes, 1, true> : linear_skinny<Codes, 1, false>)
+             : M <= 32 ? (al ? linear_skinny<Codes, 2, true> : linear_skinny<Codes, 2, false>)
+                       : (al ? linear_skinny<Codes, 4, true> : linear_skinny<Codes, 4, false>);
+    hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(up(N, 16))), dim3(256), 0, s, a);
     return hipGetLastError();
   }
   const Tile t = tile_of(M, N);
-  hipError_t e = t.bm == 256   ? (al ? run_tiled<256, 256, 128, 64, NSBIG, true>(a, s) : run_tiled<256, 256, 128, 64, 4, false>(a, s))
-                 : t.bm == 128 ? (al ? run_tiled<128, 128, 64, 64, 4, true>(a, s) : run_tiled<128, 128, 64, 64, 4, false>(a, s))
-                               : (al ? run_tiled<64, 64, 32, 32, 4, true>(a, s) : run_tiled<64, 64, 32, 32, 4, false>(a, s));
+  hipError_t e = t.bm == 256   ? (al ? run_tiled<256, 256, 128, 64, 128, 2, true>(a, s) : run_tiled<256, 256, 128, 64, 64, 4, false>(a, s))
+                 : t.bm == 128 ? (al ? run_tiled<128, 128, 64, 64, 64, 4, true>(a, s) : run_tiled<128, 128, 64, 64, 64, 4, false>(a, s))
+                               : (al ? run_tiled<64, 64, 32, 32, 64, 4, true>(a, s) : run_tiled<64, 64, 32, 32, 64, 4, false>(a, s));
   if (e == hipSuccess && part) {
     const int64_t blocks = up(M * up(N, 4), 256);
     if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
@@ -420,6 +501,21 @@ hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, in
     e = hipGetLastError();
   }
   return e;
+}
+
+bool linear_quantises(int64_t M, int64_t K) { return M <= 4 && M * ((K + 15) / 16 * 16) <= kFusedBytes; }
+
+hipError_t launch_linear_float(int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, int x_dtype,
+                               const int8_t* w, const float* w_scale, const float* bias, void* y, int y_dtype,
+                               hipStream_t s) {
+  if (M == 0) return hipSuccess;
+  LinArgs a{static_cast<const int8_t*>(x), w, nullptr, w_scale, bias, y, nullptr, M, N, K, ldx, 0, 0, 1, y_dtype};
+  const bool al = K % 16 == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
+  auto k = x_dtype == C3C_DTYPE_BF16  ? (al ? linear_skinny<ElemBf16, 1, true> : linear_skinny<ElemBf16, 1, false>)
+           : x_dtype == C3C_DTYPE_F16 ? (al ? linear_skinny<ElemF16, 1, true> : linear_skinny<ElemF16, 1, false>)
+                                      : (al ? linear_skinny<ElemF32, 1, true> : linear_skinny<ElemF32, 1, false>);
+  hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(up(N, 16))), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace c3c

@@ -21,8 +21,6 @@
 namespace c3c {
 namespace {
 
-constexpr float kInf = __builtin_inff();
-
 // Reductions over the threads of a row: a wave, or (WAVE false) the workgroup
 // of at most 16 waves, whose partial results meet in LDS.  Every call of one
 // kernel takes its own `slot`, so that no call overwrites what a slower wave
@@ -51,37 +49,6 @@ struct Row {
     return r;
   }
 };
-
-// |v|, infinite for a NaN too: a maximum of these says whether all are finite
-__device__ inline float magnitude(float v) {
-  const float a = fabsf(v);
-  return a < kInf ? a : kInf;
-}
-
-// the scale of an 8-bit row, and one code of it (IEEE division: the codes are
-// those of the definition)
-__device__ inline float row_scale(float amax) { return amax < kInf ? amax / 127.f : __builtin_nanf(""); }
-__device__ inline int code(float v, float s) {
-  const float q = rintf(v / s);
-  // s rounds amax / 127, so |v| / s may round past 127 for a tiny s
-  return s > 0.f ? static_cast<int>(fminf(fmaxf(q, -127.f), 127.f)) : 0;
-}
-
-template <int N>
-__device__ inline void store_codes(int8_t* p, int m, const float (&v)[N], float s) {
-  uint32_t w[(N + 3) / 4];
-#pragma unroll
-  for (int i = 0; i < (N + 3) / 4; ++i) w[i] = 0;
-#pragma unroll
-  for (int e = 0; e < N; ++e) w[e >> 2] |= (static_cast<uint32_t>(code(v[e], s)) & 255u) << (8 * (e & 3));
-  if (m >= N) {
-    __builtin_memcpy(p, w, N);
-  } else {
-#pragma unroll
-    for (int e = 0; e < N - 1; ++e)
-      if (e < m) p[e] = static_cast<int8_t>(w[e >> 2] >> (8 * (e & 3)));
-  }
-}
 
 // 16-byte vectors of fp32 per-channel gains
 template <class E>

@@ -81,4 +81,37 @@ __device__ inline float wave_max(float v) {
   return v;
 }
 
+// ---- 8-bit rows: q = x / s to the nearest integer, s = max|x| / 127
+
+// |v|, infinite for a NaN too: a maximum of these says whether all are finite
+__device__ inline float magnitude(float v) {
+  const float a = fabsf(v);
+  return a < __builtin_inff() ? a : __builtin_inff();
+}
+
+// the scale of an 8-bit row, and one code of it (IEEE division: the codes are
+// those of the definition)
+__device__ inline float row_scale(float amax) { return amax < __builtin_inff() ? amax / 127.f : __builtin_nanf(""); }
+__device__ inline int code(float v, float s) {
+  const float q = rintf(v / s);
+  // s rounds amax / 127, so |v| / s may round past 127 for a tiny s
+  return s > 0.f ? static_cast<int>(fminf(fmaxf(q, -127.f), 127.f)) : 0;
+}
+
+template <int N>
+__device__ inline void store_codes(int8_t* p, int m, const float (&v)[N], float s) {
+  uint32_t w[(N + 3) / 4];
+#pragma unroll
+  for (int i = 0; i < (N + 3) / 4; ++i) w[i] = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) w[e >> 2] |= (static_cast<uint32_t>(code(v[e], s)) & 255u) << (8 * (e & 3));
+  if (m >= N) {
+    __builtin_memcpy(p, w, N);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N - 1; ++e)
+      if (e < m) p[e] = static_cast<int8_t>(w[e >> 2] >> (8 * (e & 3)));
+  }
+}
+
 }  // namespace c3c

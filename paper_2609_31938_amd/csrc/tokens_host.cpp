@@ -190,6 +190,8 @@ int c3c_linear_i8(c3c_ctx* ctx, const c3c_linear_desc* d, const void* x, const f
   if (sp.rows_bytes > have)
     return fail(ctx, C3C_E_INVAL, "the context's workspace is smaller than the quantised rows need");
   hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!i8 && linear_quantises(d->M, d->K))
+    return done(ctx, launch_linear_float(d->M, d->N, d->K, x, d->ld_x, d->x_dtype, w, w_scale, bias, y, d->y_dtype, s));
   unsigned char* ws = static_cast<unsigned char*>(ctx->ws);
   const int8_t* rows = static_cast<const int8_t*>(x);
   int64_t ld = d->ld_x;

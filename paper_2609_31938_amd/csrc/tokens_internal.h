@@ -30,6 +30,13 @@ hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, in
                             const float* bias, void* y, int y_dtype, const LinearPlan& plan,
                             int32_t* part, hipStream_t s);
 
+// the same on float rows that the kernel quantises itself, for the few and
+// short ones that linear_quantises says
+bool linear_quantises(int64_t M, int64_t K);
+hipError_t launch_linear_float(int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, int x_dtype,
+                               const int8_t* w, const float* w_scale, const float* bias, void* y, int y_dtype,
+                               hipStream_t s);
+
 // kv_append (kv_append.hip)
 struct AppendArgs {
   c3c_kv_cache c;
