@@ -69,6 +69,7 @@ struct NormArgs {
   float* u_scale;
   int64_t T, C, rows;
   float alpha, eps;
+  bool stream;  // outputs are more than the caches hold
 };
 
 // NV vectors of the row in each thread's registers.
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_gate_regs(NormArgs a) 
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (lane + i * per) * V;
-      if (c < C) store_vec<E>(o + c, C - c, h[i]);
+      if (c < C) store_vec<E>(o + c, C - c, h[i], a.stream);
     }
   }
   if (!a.pre) return;
@@ -151,7 +152,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_gate_regs(NormArgs a) 
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (lane + i * per) * V;
-      if (c < C) store_vec<E>(o + c, C - c, h[i]);
+      if (c < C) store_vec<E>(o + c, C - c, h[i], a.stream);
     }
   }
   if (a.u_q) {
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(1024) void quantize_loop(QuantArgs a) {
 
 // How a row of nv vectors is spread: a wave while it holds two vectors a lane
 // at most, else a workgroup with as few vectors a thread as its 1024 threads
-// allow, two while there are rows enough to fill the device.
+// allow.
 struct Shape {
   bool wave;
   int nv;  // vectors a thread; 0: the loop
@@ -288,13 +289,13 @@ Shape shape_of(int64_t T, int64_t vecs) {
   if (vecs <= 128) return {true, vecs <= 64 ? 1 : 2, 256, static_cast<unsigned>(ceil(T, 4))};
   const unsigned blocks = static_cast<unsigned>(T);
   if (vecs > 4 * 1024) return {false, 0, 1024, blocks};
-  int nv = vecs <= 1024 ? 1 : vecs <= 2048 ? 2 : 4;
-  if (nv == 1 && T > device_compute_units()) nv = 2;
+  const int nv = vecs <= 1024 ? 1 : vecs <= 2048 ? 2 : 4;
   return {false, nv, static_cast<unsigned>(ceil(ceil(vecs, nv), 64) * 64), blocks};
 }
 
 template <class E>
-hipError_t norm_typed(const NormArgs& a, hipStream_t s) {
+hipError_t norm_typed(NormArgs a, hipStream_t s) {
+  a.stream = a.T * a.C * static_cast<int64_t>(sizeof(typename E::store)) > (32 << 20);
   const Shape p = shape_of(a.T, (a.C + E::VEC - 1) / E::VEC);
   auto k = p.nv == 0 ? norm_gate_loop<E>
            : p.wave  ? (p.nv == 1 ? norm_gate_regs<E, 1, true> : norm_gate_regs<E, 2, true>)
@@ -323,7 +324,8 @@ hipError_t launch_norm_gate(const c3c_norm_desc& d, const void* h, const void* y
                             const float* post, const float* pre, void* h_out, void* u, int8_t* u_q,
                             float* u_scale, hipStream_t s) {
   if (d.T == 0) return hipSuccess;
-  const NormArgs a{h, y, gate, post, pre, h_out, u, u_q, u_scale, d.T, d.C, gate ? d.rows_per_gate : 1, d.alpha, d.eps};
+  const NormArgs a{h, y, gate, post, pre, h_out, u, u_q, u_scale, d.T, d.C, gate ? d.rows_per_gate : 1, d.alpha, d.eps,
+                   false};
   return d.dtype == C3C_DTYPE_BF16  ? norm_typed<ElemBf16>(a, s)
          : d.dtype == C3C_DTYPE_F16 ? norm_typed<ElemF16>(a, s)
                                     : norm_typed<ElemF32>(a, s);

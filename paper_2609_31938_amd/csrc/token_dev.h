@@ -40,28 +40,49 @@ struct ElemF32 {
   __device__ static store narrow(float f) { return f; }
 };
 
+// VEC elements as they are stored
+template <class E>
+struct Raw {
+  typename E::store v[E::VEC];
+  __device__ void widen(float (&f)[E::VEC]) const {
+#pragma unroll
+    for (int e = 0; e < E::VEC; ++e) f[e] = E::widen(v[e]);
+  }
+};
+
 // VEC elements from p (any alignment of the element's size), of which the
 // first m exist; the others are 0
 template <class E>
-__device__ inline void load_vec(const typename E::store* p, int m, float (&f)[E::VEC]) {
-  typename E::store v[E::VEC];
+__device__ inline void load_raw(const typename E::store* p, int m, Raw<E>& r) {
   if (m >= E::VEC) {
-    __builtin_memcpy(v, p, 16);
-#pragma unroll
-    for (int e = 0; e < E::VEC; ++e) f[e] = E::widen(v[e]);
+    __builtin_memcpy(r.v, p, 16);
   } else {
 #pragma unroll
-    for (int e = 0; e < E::VEC; ++e) f[e] = e < m ? E::widen(p[e]) : 0.f;
+    for (int e = 0; e < E::VEC; ++e) r.v[e] = e < m ? p[e] : typename E::store(0);
   }
 }
-
 template <class E>
-__device__ inline void store_vec(typename E::store* p, int m, const float (&f)[E::VEC]) {
+__device__ inline void load_vec(const typename E::store* p, int m, float (&f)[E::VEC]) {
+  Raw<E> r;
+  load_raw<E>(p, m, r);
+  r.widen(f);
+}
+
+// stream: past the caches' memory of what was used last
+template <class E>
+__device__ inline void store_vec(typename E::store* p, int m, const float (&f)[E::VEC], bool stream = false) {
   typename E::store v[E::VEC];
 #pragma unroll
   for (int e = 0; e < E::VEC; ++e) v[e] = E::narrow(f[e]);
   if (m >= E::VEC) {
-    __builtin_memcpy(p, v, 16);
+    if (stream) {
+      typedef tok_u32x4 __attribute__((aligned(2))) any;
+      tok_u32x4 w;
+      __builtin_memcpy(&w, v, 16);
+      __builtin_nontemporal_store(w, reinterpret_cast<any*>(p));
+    } else {
+      __builtin_memcpy(p, v, 16);
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < E::VEC - 1; ++e)
