@@ -57,35 +57,28 @@ __device__ inline void load_f(const float* p, float (&f)[N]) {
   __builtin_memcpy(f, p, 4 * N);
 }
 
+// How the pairs of a rotation lie among a lane's 8 channels: all its pairs are
+// its own (NEXT), the other halves are 8 channels elsewhere (HALF), or anything.
+enum Turn { NONE, NEXT, HALF, ANY };
+
 // Rotates 8 channels from c on; src: the row (for the other half of a pair),
 // cs and sn: the angle's rows.
-template <class E>
+template <class E, Turn TURN>
 __device__ inline void rotate(const typename E::store* src, const float* cs, const float* sn, int c, int rot, int pairs,
                               float (&x)[8]) {
   const int half = rot >> 1;
   if (c >= rot) return;
-  if (pairs) {
+  if (TURN == NEXT) {
     float co[4], si[4];
-    if (c + 8 <= rot) {
-      load_f(cs + (c >> 1), co);
-      load_f(sn + (c >> 1), si);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = c + 2 * e < rot ? (c >> 1) + e : 0;
-        co[e] = cs[i];
-        si[e] = sn[i];
-      }
-    }
+    load_f(cs + (c >> 1), co);
+    load_f(sn + (c >> 1), si);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float u = x[2 * e], v = x[2 * e + 1];
-      if (c + 2 * e < rot) {
-        x[2 * e] = u * co[e] - v * si[e];
-        x[2 * e + 1] = v * co[e] + u * si[e];
-      }
+      x[2 * e] = u * co[e] - v * si[e];
+      x[2 * e + 1] = v * co[e] + u * si[e];
     }
-  } else if ((half & 7) == 0) {  // all 8 in the same half
+  } else if (TURN == HALF) {
     const bool low = c < half;
     const int j = low ? c : c - half;
     float o[8], co[8], si[8];
@@ -102,10 +95,11 @@ __device__ inline void rotate(const typename E::store* src, const float* cs, con
     for (int e = 0; e < 8; ++e) {
       const int ch = c + e;
       if (ch < rot) {
-        const bool low = ch < half;
-        const int j = low ? ch : ch - half;
-        const float a = x[e] * cs[j], b = E::widen(src[low ? ch + half : j]) * sn[j];
-        x[e] = low ? a - b : a + b;
+        // the first of a pair is turned with its second, the second with the first
+        const bool first = pairs ? (ch & 1) == 0 : ch < half;
+        const int j = pairs ? ch >> 1 : first ? ch : ch - half, other = pairs ? ch ^ 1 : first ? ch + half : j;
+        const float a = x[e] * cs[j], b = E::widen(src[other]) * sn[j];
+        x[e] = first ? a - b : a + b;
       }
     }
   }
@@ -137,8 +131,8 @@ __device__ inline uint32_t shrunk(uint32_t w, float less) {
   return codes2(a[0] * less, a[1] * less) | codes2(b[0] * less, b[1] * less) << 16;
 }
 
-template <class E, int NP>  // NP: 1, or 2 beyond 128 channels
-__global__ __launch_bounds__(256) void kv_append_k(AppendArgs a) {
+template <class E, int NP, Turn TURN>  // NP: 1, or 2 beyond 128 channels
+__global__ __launch_bounds__(256, NP == 1 && TURN != ANY ? 4 : 2) void kv_append_k(AppendArgs a) {
   typedef typename E::store S;
   const int lane = threadIdx.x & 63, g = lane >> 4, c0 = (lane & 15) * 8;
   const int64_t b = blockIdx.z;
@@ -162,7 +156,7 @@ __global__ __launch_bounds__(256) void kv_append_k(AppendArgs a) {
 
   const S* src = static_cast<const S*>(what == 0 ? a.k : what == 1 ? a.v : a.q) + static_cast<int64_t>(head) * D;
   const int64_t ld = what == 0 ? a.ld_k : what == 1 ? a.ld_v : a.ld_q;
-  const int rot = (what != 1 && a.r.cos) ? static_cast<int>(a.r.rot) : 0;
+  const int rot = (what != 1 && TURN != NONE) ? static_cast<int>(a.r.rot) : 0;
   const int nb = static_cast<int>(a.c.page) >> 4;
 
   for (int64_t blk = first + blockIdx.x; blk <= last; blk += gridDim.x) {
@@ -207,10 +201,11 @@ __global__ __launch_bounds__(256) void kv_append_k(AppendArgs a) {
             if (c0 + 128 * i < D) was[i][e] = *reinterpret_cast<const tok_u32x4*>(codes + (c0 + 128 * i + 2 * g + e) * 16);
       }
     }
-    if (rot) {
+    if (TURN != NONE && rot) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        __builtin_amdgcn_sched_barrier(0);  // one token's angles at a time: registers for more waves
+        // two tokens' angles at a time: registers for four waves a SIMD
+        if (t & 1) __builtin_amdgcn_sched_barrier(0);
         const int place = 4 * g + t;
         if (place < lo || place >= hi) continue;
         const int64_t row = a.r.pos ? a.r.pos[r0 + place] : p0 + place;
@@ -219,7 +214,7 @@ __global__ __launch_bounds__(256) void kv_append_k(AppendArgs a) {
         const float* sn = a.r.sin + (ok ? row : 0) * (rot >> 1);
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-          if (c0 + 128 * i < D) rotate<E>(src + (r0 + place) * ld, cs, sn, c0 + 128 * i, rot, a.r.pairs, x[t][i]);
+          if (c0 + 128 * i < D) rotate<E, TURN>(src + (r0 + place) * ld, cs, sn, c0 + 128 * i, rot, a.r.pairs, x[t][i]);
           if (!ok) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[t][i][e] = __builtin_nanf("");
@@ -323,11 +318,18 @@ __global__ __launch_bounds__(256) void kv_append_k(AppendArgs a) {
   }
 }
 
-template <class E>
+template <class E, int NP>
 hipError_t typed(const AppendArgs& a, dim3 grid, hipStream_t s) {
-  auto k = a.c.dim <= 128 ? kv_append_k<E, 1> : kv_append_k<E, 2>;
+  auto k = !a.r.cos                                ? kv_append_k<E, NP, NONE>
+           : a.r.pairs && a.r.rot % 8 == 0         ? kv_append_k<E, NP, NEXT>
+           : !a.r.pairs && a.r.rot % 16 == 0       ? kv_append_k<E, NP, HALF>
+                                                   : kv_append_k<E, NP, ANY>;
   hipLaunchKernelGGL(k, grid, dim3(256), 0, s, a);
   return hipGetLastError();
+}
+template <class E>
+hipError_t typed(const AppendArgs& a, dim3 grid, hipStream_t s) {
+  return a.c.dim <= 128 ? typed<E, 1>(a, grid, s) : typed<E, 2>(a, grid, s);
 }
 
 }  // namespace
