@@ -506,7 +506,10 @@ typedef __attribute__((address_space(1))) const void global_void;
 // them to f16 for all.  Two tiles in turn.  What bounds it is the vector
 // units: conversions and exponentials beside the products; that is why V is
 // converted once (K too would make LDS reads the bound).
-template <class E, int DP, int CT>
+// WHOLE: pages are multiples of 64 tokens, so that a tile lies in one page and
+// its addresses are scalars; what the vector units spend on finding blocks of
+// 16 tokens otherwise is a quarter of their work.
+template <class E, int DP, int CT, bool WHOLE>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   typedef Form<E> F;
   typedef typename E::store S;
@@ -563,32 +566,55 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   // Tiles on their way: block g of the tile of this lane, its scales, K in
   // LDS, this wave's part of V in registers.
   const int32_t* pages = a.table + static_cast<int64_t>(b) * a.cols;
-  auto page_of = [&](int tile) { return peek(a, pages, tile * 4 + g, ue); };
-  auto block = [&](int tile, uint32_t page) { return settle(a, hk, tile * 4 + g, page); };
+  auto page_of = [&](int tile) { return peek(a, pages, tile * 4 + (WHOLE ? 0 : g), ue); };  // used a round later
+  // the block of this lane; WHOLE: the first of the tile, a scalar
+  auto block = [&](int tile, uint32_t page) __attribute__((always_inline)) {
+    if constexpr (WHOLE)
+      return settle(a, hk, tile * 4, __builtin_amdgcn_readfirstlane(page));
+    else
+      return settle(a, hk, tile * 4 + g, page);
+  };
+  auto mine_of = [&](uint32_t vb) { return WHOLE && vb != kNone ? vb + g : vb; };
   tok_u32x4 vr[VW];
   typedef __attribute__((address_space(1))) const uint8_t global_u8;
   global_u8* zeros = (global_u8*)kZeros;
+  const int klane = ((r >> 2) * 16 + (r & 3)) * D + g * 16, vlane = (g * D + r) * 16;
   auto fetch_k = [&](uint32_t vb, int buf) __attribute__((always_inline)) {
-    const uint32_t kb = __shfl(vb, (r >> 2) * 16);
-    global_u8* kp = (global_u8*)a.k + (static_cast<int64_t>(kb) * 16 + (r & 3)) * D + g * 16;
+    global_u8* kp;
+    if constexpr (WHOLE) {
+      if (vb == kNone) return;  // whatever is there is hidden
+      kp = (global_u8*)a.k + static_cast<int64_t>(vb) * 16 * D + klane;
+    } else {
+      vb = __shfl(vb, (r >> 2) * 16);
+      kp = (global_u8*)a.k + (static_cast<int64_t>(vb) * 16 + (r & 3)) * D + g * 16;
+    }
 #pragma unroll
     for (int n = 0; n < NJ; ++n) {
       const int f = n * 4 + wave, t = f / NJ, j = f - t * NJ;
-      const bool ok = kb != kNone && j * 64 + g * 16 < D;
-      __builtin_amdgcn_global_load_lds((global_void*)(ok ? kp + 4 * t * D + j * 64 : zeros), (lds_void*)(&kbuf[buf][f * 1024]),
-                                       16, 0, 0);
+      global_u8* p = kp + 4 * t * D + j * 64;
+      if (WHOLE ? (D & 63) != 0 && j * 64 + g * 16 >= D : vb == kNone || j * 64 + g * 16 >= D) p = zeros;
+      __builtin_amdgcn_global_load_lds((global_void*)p, (lds_void*)(&kbuf[buf][f * 1024]), 16, 0, 0);
     }
   };
   auto fetch_v = [&](uint32_t vb) __attribute__((always_inline)) {
-    global_u8* vp = (global_u8*)a.v + (static_cast<int64_t>(vb) * D + r) * 16;
+    if (WHOLE && vb == kNone) {
+#pragma unroll
+      for (int n = 0; n < VW; ++n) vr[n] = tok_u32x4{0, 0, 0, 0};
+      return;
+    }
+    global_u8* vp = WHOLE ? (global_u8*)a.v + static_cast<int64_t>(vb) * 16 * D + vlane
+                          : (global_u8*)a.v + (static_cast<int64_t>(vb) * D + r) * 16;
 #pragma unroll
     for (int n = 0; n < VW; ++n) {
       const int d = n * 4 + wave;
-      vr[n] = *(__attribute__((address_space(1))) const tok_u32x4*)(vb != kNone && d * 16 < D ? vp + d * 256 : zeros);
+      global_u8* p = vp + d * 256;
+      if (WHOLE ? d * 16 >= D : vb == kNone || d * 16 >= D) p = zeros;
+      vr[n] = *(__attribute__((address_space(1))) const tok_u32x4*)p;
     }
   };
   // a tile that some column of the workgroup does not see whole
-  auto partial = [&](int tok0, uint32_t vb) { return tok0 < hi.begin || tok0 + 64 > lo.end || __ballot(vb == kNone) != 0; };
+  auto lost = [&](uint32_t vb) { return WHOLE ? vb == kNone : __ballot(vb == kNone) != 0; };
+  auto partial = [&](int tok0, uint32_t vb) { return tok0 < hi.begin || tok0 + 64 > lo.end || lost(vb); };
   int unit = -126, grown = -126, rest = 0;  // E, E after the next tile, what of its exponents goes to P
   auto convert = [&](int tile, uint32_t vb, float vs, int buf) __attribute__((always_inline)) {
     const int ve = exponent_of(vs);
@@ -621,6 +647,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
             codes_f16(vr[n][2 * u], vr[n][2 * u + 1], vk);
   };
   auto scales = [&](uint32_t vb, float& k, float& v) {
+    vb = mine_of(vb);
     k = vb != kNone ? a.ks[vb] : 1.f;
     v = vb != kNone ? a.vs[vb] : 0x1p-126f;
   };
@@ -681,7 +708,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     const float cg = fmaxf(a.c * ks, 0x1p-126f), shrink = pow2(unit - grown);
     const int f = rest;
     unit = grown;
-    if (tok0 < whi.begin || tok0 + 64 > wlo.end || __ballot(cur == kNone) != 0) {
+    if (tok0 < whi.begin || tok0 + 64 > wlo.end || lost(cur)) {
 #pragma unroll
       for (int x = 0; x < CT; ++x) hide(s[x], tok0 + 16 * g, mine[x], cur != kNone);
     }
@@ -707,7 +734,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     __builtin_amdgcn_sched_barrier(0);
     if (partial(tok0, cur) && (nan_seen[buf][0] | nan_seen[buf][1] | nan_seen[buf][2] | nan_seen[buf][3])) {
 #pragma unroll
-      for (int x = 0; x < CT; ++x) put_nan<DT>(a, cur, tok0, g, mine[x], acc[x]);
+      for (int x = 0; x < CT; ++x) put_nan<DT>(a, mine_of(cur), tok0, g, mine[x], acc[x]);
     }
     if (tile + 1 < t1) convert(tile + 1, nxt, vs1, buf ^ 1);
     cur = nxt;
@@ -819,6 +846,14 @@ int64_t workgroup_columns(int64_t dim, int dtype) {
 // Calls of at most 16 columns a sequence and head take attend_few.
 bool few(int64_t columns) { return columns <= 16; }
 
+template <class E, int NQ, bool WHOLE>
+auto pick_many(int dim) {
+  return dim <= 64    ? attend_many<E, 64, column_tiles(64, NQ), WHOLE>
+         : dim <= 128 ? attend_many<E, 128, column_tiles(128, NQ), WHOLE>
+         : dim <= 192 ? attend_many<E, 192, column_tiles(192, NQ), WHOLE>
+                      : attend_many<E, 256, column_tiles(256, NQ), WHOLE>;
+}
+
 template <class E>
 hipError_t run(const AttendArgs& h, const AttendPlan& p, int dtype, hipStream_t s) {
   const int64_t G = h.q_heads / h.c.heads, columns = h.b.max_new * G, nb = h.c.page / 16;
@@ -842,10 +877,7 @@ hipError_t run(const AttendArgs& h, const AttendPlan& p, int dtype, hipStream_t 
     hipLaunchKernelGGL(k, dim3(p.splits, a.heads, static_cast<unsigned>(h.b.B)), dim3(256), 0, s, a);
   } else {
     constexpr int NQ = Form<E>::NQ;
-    auto k = a.D <= 64    ? attend_many<E, 64, column_tiles(64, NQ)>
-             : a.D <= 128 ? attend_many<E, 128, column_tiles(128, NQ)>
-             : a.D <= 192 ? attend_many<E, 192, column_tiles(192, NQ)>
-                          : attend_many<E, 256, column_tiles(256, NQ)>;
+    auto k = nb % 4 == 0 ? pick_many<E, NQ, true>(a.D) : pick_many<E, NQ, false>(a.D);
     hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
   }
   hipError_t e = hipGetLastError();
