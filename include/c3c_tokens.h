@@ -170,8 +170,8 @@ typedef struct c3c_rope {
  * infinities are stored as NaN and leave the scale alone.
  * Blocks that are written must belong to one sequence only.
  * EINVAL: NULL ctx, cache, batch or required tensor; sizes out of range;
- * unknown dtype; heads or q_heads < 1, ld too small; misaligned codes;
- * outputs overlapping inputs or one another. */
+ * unknown dtype; heads or q_heads < 1; heads, q_heads or B > 65535; ld too
+ * small; misaligned codes; outputs overlapping inputs or one another. */
 int c3c_kv_append(c3c_ctx* ctx, const c3c_kv_cache* cache, const c3c_kv_batch* batch,
                   const c3c_rope* rope, int dtype, int64_t q_heads, const void* q, int64_t ld_q,
                   const void* k, int64_t ld_k, const void* v, int64_t ld_v, void* q_out,

@@ -27,7 +27,15 @@ inline bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes
   return a0 < b0 + static_cast<uintptr_t>(bbytes) && b0 < a0 + static_cast<uintptr_t>(abytes);
 }
 
-// sets the context's message and returns the status
+// sets the context's message and returns the status (the message is lost, and
+// nothing is thrown, where there is no memory for it)
+inline int fail(c3c_ctx* ctx, int status, const char* msg) noexcept {
+  try {
+    if (ctx) ctx->last_error = msg;
+  } catch (...) {
+  }
+  return status;
+}
 inline int fail(c3c_ctx* ctx, int status, const std::string& msg) {
   if (ctx) ctx->last_error = msg;
   return status;

@@ -13,6 +13,11 @@
 //
 // A row belongs to one wave (at most 128 16-byte vectors: no barrier) or to
 // one workgroup; rows beyond 4096 vectors are read again in every pass.
+// 32760 x 5120 in bf16 with post, gate and pre: 353 us, 3.8 TB/s.  The gains
+// come from L2 for every row and are more bytes than the row: with constants in
+// their place 263 us.  Slower: two rows a workgroup (363), gains kept over the
+// rows of workgroups that stay (441 to 491, fewer rows in flight), a row a wave
+// (796), two vectors a thread (358).
 #include <math.h>
 
 #include "token_dev.h"

@@ -105,6 +105,8 @@ const char* check_cache(const c3c_kv_cache* c, const c3c_kv_batch* b, int dtype,
   if (!c || !b) return "cache or batch is NULL";
   if (!elem_bytes(dtype)) return "unknown dtype";
   if (c->pages < 0 || c->pages >= kBig || c->heads < 1 || c->heads >= kBig) return "pages must be >= 0, heads >= 1";
+  // grids have 65535 places for heads and for sequences
+  if (c->heads > 65535 || q_heads > 65535 || b->B > 65535) return "heads, q_heads and B must be at most 65535";
   if (c->page < 16 || c->page % 16 || c->page >= kBig) return "page must be a multiple of 16";
   if (c->dim < 16 || c->dim > 256 || c->dim % 16) return "dim must be a multiple of 16, at most 256";
   if (b->B < 0 || b->B >= kBig || b->T < 0 || b->T >= kBig || b->cols < 0 || b->cols >= kBig)

@@ -273,6 +273,8 @@ def kv_append(ctx, cache: KVCache, batch: Batch, k, v, *, q=None, cos=None, sin=
     tokens may be strided.  Returns the rotated queries (None without q);
     ``q_out`` may be q itself where that is contiguous."""
     dtype = _float_dtype(k, "k")
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin go together")
     T, dt = k.shape[0], k.dtype
     pk, ldk = _heads(k, "k", dt, T, cache.heads, cache.dim)
     pv, ldv = _heads(v, "v", dt, T, cache.heads, cache.dim)

@@ -192,3 +192,20 @@ def test_binding_checks():
         tokens.norm_gate(c3c.Context(), x.double())
     with pytest.raises(ValueError, match="device tensor"):
         tokens.norm_gate(c3c.Context(), x, pre=torch.ones(16))
+
+
+@no_gpu
+def test_grid_limits_are_refused():
+    ctx = c3c.Context()
+    for c, b, qh in ((cache(), batch(B=65536, cols=1, T=65536, max_new=1), 4), (cache(heads=65536, dim=16), batch(), 65536),
+                     (cache(heads=2, dim=16), batch(), 65536)):
+        st = lib.c3c_paged_attention(ctx._h, C.byref(c), C.byref(b), 1, qh, at(0), 1 << 22, 0.1, 1, 0, at(3), None, None)
+        refused(st, ctx, "65535")
+
+
+def test_angles_come_in_pairs():
+    c = tokens.KVCache.__new__(tokens.KVCache)
+    c.heads, c.dim = 1, 16
+    with pytest.raises(ValueError, match="go together"):
+        x = torch.zeros(1, 1, 16)
+        tokens.kv_append(c3c.Context(), c, None, x, x, cos=torch.zeros(1, 8))
