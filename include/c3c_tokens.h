@@ -64,11 +64,12 @@ int c3c_quantize_rows(c3c_ctx* ctx, int64_t T, int64_t C, int64_t ld_x, int dtyp
  * in int32, hence K <= 131071.
  *
  * Workspace (c3c_linear_i8_workspace_bytes, 0 where none is used): the
- * quantised rows of float activations, and the partial sums of a product that
- * is split along K because its tiles are too few for the device.  A call
- * whose context has less than the bytes that it needs for the rows is EINVAL;
- * with the rows but not the partial sums it runs unsplit.  Results are the
- * same bits either way (integer sums).
+ * quantised rows of float activations, copies of rows that are no multiple of
+ * 16 bytes, and the partial sums of a product that is split along K because
+ * its tiles are too few for the device.  A call whose context has less than
+ * the bytes that it needs for the quantised rows is EINVAL; with those but not
+ * the others it runs without copies or unsplit.  Results are the same bits
+ * either way (integer sums).
  * EINVAL: NULL ctx, desc or a NULL tensor of nonzero size; M < 0, N < 1,
  * K < 1 or > 131071, ld_x < K; unknown dtypes; x_scale given with a float x
  * or missing with int8; y overlapping an input; the workspace overlapping a

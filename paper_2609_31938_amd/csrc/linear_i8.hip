@@ -5,7 +5,7 @@
 // tokens B (columns m), so that a lane's four results are four consecutive n
 // of one token and are stored together.
 //
-// skinny: at most 64 tokens.  The weights are read once, straight into
+// skinny: at most 32 tokens.  The weights are read once, straight into
 //   registers (no tile of them is used twice), by 4 waves that share 16 rows
 //   and take every fourth 128-byte piece of K, 8 of them in flight; their sums
 //   meet in LDS.  Up to 4 tokens of floats are quantised in the same kernel, by
@@ -18,7 +18,9 @@
 //   the products alone 620 (at the clock that power leaves them; 3.5 PFLOP/s
 //   with random operands in registers).  With 16-byte rows the stages are loaded
 //   straight into LDS (the buffer's bounds make rows past M or N and pieces
-//   past K zero); rows of any other length go through registers.
+//   past K zero); rows of any other length are copied to such rows first where
+//   there is workspace for them (linear_pads), else they go through registers
+//   (4096 x 4095, 8192 tokens: 298 us).
 #include "token_dev.h"
 #include "tokens_internal.h"
 
@@ -420,6 +422,15 @@ __global__ __launch_bounds__(256) void linear_join(LinArgs a) {
   put4(a, m, n, v, a.x_scale[m], channels(a, n));
 }
 
+// Rows of n bytes, ld apart, to rows of ldd (a multiple of 16), zero past n: 16
+// bytes a thread.
+__global__ __launch_bounds__(256) void pad_rows(const int8_t* src, int64_t rows, int64_t n, int64_t ld, int8_t* dst, int64_t ldd) {
+  const int64_t per = ldd / 16, i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (i >= rows * per) return;
+  const int64_t r = i / per, c = i % per * 16;
+  *reinterpret_cast<tok_i32x4*>(dst + r * ldd + c) = piece<false>(src + r * ld + c, n - c);
+}
+
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // The tile of a call: the largest whose tiles fill the device, for it moves
@@ -446,7 +457,9 @@ hipError_t run_tiled(LinArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 
-constexpr int64_t kSkinny = 64;  // tokens
+// tokens of the skinny kernel (4096 x 4096: 32 tokens 13.4 us, 65 in tiles 12.2;
+// 48 tokens took 18.7 in it)
+constexpr int64_t kSkinny = 32;
 
 }  // namespace
 
@@ -485,8 +498,7 @@ hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, in
                   reinterpret_cast<uintptr_t>(w) % 16 == 0;
   if (M <= kSkinny) {
     auto k = M <= 16   ? (al ? linear_skinny<Codes, 1, true> : linear_skinny<Codes, 1, false>)
-             : M <= 32 ? (al ? linear_skinny<Codes, 2, true> : linear_skinny<Codes, 2, false>)
-                       : (al ? linear_skinny<Codes, 4, true> : linear_skinny<Codes, 4, false>);
+                       : (al ? linear_skinny<Codes, 2, true> : linear_skinny<Codes, 2, false>);
     hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(up(N, 16))), dim3(256), 0, s, a);
     return hipGetLastError();
   }
@@ -501,6 +513,17 @@ hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, in
     e = hipGetLastError();
   }
   return e;
+}
+
+// The copy costs its traffic and a launch, and about halves the products: it
+// pays from some hundred tokens on.
+bool linear_pads(int64_t M, int64_t K, int64_t ld) { return M > 64 && (K % 16 != 0 || ld % 16 != 0); }
+
+hipError_t launch_pad_rows(const int8_t* src, int64_t rows, int64_t n, int64_t ld, int8_t* dst, int64_t ldd, hipStream_t s) {
+  const int64_t blocks = up(rows * (ldd / 16), 256);
+  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL(pad_rows, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, src, rows, n, ld, dst, ldd);
+  return hipGetLastError();
 }
 
 bool linear_quantises(int64_t M, int64_t K) { return M <= 4 && M * ((K + 15) / 16 * 16) <= kFusedBytes; }

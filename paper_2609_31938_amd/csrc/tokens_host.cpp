@@ -81,21 +81,28 @@ const char* check_linear(const c3c_linear_desc* d) {
   return nullptr;
 }
 
-// Workspace of a call: the quantised rows (each padded to 16 bytes), their
-// scales, the partial sums.
+// Workspace of a call: the quantised rows (each padded to 16 bytes) and their
+// scales, which it cannot do without; copies of w and of int8 x in rows of whole
+// 16 bytes; the partial sums.
 struct LinearSpace {
-  int64_t ldq = 0, scale_at = 0, part_at = 0, rows_bytes = 0;
+  int64_t ldq = 0, scale_at = 0, rows_bytes = 0;  // of float x
+  int64_t w_at = 0, x_at = 0, pads_end = 0;       // w_at == x_at: no copy of w; x_at == pads_end: none of x
+  int64_t part_at = 0;
   LinearPlan plan;
 };
 LinearSpace linear_space(const c3c_linear_desc& d) {
   LinearSpace s;
   s.plan = plan_linear_i8(d.M, d.N, d.K);
-  if (d.x_dtype != C3C_DTYPE_I8 && d.M > 0) {
-    s.ldq = round_up(d.K, 16);
+  const bool i8 = d.x_dtype == C3C_DTYPE_I8;
+  s.ldq = round_up(d.K, 16);
+  if (!i8 && d.M > 0) {
     s.scale_at = round_up(d.M * s.ldq, 256);
     s.rows_bytes = s.scale_at + round_up(d.M * 4, 256);
   }
-  s.part_at = s.rows_bytes;
+  s.w_at = s.rows_bytes;
+  s.x_at = s.w_at + (linear_pads(d.M, d.K, d.K) ? round_up(d.N * s.ldq, 256) : 0);
+  s.pads_end = s.x_at + (i8 && linear_pads(d.M, d.K, d.ld_x) ? round_up(d.M * s.ldq, 256) : 0);
+  s.part_at = s.pads_end;
   return s;
 }
 
@@ -206,10 +213,29 @@ int c3c_linear_i8(c3c_ctx* ctx, const c3c_linear_desc* d, const void* x, const f
     x_scale = scale;
     ld = sp.ldq;
   }
+  const int8_t* weights = w;
+  int64_t K = d->K;
+  if (sp.pads_end > sp.w_at && sp.pads_end <= have) {
+    // both operands in rows of whole 16 bytes, zero past K
+    hipError_t e = hipSuccess;
+    if (sp.x_at > sp.w_at) {
+      int8_t* to = reinterpret_cast<int8_t*>(ws + sp.w_at);
+      e = launch_pad_rows(w, d->N, d->K, d->K, to, sp.ldq, s);
+      weights = to;
+      K = sp.ldq;
+    }
+    if (e == hipSuccess && sp.pads_end > sp.x_at) {
+      int8_t* to = reinterpret_cast<int8_t*>(ws + sp.x_at);
+      e = launch_pad_rows(rows, d->M, d->K, ld, to, sp.ldq, s);
+      rows = to;
+      ld = sp.ldq;
+    }
+    if (e != hipSuccess) return done(ctx, e);
+  }
   int32_t* part = sp.plan.splits > 1 && sp.part_at + sp.plan.part_bytes <= have
                       ? reinterpret_cast<int32_t*>(ws + sp.part_at)
                       : nullptr;
-  return done(ctx, launch_linear_i8(d->M, d->N, d->K, rows, ld, x_scale, w, w_scale, bias, y, d->y_dtype,
+  return done(ctx, launch_linear_i8(d->M, d->N, K, rows, ld, x_scale, weights, w_scale, bias, y, d->y_dtype,
                                     sp.plan, part, s));
 }
 

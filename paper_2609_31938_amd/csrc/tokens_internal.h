@@ -30,6 +30,9 @@ hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, in
                             const float* bias, void* y, int y_dtype, const LinearPlan& plan,
                             int32_t* part, hipStream_t s);
 
+// whether a call copies rows of K bytes, ld apart, to rows of whole 16 bytes
+bool linear_pads(int64_t M, int64_t K, int64_t ld);
+hipError_t launch_pad_rows(const int8_t* src, int64_t rows, int64_t n, int64_t ld, int8_t* dst, int64_t ldd, hipStream_t s);
 // the same on float rows that the kernel quantises itself, for the few and
 // short ones that linear_quantises says
 bool linear_quantises(int64_t M, int64_t K);

@@ -131,11 +131,12 @@ def quantize_rows(ctx, x, q=None, scale=None, stream=None):
     return q, scale
 
 
-def linear_i8_workspace_bytes(M: int, N: int, K: int, x_dtype: str = "bf16", y_dtype: str = "bf16") -> int:
+def linear_i8_workspace_bytes(M: int, N: int, K: int, x_dtype: str = "bf16", y_dtype: str = "bf16", ld_x=None) -> int:
     """Workspace bytes of a linear_i8 call: the quantised rows of float
-    activations and the partial sums of a call that splits K."""
+    activations, copies of rows that are no multiple of 16 bytes and the
+    partial sums of a call that splits K.  ``ld_x``: x's row stride (default K)."""
     n = C.c_size_t()
-    d = LinearDesc(M, N, K, K, DTYPES[x_dtype], DTYPES[y_dtype])
+    d = LinearDesc(M, N, K, K if ld_x is None else ld_x, DTYPES[x_dtype], DTYPES[y_dtype])
     _raise(lib.c3c_linear_i8_workspace_bytes(C.byref(d), C.byref(n)), what="c3c_linear_i8_workspace_bytes")
     return n.value
 

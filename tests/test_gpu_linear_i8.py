@@ -128,3 +128,19 @@ def test_large_offsets():
     rows = [M - 300, M - 1]
     check(y[rows], x[rows].cpu().numpy(), np.ones(2, np.float32), w, ws, None, "bf16")
     assert (y[0] == 0).all()
+
+
+@pytest.mark.parametrize("M,N,K,ld", [(65, 40, 33, 33), (70, 130, 1111, 1111), (300, 257, 95, 96), (300, 257, 96, 99), (2100, 2050, 77, 80)])
+def test_rows_copied_to_whole_pieces_give_the_same_bits(M, N, K, ld):
+    """With the workspace for them odd rows of w and x are copied first."""
+    g = torch.Generator().manual_seed(2)
+    x = torch.randint(-128, 128, (M, ld), generator=g, dtype=torch.int8).cuda()[:, :K]
+    s = 0.01 + torch.rand(M, generator=g).cuda()
+    w, ws, bias = weights(N, K)
+    n = tokens.linear_i8_workspace_bytes(M, N, K, "i8", "f32", ld_x=ld)
+    assert n > 0
+    ctx = c3c.Context()
+    ctx.set_workspace(torch.full((n,), 0x55, dtype=torch.uint8, device="cuda"))
+    got = tokens.linear_i8(ctx, x, w, ws, bias, x_scale=s, out_dtype="f32")
+    check(got, x.cpu().numpy(), s.cpu().numpy(), w, ws, bias, "f32")
+    assert torch.equal(got, tokens.linear_i8(c3c.Context(), x, w, ws, bias, x_scale=s, out_dtype="f32"))
