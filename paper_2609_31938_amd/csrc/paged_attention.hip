@@ -661,21 +661,25 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   tok_f32x4 s[CT][4];
   auto first = [&](int buf, tok_f32x4 (&s)[CT][4]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int x = 0; x < CT; ++x) s[x][t] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+    // the four row tiles in turn: a product waits for none of its neighbours
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const tok_u32x4 kv = *reinterpret_cast<const tok_u32x4*>(&kbuf[buf][(t * NJ + j) * 1024 + lane * 16]);
+    for (int j = 0; j < NJ; ++j) {
+      tok_u32x4 kv[4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const tok_u32x4 kf = F::k(kv[2 * h], kv[2 * h + 1]);
+      for (int t = 0; t < 4; ++t) kv[t] = *reinterpret_cast<const tok_u32x4*>(&kbuf[buf][(t * NJ + j) * 1024 + lane * 16]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const tok_u32x4 kf = F::k(kv[t][2 * h], kv[t][2 * h + 1]);
 #pragma unroll
           for (int x = 0; x < CT; ++x)
 #pragma unroll
             for (int n = 0; n < NQ; ++n) s[x][t] = F::mfma(kf, qf[x][2 * j + h][n], s[x][t]);
         }
-      }
     }
   };
 
