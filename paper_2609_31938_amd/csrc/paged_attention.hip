@@ -724,12 +724,52 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     }
 #pragma unroll
     for (int x = 0; x < CT; ++x) rescale<DT>(s[x], cg, shrink, m[x], l[x], acc[x]);
-    __builtin_amdgcn_sched_barrier(0);
+    // Tile t + 1's first product (past the last tile: of stale codes, and never
+    // used) and this tile's probabilities, one group of products and its share
+    // of exponentials at a time: left to itself the compiler puts all of one
+    // before the other.
     tok_f32x4 s1[CT][4];
-    first(buf ^ 1, s1);  // past the last tile: of stale codes, and never used
     tok_u32x4 pf[CT][2][NP];
+    {
+      float lift[CT], sum[CT], p[CT][8];
+      tok_u32x4 kv[2][4];
+      auto read_k = [&](int j) __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < CT; ++x) weigh<NP>(s[x], cg, f, m[x], l[x], pf[x]);
+        for (int t = 0; t < 4; ++t)
+          kv[j & 1][t] = *reinterpret_cast<const tok_u32x4*>(&kbuf[buf ^ 1][(t * NJ + j) * 1024 + lane * 16]);
+      };
+      read_k(0);
+#pragma unroll
+      for (int x = 0; x < CT; ++x) {
+        lift[x] = kLift + f - (m[x] == -kInf ? 0.f : m[x]);
+        sum[x] = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s1[x][t] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      constexpr int GROUPS = 8 * NJ;
+#pragma unroll
+      for (int n = 0; n < GROUPS; ++n) {
+        const int j = n / 8, h = n / 4 % 2, t = n % 4;
+        __builtin_amdgcn_sched_barrier(0);
+        if (n % 8 == 0 && j + 1 < NJ) read_k(j + 1);
+        const tok_u32x4 kf = F::k(kv[j & 1][t][2 * h], kv[j & 1][t][2 * h + 1]);
+#pragma unroll
+        for (int x = 0; x < CT; ++x)
+#pragma unroll
+          for (int q = 0; q < NQ; ++q) s1[x][t] = F::mfma(kf, qf[x][2 * j + h][q], s1[x][t]);
+#pragma unroll
+        for (int e = n * 16 / GROUPS; e < (n + 1) * 16 / GROUPS; ++e)
+#pragma unroll
+          for (int x = 0; x < CT; ++x) {
+            p[x][e & 7] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e >> 2][e & 3], cg, lift[x]));
+            sum[x] += p[x][e & 7];
+            if ((e & 7) == 7) to_terms<tok_f16x2, NP>(p[x], pf[x][e >> 3]);
+          }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int x = 0; x < CT; ++x) l[x] = __builtin_fmaf(sum[x], pow2(-f), l[x]);
+    }
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
 #pragma unroll
