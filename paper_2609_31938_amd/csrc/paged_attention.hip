@@ -770,16 +770,25 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
 #pragma unroll
       for (int x = 0; x < CT; ++x) l[x] = __builtin_fmaf(sum[x], pow2(-f), l[x]);
     }
+    // the second product, each 16 channels' fragments read while the ones
+    // before are multiplied
+    tok_u32x4 vf[2][2];
+    auto read_v = [&](int d) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        vf[d & 1][u] = *reinterpret_cast<const tok_u32x4*>(&vbuf[buf][(d * 2 + u) * 1024 + lane * 16]);
+    };
+    read_v(0);
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (d + 1 < DT) read_v(d + 1);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const tok_u32x4 vf = *reinterpret_cast<const tok_u32x4*>(&vbuf[buf][(d * 2 + u) * 1024 + lane * 16]);
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int x = 0; x < CT; ++x)
 #pragma unroll
-          for (int n = 0; n < NP; ++n) acc[x][d] = mfma_f16(vf, pf[x][u][n], acc[x][d]);
-      }
+          for (int n = 0; n < NP; ++n) acc[x][d] = mfma_f16(vf[d & 1][u], pf[x][u][n], acc[x][d]);
     }
     __builtin_amdgcn_sched_barrier(0);
     if (partial(tok0, cur) && (nan_seen[buf][0] | nan_seen[buf][1] | nan_seen[buf][2] | nan_seen[buf][3])) {
