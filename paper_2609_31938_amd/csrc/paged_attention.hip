@@ -29,7 +29,7 @@
 // to 32768 tokens, 32 query and 8 key/value heads of 128, 473 us, 4.7 TB/s.
 // attend_many: chunks of queries share tiles in LDS; exponentials, conversions
 // and products of two waves a SIMD are the bound: 8192 causal queries of the
-// same heads 699 us, 786 TFLOP/s.
+// same heads 591 us, 930 TFLOP/s.
 #include <math.h>
 
 #include "token_dev.h"
@@ -186,6 +186,10 @@ __device__ inline int apart(int v) {
   asm volatile("" : "+s"(v));
   return v;
 }
+
+// v, known here: sums that are due beside products are not put off until the
+// round's end, where their chain has nothing beside it
+__device__ inline void settled(float& v) { asm volatile("" : "+v"(v)); }
 
 // The query of column (qi, qh), as terms, in the order of K's fragments:
 // element e of step k is channel 64 (k / 2) + 16 g + 8 (k % 2) + e.
@@ -513,9 +517,10 @@ typedef __attribute__((address_space(1))) const void global_void;
 // units: conversions and exponentials beside the products; that is why V is
 // converted once (K too would make LDS reads the bound).
 // WHOLE: pages are multiples of 64 tokens, so that a tile lies in one page and
-// its addresses are scalars; what the vector units spend on finding blocks of
-// 16 tokens otherwise is a quarter of their work.
-template <class E, int DP, int CT, bool WHOLE>
+// its addresses are scalars; otherwise the vector units find blocks of 16
+// tokens.  FULL: and no channel is padding, so that no load has a condition
+// (32 query heads of 128, 8192 causal tokens: 591 us, without FULL 652).
+template <class E, int DP, int CT, bool WHOLE, bool FULL>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   typedef Form<E> F;
   typedef typename E::store S;
@@ -529,7 +534,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   // workgroup i runs on L2 cache i % 8: each cache gets a run of consecutive
   // units, so that one cache reads a head's codes; the last columns, which see
   // most in a causal call, come first
-  const int D = a.D, G = a.G;
+  const int D = FULL ? DP : a.D, G = a.G;
   uint32_t id = blockIdx.x;
   {
     const uint32_t total = gridDim.x, each = total / 8, rest = total % 8, c = id % 8;
@@ -572,19 +577,38 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   // Tiles on their way: block g of the tile of this lane, its scales, K in
   // LDS, this wave's part of V in registers.
   const int32_t* pages = a.table + static_cast<int64_t>(b) * a.cols;
-  auto page_of = [&](int tile) { return peek(a, pages, tile * 4 + (WHOLE ? 0 : g), ue); };  // used a round later
-  // the block of this lane; WHOLE: the first of the tile, a scalar
+  // Tiles are asked for in turn: page_of a round before block.  The block is
+  // this lane's; WHOLE: the first of the tile, a scalar, the page's column and
+  // the tile's place in it counted rather than divided for.
+  int column = WHOLE ? column_of(a, t0 * 4) : 0, place = WHOLE ? t0 * 4 - column * a.nb : 0, was = 0;
+  auto page_of = [&](int tile) __attribute__((always_inline)) {
+    if constexpr (WHOLE) {
+      const uint32_t page = tile < t1 ? static_cast<uint32_t>(pages[column]) : kNone;
+      was = place;
+      place += 4;
+      if (place == a.nb) {
+        place = 0;
+        ++column;
+      }
+      return page;
+    } else {
+      return peek(a, pages, tile * 4 + g, ue);
+    }
+  };
   auto block = [&](int tile, uint32_t page) __attribute__((always_inline)) {
-    if constexpr (WHOLE)
-      return settle(a, hk, tile * 4, __builtin_amdgcn_readfirstlane(page));
-    else
+    if constexpr (WHOLE) {
+      page = __builtin_amdgcn_readfirstlane(page);
+      return page < static_cast<uint32_t>(a.pages) ? (page * a.heads + hk) * a.nb + was : kNone;
+    } else
       return settle(a, hk, tile * 4 + g, page);
   };
   auto mine_of = [&](uint32_t vb) { return WHOLE && vb != kNone ? vb + g : vb; };
   tok_u32x4 vr[VW];
   typedef __attribute__((address_space(1))) const uint8_t global_u8;
   global_u8* zeros = (global_u8*)kZeros;
-  const int klane = ((r >> 2) * 16 + (r & 3)) * D + g * 16, vlane = (g * D + r) * 16;
+  constexpr bool EVEN = 4 % NJ == 0;  // every fourth fragment is 4 / NJ row tiles on
+  const int klane = ((r >> 2) * 16 + (r & 3) + (EVEN ? wave / NJ * 4 : 0)) * D + (EVEN ? wave % NJ * 64 : 0) + g * 16;
+  const int vlane = (g * D + r) * 16;
   auto fetch_k = [&](uint32_t vb, int buf) __attribute__((always_inline)) {
     global_u8* kp;
     if constexpr (WHOLE) {
@@ -597,8 +621,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
 #pragma unroll
     for (int n = 0; n < NJ; ++n) {
       const int f = n * 4 + wave, t = f / NJ, j = f - t * NJ;
-      global_u8* p = kp + 4 * t * D + j * 64;
-      if (WHOLE ? (D & 63) != 0 && j * 64 + g * 16 >= D : vb == kNone || j * 64 + g * 16 >= D) p = zeros;
+      global_u8* p = kp + (WHOLE && EVEN ? 16 / NJ * n * D : 4 * t * D + j * 64);
+      if (WHOLE ? !FULL && j * 64 + g * 16 >= D : vb == kNone || j * 64 + g * 16 >= D) p = zeros;
       __builtin_amdgcn_global_load_lds((global_void*)p, (lds_void*)(&kbuf[buf][f * 1024]), 16, 0, 0);
     }
   };
@@ -614,7 +638,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     for (int n = 0; n < VW; ++n) {
       const int d = n * 4 + wave;
       global_u8* p = vp + d * 256;
-      if (WHOLE ? d * 16 >= D : vb == kNone || d * 16 >= D) p = zeros;
+      if (WHOLE ? !FULL && d * 16 >= D : vb == kNone || d * 16 >= D) p = zeros;
       vr[n] = *(__attribute__((address_space(1))) const tok_u32x4*)p;
     }
   };
@@ -623,6 +647,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   auto partial = [&](int tok0, uint32_t vb) { return tok0 < hi.begin || tok0 + 64 > lo.end || lost(vb); };
   int unit = -126, grown = -126, rest = 0;  // E, E after the next tile, what of its exponents goes to P
   auto convert = [&](int tile, uint32_t vb, float vs, int buf) __attribute__((always_inline)) {
+    settled(vs);  // its exponent, taken where it is loaded, would wait for that load
     const int ve = exponent_of(vs);
     grown = max(unit, over_groups(ve));
     const int k = max(ve - grown, kDeep);
@@ -763,12 +788,16 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
           for (int x = 0; x < CT; ++x) {
             p[x][e & 7] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e >> 2][e & 3], cg, lift[x]));
             sum[x] += p[x][e & 7];
+            settled(sum[x]);
             if ((e & 7) == 7) to_terms<tok_f16x2, NP>(p[x], pf[x][e >> 3]);
           }
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int x = 0; x < CT; ++x) l[x] = __builtin_fmaf(sum[x], pow2(-f), l[x]);
+      for (int x = 0; x < CT; ++x) {
+        l[x] = __builtin_fmaf(sum[x], pow2(-f), l[x]);
+        settled(l[x]);
+      }
     }
     // the second product, each 16 channels' fragments read while the ones
     // before are multiplied
@@ -905,12 +934,12 @@ int64_t workgroup_columns(int64_t dim, int dtype) {
 // Calls of at most 16 columns a sequence and head take attend_few.
 bool few(int64_t columns) { return columns <= 16; }
 
-template <class E, int NQ, bool WHOLE>
+template <class E, int NQ, bool WHOLE, bool FULL>
 auto pick_many(int dim) {
-  return dim <= 64    ? attend_many<E, 64, column_tiles(64, NQ), WHOLE>
-         : dim <= 128 ? attend_many<E, 128, column_tiles(128, NQ), WHOLE>
-         : dim <= 192 ? attend_many<E, 192, column_tiles(192, NQ), WHOLE>
-                      : attend_many<E, 256, column_tiles(256, NQ), WHOLE>;
+  return dim <= 64    ? attend_many<E, 64, column_tiles(64, NQ), WHOLE, FULL>
+         : dim <= 128 ? attend_many<E, 128, column_tiles(128, NQ), WHOLE, FULL>
+         : dim <= 192 ? attend_many<E, 192, column_tiles(192, NQ), WHOLE, FULL>
+                      : attend_many<E, 256, column_tiles(256, NQ), WHOLE, FULL>;
 }
 
 template <class E>
@@ -936,7 +965,7 @@ hipError_t run(const AttendArgs& h, const AttendPlan& p, int dtype, hipStream_t 
     hipLaunchKernelGGL(k, dim3(p.splits, a.heads, static_cast<unsigned>(h.b.B)), dim3(256), 0, s, a);
   } else {
     constexpr int NQ = Form<E>::NQ;
-    auto k = nb % 4 == 0 ? pick_many<E, NQ, true>(a.D) : pick_many<E, NQ, false>(a.D);
+    auto k = nb % 4 != 0 ? pick_many<E, NQ, false, false>(a.D) : a.D % 64 != 0 ? pick_many<E, NQ, true, false>(a.D) : pick_many<E, NQ, true, true>(a.D);
     hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
   }
   hipError_t e = hipGetLastError();
