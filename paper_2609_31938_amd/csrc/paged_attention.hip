@@ -508,6 +508,12 @@ __device__ const uint32_t kZeros[4] = {0, 0, 0, 0};
 typedef __attribute__((address_space(3))) void lds_void;
 typedef __attribute__((address_space(1))) const void global_void;
 
+// Workgroup barrier behind which every wave sees what the others stored in LDS
+// and loaded into it.  The waits are written out: __syncthreads() asks for none
+// for a wave's loads into LDS, and at the head of a loop this compiler drops the
+// one for the stores of the loop's end.
+__device__ inline void lds_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // One workgroup: 4 waves of CT column tiles each, one sequence, one key/value
 // head, one split of the tokens.  K's codes of a 64-token tile come straight
 // into LDS, fragment by fragment (1 KB each: a lane's 16 bytes side by side, so
@@ -726,12 +732,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
     }
     page = page_of(t0 + 2);
     convert(t0, cur, vs, t0 & 1);
-    __syncthreads();
+    lds_barrier();
     first(t0 & 1, s);
   }
   for (int tile = t0; tile < t1; ++tile) {
     const int buf = tile & 1, tok0 = tile * 64;
-    __syncthreads();  // what this round reads is in LDS, and nobody reads what it writes
+    lds_barrier();  // what this round reads is in LDS, and nobody reads what it writes
     float ks1 = 1.f, vs1 = 1.f;
     const uint32_t far = block(tile + 2, page);
     if (tile + 1 < t1) {
