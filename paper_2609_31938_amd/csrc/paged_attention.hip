@@ -167,14 +167,15 @@ __device__ inline Seq sequence(const Dev& a, int b) {
 }
 
 // Blocks of a sequence are found in two steps, so that nothing waits for the
-// page table: peek reads the page of block blk (none where the block begins at
-// `end` or later), settle makes it the block's index among the cache's (of
-// head hk), or kNone.
+// page table: peek reads the page of block blk (none where no token of it lies
+// in [begin, end)), settle makes it the block's index among the cache's (of
+// head hk), or kNone.  A block that no query sees may hold anything, its scales
+// included: it is not read.
 constexpr uint32_t kNone = 0xffffffffu;
 __device__ inline int column_of(const Dev& a, int blk) { return a.pow >= 0 ? blk >> a.pow : blk / a.nb; }
-__device__ inline uint32_t peek(const Dev& a, const int32_t* row, int blk, int end) {
+__device__ inline uint32_t peek(const Dev& a, const int32_t* row, int blk, int begin, int end) {
   const int col = column_of(a, blk);
-  return blk * 16 < end && col < a.cols ? static_cast<uint32_t>(row[col]) : kNone;
+  return blk * 16 + 15 >= begin && blk * 16 < end && col < a.cols ? static_cast<uint32_t>(row[col]) : kNone;
 }
 __device__ inline uint32_t settle(const Dev& a, int hk, int blk, uint32_t page) {
   return page < static_cast<uint32_t>(a.pages) ? (page * a.heads + hk) * a.nb + (blk - column_of(a, blk) * a.nb) : kNone;
@@ -380,19 +381,19 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few(Dev a) {
     }
   };
   Tile next;
-  uint32_t page = peek(a, pages, (t0 + wave) * 4 + g, ue);
+  uint32_t page = peek(a, pages, (t0 + wave) * 4 + g, ub, ue);
   if (AHEAD && t0 + wave < t1) load(t0 + wave, page, next);
-  page = peek(a, pages, (t0 + wave + (AHEAD ? 4 : 0)) * 4 + g, ue);
+  page = peek(a, pages, (t0 + wave + (AHEAD ? 4 : 0)) * 4 + g, ub, ue);
   for (int tile = t0 + wave; tile < t1; tile += 4) {
     const int tok0 = tile * 64;
     Tile now;
     if (AHEAD) {
       now = next;
       if (tile + 4 < t1) load(tile + 4, page, next);
-      page = peek(a, pages, (tile + 8) * 4 + g, ue);
+      page = peek(a, pages, (tile + 8) * 4 + g, ub, ue);
     } else {
       load(tile, page, now);
-      page = peek(a, pages, (tile + 4) * 4 + g, ue);
+      page = peek(a, pages, (tile + 4) * 4 + g, ub, ue);
     }
     const uint32_t vb = now.vb;
     const bool vok = vb != kNone;
@@ -598,7 +599,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
       }
       return page;
     } else {
-      return peek(a, pages, tile * 4 + g, ue);
+      return peek(a, pages, tile * 4 + g, ub, ue);
     }
   };
   auto block = [&](int tile, uint32_t page) __attribute__((always_inline)) {
@@ -654,7 +655,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   int unit = -126, grown = -126, rest = 0;  // E, E after the next tile, what of its exponents goes to P
   auto convert = [&](int tile, uint32_t vb, float vs, int buf) __attribute__((always_inline)) {
     settled(vs);  // its exponent, taken where it is loaded, would wait for that load
-    const int ve = exponent_of(vs);
+    int ve = exponent_of(vs);
+    // whole tiles have blocks that no query sees, whose scales may be anything
+    // (key scales do no harm: scores of -inf stay so)
+    if (WHOLE && (tile * 64 + 16 * g + 15 < ub || tile * 64 + 16 * g >= ue)) ve = -126;
     grown = max(unit, over_groups(ve));
     const int k = max(ve - grown, kDeep);
     rest = max(ve - grown - k, kLeast);
