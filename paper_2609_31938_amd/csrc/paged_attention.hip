@@ -656,13 +656,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   auto convert = [&](int tile, uint32_t vb, float vs, int buf) __attribute__((always_inline)) {
     settled(vs);  // its exponent, taken where it is loaded, would wait for that load
     int ve = exponent_of(vs);
-    // whole tiles have blocks that no query sees, whose scales may be anything
-    // (key scales do no harm: scores of -inf stay so)
-    if (WHOLE && (tile * 64 + 16 * g + 15 < ub || tile * 64 + 16 * g >= ue)) ve = -126;
-    grown = max(unit, over_groups(ve));
-    const int k = max(ve - grown, kDeep);
-    rest = max(ve - grown - k, kLeast);
-    const float vk = pow2(k);
     if (partial(tile * 64, vb)) {
       // values that no column sees become 0; NaN among the others are taken
       // out of the product and put back where they are seen
@@ -677,9 +670,17 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
           vr[n][t] = no_nan(vr[n][t]);
         }
       }
+      // nor do the scales of whole tiles' unseen blocks count, which may be
+      // anything (key scales do no harm: scores of -inf stay so).  Outside this
+      // branch the test costs 10 us of the 596 of 8192 causal tokens.
+      if (WHOLE && (tile * 64 + 16 * g + 15 < ub || tile * 64 + 16 * g >= ue)) ve = -126;
       const bool seen = __ballot(any) != 0;
       if (lane == 0) nan_seen[buf][wave] = seen;
     }
+    grown = max(unit, over_groups(ve));
+    const int k = max(ve - grown, kDeep);
+    rest = max(ve - grown - k, kLeast);
+    const float vk = pow2(k);
 #pragma unroll
     for (int n = 0; n < VW; ++n)
 #pragma unroll
