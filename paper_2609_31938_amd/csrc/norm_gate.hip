@@ -74,7 +74,8 @@ struct NormArgs {
   float* u_scale;
   int64_t T, C, rows;
   float alpha, eps;
-  bool stream;  // outputs are more than the caches hold
+  bool stream;    // outputs are more than the caches hold
+  int64_t first;  // workgroup of this launch
 };
 
 // NV vectors of the row in each thread's registers.
@@ -85,7 +86,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_gate_regs(NormArgs a) 
   __shared__ float lds[3 * 16];
   const Row<WAVE> row{lds};
   const int per = WAVE ? 64 : blockDim.x;  // threads of a row
-  const int64_t t = WAVE ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const int64_t wg = a.first + blockIdx.x, t = WAVE ? wg * 4 + (threadIdx.x >> 6) : wg;
   const int lane = WAVE ? threadIdx.x & 63 : threadIdx.x;
   if (WAVE && t >= a.T) return;  // whole waves, and no barrier follows
   const int C = static_cast<int>(a.C);
@@ -184,7 +185,7 @@ __global__ __launch_bounds__(1024) void norm_gate_loop(NormArgs a) {
   typedef typename E::store S;
   __shared__ float lds[3 * 16];
   const Row<false> row{lds};
-  const int64_t t = blockIdx.x;
+  const int64_t t = a.first + blockIdx.x;
   const S* hp = static_cast<const S*>(a.h) + t * a.C;
   const S* yp = a.y ? static_cast<const S*>(a.y) + t * a.C : nullptr;
   const S* gp = a.gate ? static_cast<const S*>(a.gate) + t / a.rows * a.C : nullptr;
@@ -236,6 +237,7 @@ struct QuantArgs {
   int8_t* q;
   float* scale;
   int64_t T, C, ld_x, ld_q;  // q's rows are zero from C to ld_q
+  int64_t first;             // workgroup of this launch
 };
 
 template <class E, int NV, bool WAVE>
@@ -244,7 +246,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void quantize_regs(QuantArgs a) 
   __shared__ float lds[16];
   const Row<WAVE> row{lds};
   const int per = WAVE ? 64 : blockDim.x;
-  const int64_t t = WAVE ? static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const int64_t wg = a.first + blockIdx.x, t = WAVE ? wg * 4 + (threadIdx.x >> 6) : wg;
   const int lane = WAVE ? threadIdx.x & 63 : threadIdx.x;
   if (WAVE && t >= a.T) return;
   const int C = static_cast<int>(a.C), Q = static_cast<int>(a.ld_q);
@@ -271,7 +273,7 @@ template <class E>
 __global__ __launch_bounds__(1024) void quantize_loop(QuantArgs a) {
   __shared__ float lds[16];
   const Row<false> row{lds};
-  const int64_t t = blockIdx.x;
+  const int64_t t = a.first + blockIdx.x;
   const typename E::store* x = static_cast<const typename E::store*>(a.x) + t * a.ld_x;
   float top = 0.f;
   for (int64_t c = threadIdx.x; c < a.C; c += blockDim.x) top = fmaxf(top, magnitude(E::widen(x[c])));
@@ -287,15 +289,15 @@ __global__ __launch_bounds__(1024) void quantize_loop(QuantArgs a) {
 struct Shape {
   bool wave;
   int nv;  // vectors a thread; 0: the loop
-  unsigned threads, blocks;
+  unsigned threads;
+  int64_t blocks;
 };
 Shape shape_of(int64_t T, int64_t vecs) {
   auto ceil = [](int64_t a, int64_t b) { return (a + b - 1) / b; };
-  if (vecs <= 128) return {true, vecs <= 64 ? 1 : 2, 256, static_cast<unsigned>(ceil(T, 4))};
-  const unsigned blocks = static_cast<unsigned>(T);
-  if (vecs > 4 * 1024) return {false, 0, 1024, blocks};
+  if (vecs <= 128) return {true, vecs <= 64 ? 1 : 2, 256, ceil(T, 4)};
+  if (vecs > 4 * 1024) return {false, 0, 1024, T};
   const int nv = vecs <= 1024 ? 1 : vecs <= 2048 ? 2 : 4;
-  return {false, nv, static_cast<unsigned>(ceil(ceil(vecs, nv), 64) * 64), blocks};
+  return {false, nv, static_cast<unsigned>(ceil(ceil(vecs, nv), 64) * 64), T};
 }
 
 template <class E>
@@ -307,20 +309,24 @@ hipError_t norm_typed(NormArgs a, hipStream_t s) {
            : p.nv == 1 ? norm_gate_regs<E, 1, false>
            : p.nv == 2 ? norm_gate_regs<E, 2, false>
                        : norm_gate_regs<E, 4, false>;
-  hipLaunchKernelGGL(k, dim3(p.blocks), dim3(p.threads), 0, s, a);
-  return hipGetLastError();
+  return in_launches(p.blocks, p.threads, [&](int64_t first, unsigned count) {
+    a.first = first;
+    hipLaunchKernelGGL(k, dim3(count), dim3(p.threads), 0, s, a);
+  });
 }
 
 template <class E>
-hipError_t quantize_typed(const QuantArgs& a, hipStream_t s) {
+hipError_t quantize_typed(QuantArgs a, hipStream_t s) {
   const Shape p = shape_of(a.T, (a.ld_q + E::VEC - 1) / E::VEC);
   auto k = p.nv == 0 ? quantize_loop<E>
            : p.wave  ? (p.nv == 1 ? quantize_regs<E, 1, true> : quantize_regs<E, 2, true>)
            : p.nv == 1 ? quantize_regs<E, 1, false>
            : p.nv == 2 ? quantize_regs<E, 2, false>
                        : quantize_regs<E, 4, false>;
-  hipLaunchKernelGGL(k, dim3(p.blocks), dim3(p.threads), 0, s, a);
-  return hipGetLastError();
+  return in_launches(p.blocks, p.threads, [&](int64_t first, unsigned count) {
+    a.first = first;
+    hipLaunchKernelGGL(k, dim3(count), dim3(p.threads), 0, s, a);
+  });
 }
 
 }  // namespace
@@ -330,7 +336,7 @@ hipError_t launch_norm_gate(const c3c_norm_desc& d, const void* h, const void* y
                             float* u_scale, hipStream_t s) {
   if (d.T == 0) return hipSuccess;
   const NormArgs a{h, y, gate, post, pre, h_out, u, u_q, u_scale, d.T, d.C, gate ? d.rows_per_gate : 1, d.alpha, d.eps,
-                   false};
+                   false, 0};
   return d.dtype == C3C_DTYPE_BF16  ? norm_typed<ElemBf16>(a, s)
          : d.dtype == C3C_DTYPE_F16 ? norm_typed<ElemF16>(a, s)
                                     : norm_typed<ElemF32>(a, s);
@@ -339,7 +345,7 @@ hipError_t launch_norm_gate(const c3c_norm_desc& d, const void* h, const void* y
 hipError_t launch_quantize_rows(int64_t T, int64_t C, int64_t ld_x, int dtype, const void* x,
                                 int8_t* q, int64_t ld_q, float* scale, hipStream_t s) {
   if (T == 0) return hipSuccess;
-  const QuantArgs a{x, q, scale, T, C, ld_x, ld_q};
+  const QuantArgs a{x, q, scale, T, C, ld_x, ld_q, 0};
   return dtype == C3C_DTYPE_BF16  ? quantize_typed<ElemBf16>(a, s)
          : dtype == C3C_DTYPE_F16 ? quantize_typed<ElemF16>(a, s)
                                   : quantize_typed<ElemF32>(a, s);

@@ -11,6 +11,19 @@ namespace c3c {
 
 int64_t device_compute_units();  // of the current device (256 when none is visible)
 
+// A dimension of a launch has fewer than 2^32 threads: more workgroups than
+// that go in several launches, launch(first, count) each.
+template <class F>
+hipError_t in_launches(int64_t workgroups, int64_t threads, F launch) {
+  const int64_t most = (int64_t(1) << 31) / threads;
+  hipError_t e = hipSuccess;
+  for (int64_t first = 0; first < workgroups && e == hipSuccess; first += most) {
+    launch(first, static_cast<unsigned>(workgroups - first < most ? workgroups - first : most));
+    e = hipGetLastError();
+  }
+  return e;
+}
+
 // quantize_rows and norm_gate (norm_gate.hip)
 hipError_t launch_quantize_rows(int64_t T, int64_t C, int64_t ld_x, int dtype, const void* x,
                                 int8_t* q, int64_t ld_q, float* scale, hipStream_t s);
