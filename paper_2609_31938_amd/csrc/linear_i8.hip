@@ -48,6 +48,7 @@ struct LinArgs {
   int tiles_m, tiles_n;
   int splits;     // along K, in stages
   int y_dtype;
+  int64_t first;  // workgroup of this launch
 };
 
 // w_scale and bias of four consecutive channels (the last one's past N)
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(256) void linear_skinny(LinArgs a) {
   __shared__ float tops[4][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int r = lane & 15, g = lane >> 4;
-  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 16;
+  const int64_t n0 = (a.first + blockIdx.x) * 16;
   const int64_t nr = n0 + r < a.N ? n0 + r : a.N - 1;
   const int8_t* wp = a.w + nr * a.K;
   constexpr int U = 8 / MT < 4 ? 4 : 8 / MT;  // stages in flight
@@ -246,7 +247,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
   // tiles, walked in columns of 6 tiles of tokens (32760 x 5120 x 5120: 794 us;
   // columns of 4 809, of 8 857)
   const int total = a.tiles_m * a.tiles_n;
-  int b = blockIdx.x;
+  int b = static_cast<int>(a.first) + blockIdx.x;
   const int split = b / total;
   b -= split * total;
   {
@@ -424,8 +425,9 @@ __global__ __launch_bounds__(256) void linear_join(LinArgs a) {
 
 // Rows of n bytes, ld apart, to rows of ldd (a multiple of 16), zero past n: 16
 // bytes a thread.
-__global__ __launch_bounds__(256) void pad_rows(const int8_t* src, int64_t rows, int64_t n, int64_t ld, int8_t* dst, int64_t ldd) {
-  const int64_t per = ldd / 16, i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void pad_rows(const int8_t* src, int64_t rows, int64_t n, int64_t ld, int8_t* dst, int64_t ldd,
+                                               int64_t first) {
+  const int64_t per = ldd / 16, i = (first + blockIdx.x) * 256 + threadIdx.x;
   if (i >= rows * per) return;
   const int64_t r = i / per, c = i % per * 16;
   *reinterpret_cast<tok_i32x4*>(dst + r * ldd + c) = piece<false>(src + r * ld + c, n - c);
@@ -453,8 +455,17 @@ hipError_t run_tiled(LinArgs a, hipStream_t s) {
   a.tiles_n = static_cast<int>(up(a.N, BN));
   const int64_t blocks = static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.splits;
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)), dim3(threads), 0, s, a);
-  return hipGetLastError();
+  return in_launches(blocks, threads, [&](int64_t first, unsigned count) {
+    a.first = first;
+    hipLaunchKernelGGL(k, dim3(count), dim3(threads), 0, s, a);
+  });
+}
+
+hipError_t run_skinny(void (*k)(LinArgs), LinArgs a, hipStream_t s) {
+  return in_launches(up(a.N, 16), 256, [&](int64_t first, unsigned count) {
+    a.first = first;
+    hipLaunchKernelGGL(k, dim3(count), dim3(256), 0, s, a);
+  });
 }
 
 // tokens of the skinny kernel (4096 x 4096: 32 tokens 13.4 us, 65 in tiles 12.2;
@@ -492,23 +503,21 @@ hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, in
                             const float* bias, void* y, int y_dtype, const LinearPlan& plan,
                             int32_t* part, hipStream_t s) {
   if (M == 0) return hipSuccess;
-  LinArgs a{x, w, x_scale, w_scale, bias, y, part, M, N, K, ldx, 0, 0, part ? plan.splits : 1, y_dtype};
+  LinArgs a{x, w, x_scale, w_scale, bias, y, part, M, N, K, ldx, 0, 0, part ? plan.splits : 1, y_dtype, 0};
   // 16-byte pieces, and a tile's rows within the 31-bit offsets of a buffer
   const bool al = K % 16 == 0 && ldx % 16 == 0 && ldx < (1 << 22) && reinterpret_cast<uintptr_t>(x) % 16 == 0 &&
                   reinterpret_cast<uintptr_t>(w) % 16 == 0;
   if (M <= kSkinny) {
     auto k = M <= 16   ? (al ? linear_skinny<Codes, 1, true> : linear_skinny<Codes, 1, false>)
                        : (al ? linear_skinny<Codes, 2, true> : linear_skinny<Codes, 2, false>);
-    hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(up(N, 16))), dim3(256), 0, s, a);
-    return hipGetLastError();
+    return run_skinny(k, a, s);
   }
   const Tile t = tile_of(M, N);
   hipError_t e = t.bm == 256   ? (al ? run_tiled<256, 256, 128, 64, 128, 2, true>(a, s) : run_tiled<256, 256, 128, 64, 64, 4, false>(a, s))
                  : t.bm == 128 ? (al ? run_tiled<128, 128, 64, 64, 64, 4, true>(a, s) : run_tiled<128, 128, 64, 64, 64, 4, false>(a, s))
                                : (al ? run_tiled<64, 64, 32, 32, 64, 4, true>(a, s) : run_tiled<64, 64, 32, 32, 64, 4, false>(a, s));
   if (e == hipSuccess && part) {
-    const int64_t blocks = up(M * up(N, 4), 256);
-    if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+    const int64_t blocks = up(M * up(N, 4), 256);  // few: a call of many tiles is not split
     hipLaunchKernelGGL(linear_join, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
     e = hipGetLastError();
   }
@@ -520,10 +529,9 @@ hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, in
 bool linear_pads(int64_t M, int64_t K, int64_t ld) { return M > 64 && (K % 16 != 0 || ld % 16 != 0); }
 
 hipError_t launch_pad_rows(const int8_t* src, int64_t rows, int64_t n, int64_t ld, int8_t* dst, int64_t ldd, hipStream_t s) {
-  const int64_t blocks = up(rows * (ldd / 16), 256);
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL(pad_rows, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, src, rows, n, ld, dst, ldd);
-  return hipGetLastError();
+  return in_launches(up(rows * (ldd / 16), 256), 256, [&](int64_t first, unsigned count) {
+    hipLaunchKernelGGL(pad_rows, dim3(count), dim3(256), 0, s, src, rows, n, ld, dst, ldd, first);
+  });
 }
 
 bool linear_quantises(int64_t M, int64_t K) { return M <= 4 && M * ((K + 15) / 16 * 16) <= kFusedBytes; }
@@ -532,13 +540,12 @@ hipError_t launch_linear_float(int64_t M, int64_t N, int64_t K, const void* x, i
                                const int8_t* w, const float* w_scale, const float* bias, void* y, int y_dtype,
                                hipStream_t s) {
   if (M == 0) return hipSuccess;
-  LinArgs a{static_cast<const int8_t*>(x), w, nullptr, w_scale, bias, y, nullptr, M, N, K, ldx, 0, 0, 1, y_dtype};
+  LinArgs a{static_cast<const int8_t*>(x), w, nullptr, w_scale, bias, y, nullptr, M, N, K, ldx, 0, 0, 1, y_dtype, 0};
   const bool al = K % 16 == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
   auto k = x_dtype == C3C_DTYPE_BF16  ? (al ? linear_skinny<ElemBf16, 1, true> : linear_skinny<ElemBf16, 1, false>)
            : x_dtype == C3C_DTYPE_F16 ? (al ? linear_skinny<ElemF16, 1, true> : linear_skinny<ElemF16, 1, false>)
                                       : (al ? linear_skinny<ElemF32, 1, true> : linear_skinny<ElemF32, 1, false>);
-  hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(up(N, 16))), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return run_skinny(k, a, s);
 }
 
 }  // namespace c3c

@@ -38,3 +38,28 @@ def test_quantize_rows():
     for at in ends(MANY):
         qw, sw = tokens.quantize_rows(ctx, x[at])
         assert torch.equal(q[at], qw) and torch.equal(s[at], sw), at
+
+
+@pytest.mark.parametrize("x_dtype", ["i8", "bf16"])
+def test_linear_of_few_tokens(x_dtype):
+    """Output channels by 16 a workgroup of 256 threads: more than 2^28."""
+    N, K, ctx = (1 << 28) + 33, 8, c3c.Context()
+    w = torch.randint(-127, 128, (N, K), dtype=torch.int8, device="cuda")
+    ws = torch.rand(N, device="cuda")
+    x = torch.randint(-127, 128, (1, K), device="cuda")
+    x, xs = (x.to(torch.int8), torch.ones(1, device="cuda")) if x_dtype == "i8" else (x.bfloat16(), None)
+    ctx.set_workspace(torch.empty(4096, dtype=torch.uint8, device="cuda"))
+    y = tokens.linear_i8(ctx, x, w, ws, x_scale=xs)
+    for s in (slice(0, 301), slice((1 << 27) - 300, (1 << 27) + 300), slice((1 << 28) - 300, N)):
+        assert torch.equal(y[:, s], tokens.linear_i8(ctx, x, w[s], ws[s], x_scale=xs)), s
+
+
+def test_linear_of_many_tokens():
+    """256 tokens a workgroup of 512 threads: 2^31 - 1."""
+    M, ctx = (1 << 31) - 1, c3c.Context()
+    x = torch.randint(-127, 128, (M, 1), dtype=torch.int8, device="cuda")
+    s = torch.full((M,), 0.25, device="cuda")
+    w, ws = torch.full((1, 1), 3, dtype=torch.int8, device="cuda"), torch.ones(1, device="cuda")
+    y = tokens.linear_i8(ctx, x, w, ws, x_scale=s)
+    for at in (slice(0, 999), slice((1 << 30) - 999, (1 << 30) + 999), slice(M - 999, M)):
+        assert torch.equal(y[at], (x[at].float() * 0.75).bfloat16()), at
