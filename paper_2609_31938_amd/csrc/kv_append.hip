@@ -338,10 +338,12 @@ hipError_t typed(const AppendArgs& a, dim3 grid, hipStream_t s) {
 
 hipError_t launch_kv_append(const AppendArgs& a, int dtype, hipStream_t s) {
   if (a.b.B == 0 || a.b.T == 0 || a.b.max_new == 0) return hipSuccess;
-  // n new tokens touch at most (n + 14) / 16 + 1 blocks
-  int64_t bx = (a.b.max_new + 14) / 16 + 1;
+  // n new tokens touch at most (n + 14) / 16 + 1 blocks; no sequence has more
+  // than T, and blocks past the 2^23 of a launch's threads are taken in turn
+  const int64_t n = a.b.max_new < a.b.T ? a.b.max_new : a.b.T, most = int64_t(1) << 23;
+  const int64_t bx = (n + 14) / 16 + 1 < most ? (n + 14) / 16 + 1 : most;
   const int64_t units = 2 * a.c.heads + (a.q_out ? a.q_heads : 0), by = (units + 3) / 4;
-  if (a.b.B > 65535 || by > 65535 || bx > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (a.b.B > 65535 || by > 65535) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<unsigned>(bx), static_cast<unsigned>(by), static_cast<unsigned>(a.b.B));
   return dtype == C3C_DTYPE_BF16  ? typed<ElemBf16>(a, grid, s)
          : dtype == C3C_DTYPE_F16 ? typed<ElemF16>(a, grid, s)

@@ -63,3 +63,33 @@ def test_linear_of_many_tokens():
     y = tokens.linear_i8(ctx, x, w, ws, x_scale=s)
     for at in (slice(0, 999), slice((1 << 30) - 999, (1 << 30) + 999), slice(M - 999, M)):
         assert torch.equal(y[at], (x[at].float() * 0.75).bfloat16()), at
+
+
+def cache_and_batch(new, old, max_new, Hkv=2, D=16, page=16):
+    """A cache of junk in order of pages, and a batch with this bound."""
+    lens = [n + o for n, o in zip(new, old)]
+    used = [-(-n // page) for n in lens]
+    table = torch.full((len(new), max(used)), -1, dtype=torch.int32)
+    at = 0
+    for b, u in enumerate(used):
+        table[b, :u] = torch.arange(at, at + u)
+        at += u
+    cache = tokens.KVCache.empty(at, Hkv, page, D)
+    for i, t in enumerate((cache.k, cache.v)):
+        t.view(torch.uint8).copy_(torch.randint(0, 120, t.shape, generator=torch.Generator().manual_seed(i)).to(torch.uint8))
+    cu = torch.tensor([0] + new).cumsum(0).int()
+    return cache, tokens.Batch(table.cuda(), cu.cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), max_new=max_new,
+                               max_len=max(lens))
+
+
+@pytest.mark.parametrize("bound", [(1 << 28) - 20, 1 << 28, (1 << 31) - 1])
+def test_append_with_a_loose_bound(bound):
+    """max_new only says that no sequence has more new tokens."""
+    new, old = [40, 1, 7], [3, 20, 0]
+    k, v, q = (ref.randn(s, 48, h, 16).bfloat16() for s, h in ((1, 2), (2, 2), (3, 4)))
+    results = []
+    for m in (40, bound):
+        cache, batch = cache_and_batch(new, old, m)
+        got = tokens.kv_append(c3c.Context(), cache, batch, k, v, q=q)
+        results.append([got] + [t.view(torch.uint8) for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
