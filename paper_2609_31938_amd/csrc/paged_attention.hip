@@ -139,6 +139,8 @@ struct Dev {
   int causal, window;
   float c;                        // scale * log2 e
   int splits, split_tiles, coltiles;
+  uint32_t total;  // workgroups of attend_many
+  int64_t first;   // workgroup of this launch (attend_many, attend_join)
 };
 
 // What a column (a query) sees: tokens [begin, end) of its sequence.
@@ -542,9 +544,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   // units, so that one cache reads a head's codes; the last columns, which see
   // most in a causal call, come first
   const int D = FULL ? DP : a.D, G = a.G;
-  uint32_t id = blockIdx.x;
+  uint32_t id = static_cast<uint32_t>(a.first) + blockIdx.x;
   {
-    const uint32_t total = gridDim.x, each = total / 8, rest = total % 8, c = id % 8;
+    const uint32_t total = a.total, each = total / 8, rest = total % 8, c = id % 8;
     id = c * each + (c < rest ? c : rest) + id / 8;
   }
   const int ct = a.coltiles - 1 - static_cast<int>(id % a.coltiles);
@@ -886,7 +888,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
 template <class E, int NV>  // NV: channels a lane
 __global__ __launch_bounds__(256) void attend_join(Dev a) {
   constexpr int U = 8;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6), rows = static_cast<int64_t>(a.T) * a.q_heads;
+  const int64_t row = (a.first + blockIdx.x) * 4 + (threadIdx.x >> 6), rows = static_cast<int64_t>(a.T) * a.q_heads;
   if (row >= rows) return;
   const int lane = threadIdx.x & 63, D = a.D;
   const float* part = a.part + row * (D + 2);
@@ -958,11 +960,11 @@ hipError_t run(const AttendArgs& h, const AttendPlan& p, int dtype, hipStream_t 
   const int64_t G = h.q_heads / h.c.heads, columns = h.b.max_new * G, nb = h.c.page / 16;
   const int64_t cap = h.b.cols * h.c.page, coltiles = up(columns, workgroup_columns(h.c.dim, dtype));
   const int64_t blocks = coltiles * p.splits * h.c.heads * h.b.B, joins = up(h.b.T * h.q_heads, 4);
-  // 32-bit numbering of columns (of T rows at most), blocks, workgroups and grids
-  if (up(h.b.T * G, 16) * 16 + 1024 > 0x7fffffff || columns > 0x7fffffff - 1024 || joins > 0x7fffffff ||
+  // 32-bit numbering of columns (of T rows at most), blocks and workgroups
+  if (up(h.b.T * G, 16) * 16 + 1024 > 0x7fffffff || columns > 0x7fffffff - 1024 ||
       h.c.pages * h.c.heads * nb >= 0xffffffffll || (few(columns) ? h.b.B > 65535 || h.c.heads > 65535 : blocks > 0x7fffffff))
     return hipErrorInvalidConfiguration;
-  const Dev a{static_cast<const uint8_t*>(h.c.k), static_cast<const uint8_t*>(h.c.v), h.c.k_scale, h.c.v_scale,
+  Dev a{static_cast<const uint8_t*>(h.c.k), static_cast<const uint8_t*>(h.c.v), h.c.k_scale, h.c.v_scale,
               h.b.table, h.b.cu, h.b.len, h.q, h.out, h.lse, h.part, h.ld_q,
               static_cast<int>(h.b.T), static_cast<int>(h.q_heads), static_cast<int>(h.c.heads), static_cast<int>(G),
               static_cast<int>(h.c.dim), static_cast<int>(h.c.pages), static_cast<int>(nb),
@@ -970,20 +972,26 @@ hipError_t run(const AttendArgs& h, const AttendPlan& p, int dtype, hipStream_t 
               // room for the tile arithmetic past the last token
               static_cast<int>(cap < 0x7fff0000 ? cap : 0x7fff0000), h.causal, static_cast<int>(h.window),
               h.scale * kLog2e, p.splits, static_cast<int>(up(tiles_seen(h.b, h.c.page, h.window), p.splits)),
-              static_cast<int>(coltiles)};
+              static_cast<int>(coltiles), static_cast<uint32_t>(few(columns) ? 0 : blocks), 0};
+  hipError_t e;
   if (few(columns)) {
     auto k = a.D <= 64 ? attend_few<E, 64> : a.D <= 128 ? attend_few<E, 128> : a.D <= 192 ? attend_few<E, 192> : attend_few<E, 256>;
     hipLaunchKernelGGL(k, dim3(p.splits, a.heads, static_cast<unsigned>(h.b.B)), dim3(256), 0, s, a);
+    e = hipGetLastError();
   } else {
     constexpr int NQ = Form<E>::NQ;
     auto k = nb % 4 != 0 ? pick_many<E, NQ, false, false>(a.D) : a.D % 64 != 0 ? pick_many<E, NQ, true, false>(a.D) : pick_many<E, NQ, true, true>(a.D);
-    hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
+    e = in_launches(blocks, 256, [&](int64_t first, unsigned count) {
+      a.first = first;
+      hipLaunchKernelGGL(k, dim3(count), dim3(256), 0, s, a);
+    });
   }
-  hipError_t e = hipGetLastError();
   if (e == hipSuccess && p.splits > 1) {
     auto join = a.D <= 64 ? attend_join<E, 1> : a.D <= 128 ? attend_join<E, 2> : attend_join<E, 4>;
-    hipLaunchKernelGGL(join, dim3(static_cast<unsigned>(joins)), dim3(256), 0, s, a);
-    e = hipGetLastError();
+    e = in_launches(joins, 256, [&](int64_t first, unsigned count) {
+      a.first = first;
+      hipLaunchKernelGGL(join, dim3(count), dim3(256), 0, s, a);
+    });
   }
   return e;
 }

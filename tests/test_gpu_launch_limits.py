@@ -93,3 +93,23 @@ def test_append_with_a_loose_bound(bound):
         got = tokens.kv_append(c3c.Context(), cache, batch, k, v, q=q)
         results.append([got] + [t.view(torch.uint8) for t in (cache.k, cache.v, cache.k_scale, cache.v_scale)])
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_attention_of_many_workgroups():
+    """5000 sequences, one of 31000 new tokens: 5000 x 16 heads x 243 tiles of
+    128 columns, 2^24 and more workgroups of 256 threads."""
+    long, B, H, D = 31000, 5000, 16, 16
+    new, old = [long] + [1] * (B - 1), [0] + [5 + b % 90 for b in range(B - 1)]
+    cache, batch = cache_and_batch(new, old, long, Hkv=H)
+    q = ref.randn(1, long + B - 1, H, D).bfloat16()
+    ctx = c3c.Context()
+    got = tokens.paged_attention(ctx, cache, batch, q)
+    zero = torch.zeros(1, dtype=torch.int32, device="cuda")
+    one = tokens.Batch(batch.table[:1].contiguous(), batch.cu[:2].contiguous(), batch.lens[:1].contiguous(),
+                       max_new=long, max_len=long)
+    assert torch.equal(got[:long], tokens.paged_attention(ctx, cache, one, q[:long].contiguous()))
+    for b in (1, 900, 2000, B - 200):  # a hundred single tokens, as chunk calls take them
+        cu = torch.cat([zero, torch.arange(1, 101, dtype=torch.int32, device="cuda")])
+        part = tokens.Batch(batch.table[b:b + 100].contiguous(), cu, batch.lens[b:b + 100].contiguous(), max_new=100, max_len=100)
+        rows = slice(long + b - 1, long + b + 99)
+        assert torch.equal(got[rows], tokens.paged_attention(ctx, cache, part, q[rows].contiguous())), b
