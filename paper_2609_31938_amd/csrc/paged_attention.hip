@@ -930,10 +930,13 @@ __global__ __launch_bounds__(256) void attend_join(Dev a) {
 
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// New tokens of a sequence: max_new is a bound, which may be a loose one.
+int64_t most_new(const c3c_kv_batch& b) { return b.max_new < b.T ? b.max_new : b.T; }
+
 // 64-token tiles that one column tile sees at most
 int64_t tiles_seen(const c3c_kv_batch& b, int64_t page, int64_t window) {
   int64_t tokens = b.max_len < b.cols * page ? b.max_len : b.cols * page;
-  if (window > 0 && window + b.max_new < tokens) tokens = window + b.max_new + 64;
+  if (window > 0 && window + most_new(b) < tokens) tokens = window + most_new(b) + 64;
   return up(tokens, 64);
 }
 
@@ -957,11 +960,11 @@ auto pick_many(int dim) {
 
 template <class E>
 hipError_t run(const AttendArgs& h, const AttendPlan& p, int dtype, hipStream_t s) {
-  const int64_t G = h.q_heads / h.c.heads, columns = h.b.max_new * G, nb = h.c.page / 16;
+  const int64_t G = h.q_heads / h.c.heads, columns = most_new(h.b) * G, nb = h.c.page / 16;
   const int64_t cap = h.b.cols * h.c.page, coltiles = up(columns, workgroup_columns(h.c.dim, dtype));
   const int64_t blocks = coltiles * p.splits * h.c.heads * h.b.B, joins = up(h.b.T * h.q_heads, 4);
-  // 32-bit numbering of columns (of T rows at most), blocks and workgroups
-  if (up(h.b.T * G, 16) * 16 + 1024 > 0x7fffffff || columns > 0x7fffffff - 1024 ||
+  // 32-bit numbering of columns, blocks and workgroups
+  if (up(h.b.T * G, 16) * 16 + 1024 > 0x7fffffff ||
       h.c.pages * h.c.heads * nb >= 0xffffffffll || (few(columns) ? h.b.B > 65535 || h.c.heads > 65535 : blocks > 0x7fffffff))
     return hipErrorInvalidConfiguration;
   Dev a{static_cast<const uint8_t*>(h.c.k), static_cast<const uint8_t*>(h.c.v), h.c.k_scale, h.c.v_scale,
@@ -1001,7 +1004,7 @@ hipError_t run(const AttendArgs& h, const AttendPlan& p, int dtype, hipStream_t 
 AttendPlan plan_attend(const c3c_kv_cache& c, const c3c_kv_batch& b, int dtype, int64_t q_heads,
                        int causal, int64_t window) {
   AttendPlan p;
-  const int64_t columns = b.max_new * (q_heads / c.heads), tiles = tiles_seen(b, c.page, window);
+  const int64_t columns = most_new(b) * (q_heads / c.heads), tiles = tiles_seen(b, c.page, window);
   const int64_t base = up(columns, few(columns) ? 16 : workgroup_columns(c.dim, dtype)) * c.heads * b.B;
   if (base == 0) return p;
   const int64_t cus = device_compute_units(), most = up(tiles, 4);

@@ -95,6 +95,18 @@ def test_append_with_a_loose_bound(bound):
     assert all(torch.equal(a, b) for a, b in zip(*results))
 
 
+@pytest.mark.parametrize("bound", [1 << 28, (1 << 31) - 1])
+@pytest.mark.parametrize("window", [0, 20])
+def test_attention_with_a_loose_bound(bound, window):
+    new, old = [40, 1, 7], [3, 200, 0]
+    q, results = ref.randn(1, 48, 4, 16).bfloat16(), []
+    for m in (40, bound):
+        cache, batch = cache_and_batch(new, old, m)
+        results.append(tokens.paged_attention(c3c.Context(), cache, batch, q, window=window))
+        assert tokens.paged_attention_workspace_bytes(cache, q, batch, window=window) < 1 << 24
+    assert torch.equal(*results)
+
+
 def test_attention_of_many_workgroups():
     """5000 sequences, one of 31000 new tokens: 5000 x 16 heads x 243 tiles of
     128 columns, 2^24 and more workgroups of 256 threads."""
