@@ -249,8 +249,14 @@ class Batch:
                              _check(lens, "lens", i32, (B,)), B, cols, 0, max_new, max_len)
 
     def _of(self, T):
-        self._d.T = T
-        return C.byref(self._d)
+        # a descriptor is never changed once a call may have it: threads with
+        # contexts of their own share a batch
+        d = self._d
+        if d.T != T:
+            d = _BatchDesc.from_buffer_copy(d)
+            d.T = T
+            self._d = d
+        return C.byref(d)
 
 
 def _heads(t, name, dtype, T, heads, dim):
