@@ -188,11 +188,14 @@ int c3c_kv_append(c3c_ctx* ctx, const c3c_kv_cache* cache, const c3c_kv_batch* b
  *   out[h]  = sum_j softmax_j(scale * q . k_j) v_j
  *   lse[h]  = log sum_j exp(scale * q . k_j)      (fp32 [T][q_heads], or NULL)
  * A query that sees no token has out 0 and lse -infinity.  What a query does
- * not see does not reach it, NaN included.  out: [T][q_heads][dim] contiguous,
+ * not see does not reach it, NaN included; blocks that no query of the call
+ * sees may hold anything, scales included.  out: [T][q_heads][dim] contiguous,
  * dtype.  Rows of q that belong to no sequence leave theirs undefined.
  * Probabilities enter the matrix cores as sums of 1 (bf16), 2 (f16) or 3 (f32)
- * f16 terms; a value loses precision where its block's scale is more than
- * 2^24 below the largest value scale that the query's neighbours see.
+ * f16 terms of 11 bits each, and are held to 2^-32 of the row's largest.  Where
+ * the scale of a value's block is 2^d, d > 15, below the largest value scale
+ * that the call's queries see of its sequence and head, its probability is
+ * held to 2^(d - 47) of the row's largest.
  *
  * Workspace (c3c_paged_attention_workspace_bytes): the partial results of a
  * call whose sequences are split because there are too few queries for the

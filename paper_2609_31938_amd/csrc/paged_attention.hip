@@ -22,8 +22,9 @@
 //   seen in a bf16 output.
 // V: codes in f16 times 2^k.  The accumulator is kept in units of 2^E, E the
 //   largest exponent of a value scale so far; k = e - E while that is -15 or
-//   more (codes then stay exact), and what is left of e - E goes to P.  Values
-//   lose precision from 2^30 below the largest value scale seen on.
+//   more (codes then stay exact), and what is left of e - E goes to P.  P's terms
+//   are spaced by 2^-24 at least: p is held to 2^-25 / 2^7 = 2^-32 beside its
+//   relative 11 bits a term, and to 2^(d - 47) where e is d > 15 below E.
 // attend_few: few queries (single tokens): the cache is read once, from HBM
 // straight into registers, and its traffic is the bound: 64 sequences of 1000
 // to 32768 tokens, 32 query and 8 key/value heads of 128, 473 us, 4.7 TB/s.
