@@ -200,9 +200,9 @@ int c3c_kv_append(c3c_ctx* ctx, const c3c_kv_cache* cache, const c3c_kv_batch* b
  * Workspace (c3c_paged_attention_workspace_bytes): the partial results of a
  * call whose sequences are split because there are too few queries for the
  * device; with a smaller workspace it runs unsplit.
- * EINVAL: as c3c_kv_append; heads not dividing q_heads; scale not finite and
- * positive; causal not 0 or 1; window < 0; the workspace overlapping a
- * tensor. */
+ * EINVAL: as c3c_kv_append; heads not dividing q_heads; T * q_heads / heads of
+ * 2^31 - 2048 or more; scale not finite and positive; causal not 0 or 1;
+ * window < 0; the workspace overlapping a tensor. */
 int c3c_paged_attention_workspace_bytes(const c3c_kv_cache* cache, const c3c_kv_batch* batch,
                                         int dtype, int64_t q_heads, int causal, int64_t window,
                                         size_t* bytes);

@@ -331,6 +331,8 @@ int c3c_paged_attention(c3c_ctx* ctx, const c3c_kv_cache* cache, const c3c_kv_ba
   const char* why = check_cache(cache, batch, dtype, q_heads, true);
   if (why) return fail(ctx, C3C_E_INVAL, why);
   if (q_heads % cache->heads) return fail(ctx, C3C_E_INVAL, "heads must divide q_heads");
+  if (batch->T * (q_heads / cache->heads) >= kBig - 2048)
+    return fail(ctx, C3C_E_INVAL, "T * q_heads / heads must be below 2^31 - 2048");
   if (!std::isfinite(scale) || scale <= 0.f) return fail(ctx, C3C_E_INVAL, "scale must be finite and positive");
   if (causal != 0 && causal != 1) return fail(ctx, C3C_E_INVAL, "causal must be 0 or 1");
   if (window < 0 || window >= kBig) return fail(ctx, C3C_E_INVAL, "window must be >= 0 and below 2^31");

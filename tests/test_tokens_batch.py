@@ -1,8 +1,17 @@
 """A Batch shared by calls of different sizes that overlap in time (threads
-with a context each): every call keeps the description that it was given."""
+with a context each): every call keeps the description that it was given.
+And calls of more queries than their numbering holds (fake device addresses;
+skipped where a GPU is present)."""
+import ctypes as C
 import threading
 
-from paper_2609_31938_amd import tokens
+import pytest
+import torch
+
+from paper_2609_31938_amd import c3c, tokens
+
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="fake-pointer argument tests run on CPU-only hosts")
+lib = c3c.lib
 
 
 def shared():
@@ -38,3 +47,13 @@ def test_threads_that_share_a_batch():
     for t in threads:
         t.join()
     assert not wrong
+
+
+@no_gpu
+def test_columns_past_32_bits_are_refused():
+    ctx = c3c.Context()
+    for T, qh in (((1 << 30), 4), ((1 << 31) - 1, 2), ((1 << 29) - 512, 8)):
+        b = tokens._BatchDesc(1 << 20, 2 << 20, 3 << 20, 1, 1, T, 1, 1)
+        c = tokens._CacheDesc(4 << 20, 5 << 20, 6 << 20, 7 << 20, 1, 2, 16, 16)
+        st = lib.c3c_paged_attention(ctx._h, C.byref(c), C.byref(b), 1, qh, 1 << 40, qh * 16, 0.1, 1, 0, 1 << 50, None, None)
+        assert st == c3c.E_INVAL and "2^31" in ctx.last_error, (T, qh, ctx.last_error)
