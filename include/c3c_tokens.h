@@ -66,9 +66,10 @@ int c3c_quantize_rows(c3c_ctx* ctx, int64_t T, int64_t C, int64_t ld_x, int dtyp
  * Workspace (c3c_linear_i8_workspace_bytes, 0 where none is used): the
  * quantised rows of float activations, copies of rows that are no multiple of
  * 16 bytes, and the partial sums of a product that is split along K because
- * its tiles are too few for the device.  A call whose context has less than
- * the bytes that it needs for the quantised rows is EINVAL; with those but not
- * the others it runs without copies or unsplit.  Results are the same bits
+ * its tiles are too few for the device.  A call of float activations whose
+ * context has less than the quantised rows' bytes is EINVAL, also where few
+ * tokens are quantised without them; with those but not the others it runs
+ * without copies or unsplit.  Results are the same bits
  * either way (integer sums).
  * EINVAL: NULL ctx, desc or a NULL tensor of nonzero size; M < 0, N < 1,
  * K < 1 or > 131071, ld_x < K; unknown dtypes; x_scale given with a float x
@@ -202,7 +203,9 @@ int c3c_kv_append(c3c_ctx* ctx, const c3c_kv_cache* cache, const c3c_kv_batch* b
  * device; with a smaller workspace it runs unsplit.
  * EINVAL: as c3c_kv_append; heads not dividing q_heads; T * q_heads / heads of
  * 2^31 - 2048 or more; scale not finite and positive; causal not 0 or 1;
- * window < 0; the workspace overlapping a tensor. */
+ * window < 0; the workspace overlapping a tensor.  EDEVICE also: 2^31 or more
+ * workgroups, of which each sequence and key/value head has one for every 64 or
+ * 128 of the most queries that any sequence may have. */
 int c3c_paged_attention_workspace_bytes(const c3c_kv_cache* cache, const c3c_kv_batch* batch,
                                         int dtype, int64_t q_heads, int causal, int64_t window,
                                         size_t* bytes);

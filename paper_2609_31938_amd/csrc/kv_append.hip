@@ -11,11 +11,12 @@
 // writes the block, so the scale needs no atomics, and an append of many tokens
 // and many appends of one give the same scales.  V's 4 x 4 (lane groups x
 // pairs of channels) dwords of 4 tokens are transposed between the lane groups,
-// so that a lane stores whole 16-byte rows.  Everything that an address needs
-// is read before the values are worked on: a single token's time is a chain of
-// memory latencies (64 tokens of 64 sequences, 32 + 8 + 8 heads of 128: 7 us).
-// Frames are bound by memory traffic: 4 x 1560 tokens, 3 x 12 heads of 128 in
-// bf16, 26 us, 3.8 TB/s.
+// so that a lane stores whole 16-byte rows.  The page, a lane's
+// four tokens, the block's old scale and the tokens' angles are read one after
+// another: each load stands behind a condition and is waited for there.  A
+// single token's time is that chain of memory latencies (64 tokens of 64
+// sequences, 32 + 8 + 8 heads of 128: 7 us); frames move 3.8 TB/s (4 x 1560
+// tokens, 3 x 12 heads of 128 in bf16: 26 us).
 //
 // The products and sums of a rotation are rounded one by one (no fused
 // multiply-add), so that a code is decided by the formula's own fp32 value.

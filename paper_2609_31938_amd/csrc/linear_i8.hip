@@ -9,11 +9,13 @@
 //   registers (no tile of them is used twice), by 4 waves that share 16 rows
 //   and take every fourth 128-byte piece of K, 8 of them in flight; their sums
 //   meet in LDS.  Up to 4 tokens of floats are quantised in the same kernel, by
-//   every workgroup for itself, while its first weights are on their way.
+//   every workgroup for itself, which saves a launch and its wait.  The first
+//   weights are asked for before the tokens; loads return in order, so the
+//   quantisation waits for them.
 // tiled: BM x BN tiles, stages of 64 or 128 bytes of K in an LDS ring, the
 //   fragments of the next 64 bytes read between the products of these.  The
-//   largest tile takes two stages of 128 bytes (whole cache lines; 794 us for
-//   32760 x 5120 x 5120 quantised normal values, 2.16 PFLOP/s) over four of 64
+//   largest tile takes two stages of 128 bytes (whole cache lines; 790 us for
+//   32760 x 5120 x 5120 quantised normal values, 2.17 POP/s) over four of 64
 //   (865 us).  What bounds it is the way to LDS: the loads alone take 710 us,
 //   the products alone 620 (at the clock that power leaves them; 3.5 PFLOP/s
 //   with random operands in registers).  With 16-byte rows the stages are loaded
@@ -244,8 +246,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
 
   // tiles in an order that keeps each of the 8 L2 caches on neighbouring
   // ones: workgroup b runs on cache b % 8, which gets a run of consecutive
-  // tiles, walked in columns of 6 tiles of tokens (32760 x 5120 x 5120: 794 us;
-  // columns of 4 809, of 8 857)
+  // tiles, walked in columns of 6 tiles of tokens (32760 x 5120 x 5120, in
+  // one sitting: 794 us, columns of 4 809, of 8 857; other shapes not tried)
   const int total = a.tiles_m * a.tiles_n;
   int b = static_cast<int>(a.first) + blockIdx.x;
   const int split = b / total;

@@ -13,9 +13,11 @@
 //
 // A row belongs to one wave (at most 128 16-byte vectors: no barrier) or to
 // one workgroup; rows beyond 4096 vectors are read again in every pass.
-// 32760 x 5120 in bf16 with post, gate and pre: 353 us, 3.8 TB/s.  The gains
-// come from L2 for every row and are more bytes than the row: with constants in
-// their place 263 us.  Slower: two rows a workgroup (363), gains kept over the
+// 32760 x 5120 in bf16 with post, gate and pre: 356 us, 3.8 TB/s.  A row's loads
+// follow one another: each stands behind the condition on the row's end, whose
+// branch also widens it, and so is waited for before the next is issued.  The
+// gains come from L2 for every row and are more bytes than the row; with
+// constants in their place, and so without their waits, 263 us.  Slower: two rows a workgroup (363), gains kept over the
 // rows of workgroups that stay (441 to 491, fewer rows in flight), a row a wave
 // (796), two vectors a thread (358).
 #include <math.h>
@@ -94,7 +96,7 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void norm_gate_regs(NormArgs a) 
   const S* yp = a.y ? static_cast<const S*>(a.y) + t * a.C : nullptr;
   const S* gp = a.gate ? static_cast<const S*>(a.gate) + t / a.rows * a.C : nullptr;
   float h[NV][V], y[NV][V], g[NV][V], p[NV][V];
-  // every load of the row before the first sum
+  // the row's loads, before the first sum
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (lane + i * per) * V, m = C - c;

@@ -27,10 +27,10 @@
 //   relative 11 bits a term, and to 2^(d - 47) where e is d > 15 below E.
 // attend_few: few queries (single tokens): the cache is read once, from HBM
 // straight into registers, and its traffic is the bound: 64 sequences of 1000
-// to 32768 tokens, 32 query and 8 key/value heads of 128, 473 us, 4.7 TB/s.
+// to 32768 tokens, 32 query and 8 key/value heads of 128, 483 us, 4.6 TB/s.
 // attend_many: chunks of queries share tiles in LDS; exponentials, conversions
 // and products of two waves a SIMD are the bound: 8192 causal queries of the
-// same heads 591 us, 930 TFLOP/s.
+// same heads 599 us, 918 TFLOP/s.
 #include <math.h>
 
 #include "token_dev.h"
@@ -354,8 +354,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_few(Dev a) {
   int unit = -126;           // E
 
   const int32_t* pages = a.table + static_cast<int64_t>(b) * a.cols;
-  // A tile's codes and scales are loaded while the tile before is worked on,
-  // where the registers hold both.
+  // A tile's codes and scales are asked for before the tile before is worked on,
+  // where the registers hold both.  (The page read behind them, under a condition,
+  // waits for them: what overlaps is the work of the compute unit's other waves.)
   constexpr bool AHEAD = DP <= 128;
   struct Tile {
     uint32_t vb;  // block g, or kNone
@@ -529,7 +530,7 @@ __device__ inline void lds_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(
 // WHOLE: pages are multiples of 64 tokens, so that a tile lies in one page and
 // its addresses are scalars; otherwise the vector units find blocks of 16
 // tokens.  FULL: and no channel is padding, so that no load has a condition
-// (32 query heads of 128, 8192 causal tokens: 591 us, without FULL 652).
+// (32 query heads of 128, 8192 causal tokens: a tenth more time without FULL).
 template <class E, int DP, int CT, bool WHOLE, bool FULL>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attend_many(Dev a) {
   typedef Form<E> F;
