@@ -9,6 +9,11 @@
 
 namespace c3c {
 
+// Whether a launch asks for more than it gets: a dimension of a grid has fewer
+// than 2^32 threads, and one of more is cut to their number modulo 2^32 without
+// an error.
+inline bool too_many(int64_t workgroups, int64_t threads) { return workgroups > 0xffffffffll / threads; }
+
 // Geometry of one validated call (Sec. 4.2: |Z|, p_l, T_o; spatial analogue).
 struct Geo {
   c3c_conv_desc d;

@@ -786,7 +786,7 @@ hipError_t run(const Geo& g, Args a, const Plan& p, bool aligned, int fused, hip
     return hipSuccess;
   }
   if (blocks == 0) return hipSuccess;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (too_many(blocks, 64 * WAVES_CO * WAVES_PX)) return hipErrorInvalidConfiguration;
   a.nblocks = static_cast<int>(blocks);
   const dim3 grid(static_cast<unsigned>(blocks)), block(64 * WAVES_CO * WAVES_PX);
   const bool split = a.splits > 1;

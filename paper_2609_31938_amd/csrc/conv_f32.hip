@@ -388,7 +388,7 @@ hipError_t launch_fast_f32(const Geo& g, const void* x, const void* cache, const
     return hipSuccess;
   }
   if (blocks == 0) return hipSuccess;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (too_many(blocks, 256)) return hipErrorInvalidConfiguration;
   a.nblocks = static_cast<int>(blocks);
   // Waves per pixel block: a launch that leaves a compute unit one or two
   // workgroups splits their channel pairs over two waves, so that a SIMD has

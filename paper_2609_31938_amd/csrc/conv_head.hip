@@ -535,7 +535,7 @@ hipError_t launch_head(const Geo& g, const void* x, const void* cache, const voi
     return hipSuccess;
   }
   if (blocks == 0) return hipSuccess;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (too_many(blocks, 256)) return hipErrorInvalidConfiguration;
   a.nblocks = static_cast<int>(blocks);
   const int nf = static_cast<int>((9 * d.Co + 15) / 16);
   const bool nb4 = head_table_entries(d) <= wtab_entries(4);

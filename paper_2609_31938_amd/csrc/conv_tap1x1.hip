@@ -796,7 +796,7 @@ hipError_t launch_tap1x1(const Geo& g, const void* x, const void* cache, const v
   }
   if (cache_written) *cache_written = a.write_cache != 0;
   if (blocks == 0) return hipSuccess;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (too_many(blocks, 256)) return hipErrorInvalidConfiguration;
   a.nblocks = static_cast<int>(blocks);
   const dim3 grid(static_cast<unsigned>(blocks)), block(256);
   if (chunk_form)

@@ -520,7 +520,7 @@ bool pick(const Geo& g, bool al, FmArgs* a, int* cfg) {
       blocks = nb;
     }
   }
-  if (blocks > 0x7fffffff || (FM_BCO[*cfg] == 16 && direct_pays(g, Ktot, blocks, al))) return false;
+  if (too_many(blocks, 256) || (FM_BCO[*cfg] == 16 && direct_pays(g, Ktot, blocks, al))) return false;
   a->nblocks = static_cast<int>(blocks);
   a->groups = static_cast<int>(d.groups);
   a->cig = static_cast<int>(cig);

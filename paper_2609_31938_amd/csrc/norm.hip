@@ -211,7 +211,7 @@ hipError_t launch_rms_prologue(const Geo& g, const void* x, const float* gamma, 
   if (d.N * d.Ci * d.T * hw == 0) return hipSuccess;
   const int64_t tiles = (hw + NPX - 1) / NPX;
   const int64_t blocks = d.N * d.T * tiles;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (too_many(blocks, 256)) return hipErrorInvalidConfiguration;
   const bool al = hw % 8 == 0 && aligned16(x) && aligned16(u);
   auto k = al ? pick_kernel<true>(d.Ci) : pick_kernel<false>(d.Ci);
   hipLaunchKernelGGL(k, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s,

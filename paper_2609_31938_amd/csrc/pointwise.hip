@@ -777,7 +777,7 @@ hipError_t launch_pw(const Geo& g, PwArgs a, bool f16, bool al, hipStream_t s, i
     return hipSuccess;
   }
   if (blocks == 0) return hipSuccess;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (too_many(blocks, PW_NT)) return hipErrorInvalidConfiguration;
   int ntap = 0;
   for (int64_t t = 0; t < g.To; ++t) {
     int nt = 0;
