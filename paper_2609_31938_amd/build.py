@@ -20,7 +20,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["c3c_host.cpp", "fast_conv.hip", "conv_bf16.hip", "conv_f32.hip", "conv_tap1x1.hip", "conv_head.hip",
            "fallback.hip", "fallback_mfma.hip", "pointwise.hip", "mfma_probe.hip", "noalloc.hip", "norm.hip",
-           "tokens_host.cpp", "linear_i8.hip", "kv_append.hip", "paged_attention.hip", "norm_gate.hip"]
+           "tokens_host.cpp", "linear_i8.hip", "kv_append.hip", "paged_attention.hip", "norm_gate.hip",
+           "linear_attention.hip"]
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-I", INC, "-I", CSRC]

@@ -1,0 +1,706 @@
+// Linear attention with a decay for each head:
+//   S <- exp(g_t) S + k_t v_t^T,   out_t = scale q_t S        (S: dim_k x dim_v)
+//
+// By chunks of C tokens, with G_i the sum of g over the chunk's tokens up to i:
+//   out_i = scale (exp(G_i) q_i S + sum_{j <= i} exp(G_i - G_j) (q_i . k_j) v_j)
+//   S    <- exp(G_C) S + sum_j k_j (exp(G_C - G_j) v_j)^T
+// Four products for the matrix cores.  Every weight is the exponential of a
+// difference that is at most 0 for decays, so nothing overflows however fast a
+// head forgets; the sums G are formed in 64 bits and kept as two floats, since
+// they may be large (a token that resets the state) next to their differences.
+//
+// chunks: a workgroup of 4 waves takes one head and up to 128 columns of S, of
+//   which every wave holds its quarter in the matrix cores' accumulators, all
+//   dim_k rows of it: the layout of an accumulator is that of an operand whose
+//   rows are taken in another order, so S goes into the first product without
+//   passing through LDS, and no two waves share a column of out.  What the waves
+//   share is q, k and the weighted products P of queries and keys, in LDS.
+// parts: few heads and sequences leave compute units idle.  Their sequences
+//   are split into parts of whole chunks: one launch forms each part's own
+//   state, one joins them in order, one forms the outputs of all parts.
+// tokens: few new tokens (single ones, drafted ones) take the recurrence
+//   as it stands, S in registers: it is bound by reading and writing S.
+#include "token_dev.h"
+#include "tokens_internal.h"
+
+namespace c3c {
+namespace {
+
+typedef short tok_i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) tok_i16x4 lds_i16x4;
+
+constexpr double kLog2e = 1.4426950408889634;
+constexpr float kForget = -110.f;  // exp of it is 0 in fp32
+
+struct Args {
+  float* state;
+  const int32_t *cu, *len, *slot;
+  const void *q, *k, *v;
+  const float* decay;
+  void* out;
+  float* part;    // [B][parts][heads][dim_k][dim_v], then a factor for each
+  float* factor;  // [B][parts][heads]
+  int64_t slots, B, T, ld_q, ld_k, ld_v, ld_decay;
+  int64_t part_tokens;  // of every part but the last
+  int64_t first;        // workgroup of this launch
+  int64_t groups;       // workgroups of the call
+  int heads, qk_heads, dim_k, dim_v, parts, slices;
+  float scale;
+};
+
+// The new tokens of a sequence.
+struct Seq {
+  int64_t first, n;
+  int64_t slot;  // -1: none
+  bool fresh;    // begins at zero
+};
+__device__ inline Seq sequence(const Args& a, int64_t b) {
+  Seq s;
+  const int64_t c0 = a.cu[b], c1 = a.cu[b + 1];
+  s.first = c0 < 0 ? 0 : c0 < a.T ? c0 : a.T;
+  const int64_t end = c1 < s.first ? s.first : c1 < a.T ? c1 : a.T;
+  s.n = end - s.first;
+  const int64_t slot = a.slot ? a.slot[b] : b;
+  s.slot = slot >= 0 && slot < a.slots ? slot : -1;
+  s.fresh = s.slot < 0 || a.len[b] <= c1 - c0;
+  return s;
+}
+// parts of it that hold tokens
+__device__ inline int live_parts(const Args& a, int64_t n) {
+  const int64_t p = (n + a.part_tokens - 1) / a.part_tokens;
+  return static_cast<int>(p < 1 ? 1 : p < a.parts ? p : a.parts);
+}
+
+__device__ inline float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <class E>
+struct Terms;  // bf16 terms that hold an input exactly
+template <>
+struct Terms<ElemBf16> {
+  static constexpr int IN = 1, OUT = 2;
+};
+template <>
+struct Terms<ElemF16> {
+  static constexpr int IN = 2, OUT = 2;
+};
+template <>
+struct Terms<ElemF32> {
+  static constexpr int IN = 3, OUT = 3;
+};
+constexpr int kStateTerms = 3;  // of a weighted value: the state is an output in fp32
+
+// Two values as NT terms of bf16 each, the next the rounding error of those
+// before it: 2 terms hold 2^-18 of a value, 3 all of a float.
+template <int NT>
+__device__ inline void split2(float x, float y, uint32_t (&w)[NT]) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    w[t] = __builtin_bit_cast(uint32_t, __builtin_convertvector((tok_f32x2{x, y}), tok_bf16x2));
+    if (t + 1 < NT) {
+      x -= __uint_as_float(w[t] << 16);
+      y -= __uint_as_float(w[t] & 0xffff0000u);
+    }
+  }
+}
+
+template <int NT>
+__device__ inline void split8(const float (&f)[8], tok_bf16x8 (&o)[NT]) {
+  tok_u32x4 w[NT];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t p[NT];
+    split2<NT>(f[2 * i], f[2 * i + 1], p);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) w[t][i] = p[t];
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) o[t] = __builtin_bit_cast(tok_bf16x8, w[t]);
+}
+
+// acc += a b over the pairs of terms whose product exceeds 2^-9(LAST + 1)
+template <int LAST, int NA, int NB>
+__device__ inline void mfma_terms(const tok_bf16x8 (&a)[NA], const tok_bf16x8 (&b)[NB], tok_f32x4& acc) {
+#pragma unroll
+  for (int i = 0; i < NA; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+      if (i + j <= LAST) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[i], b[j], acc, 0, 0, 0);
+}
+
+// Everything that this wave has stored to LDS has landed before the others
+// pass.  (A __syncthreads() at a loop's head has been compiled without the wait
+// for the stores at the loop's end.)
+__device__ inline void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// The operand of 8 tokens (rows from t0 + 8 g on) by the column of this lane:
+// ds_read_b64_tr_b16 gives lane i of 16 element i % 4 of what lanes 4 e + i / 4
+// address, e = 0 .. 3.  at: where this lane reads, in the first row's place.
+__device__ inline tok_bf16x8 column8(const unsigned char* at, int pitch) {
+  const tok_i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
+  const tok_i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 4 * pitch));
+  return __builtin_bit_cast(tok_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// E: input type.  DK: rows of S (dim_k, filled up with zeros).  DVS: columns of
+// this workgroup.  C: tokens of a chunk.  STATES: only the state of a part.
+template <class E, int DK, int DVS, int C, bool STATES>
+struct Chunk {
+  static constexpr int NI = Terms<E>::IN, NO = Terms<E>::OUT;
+  static constexpr int QK_PITCH = DK * 2 + 16, V_PITCH = DVS * 2 + 16, P_PITCH = C * 2 + 16;
+  static constexpr int QK_BYTES = NI * C * QK_PITCH, V_BYTES = NI * C * V_PITCH;
+  static constexpr int P_BYTES = STATES ? 0 : NO * C * P_PITCH;
+  static constexpr int K_AT = STATES ? 0 : QK_BYTES, V_AT = K_AT + QK_BYTES, P_AT = V_AT + V_BYTES;
+  static constexpr int W_AT = P_AT + P_BYTES;  // weights: 4 floats a token, and the chunk's
+  static constexpr int BYTES = W_AT + 4 * C * 4 + 16;
+  static constexpr int EVEC = E::VEC;
+  static constexpr int KP = C * DK / EVEC / 256, VP = C * DVS / EVEC / 256;  // 16-byte pieces a thread
+  static constexpr int CT = DVS / 64;                                         // column tiles of 16 of a wave
+};
+
+template <class E, int DK, int DVS, int C, bool STATES>
+__global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1024 ? 2 : 1)) void chunks(Args a) {
+  typedef Chunk<E, DK, DVS, C, STATES> K;
+  typedef typename E::store store;
+  constexpr int NI = K::NI, NO = K::NO, CT = K::CT, VEC = E::VEC;
+  constexpr int LAST = NO - 1;
+  constexpr int KS = DK / 32, JS = C / 32, RT = C / 16;
+  __shared__ __align__(16) unsigned char lds[K::BYTES];
+  float* const g_hi = reinterpret_cast<float*>(lds + K::W_AT);  // G in units of log 2: its float and the rest
+  float* const g_lo = g_hi + C;
+  float* const w_q = g_lo + C;  // exp(G_i)
+  float* const w_k = w_q + C;   // exp(G_C - G_i)
+  float* const w_all = w_k + C;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r = lane & 15, g = lane >> 4;
+
+  // workgroup -> (sequence, part, head) and slice: the slices of a head, which
+  // read the same q and k, run on the same one of the 8 L2 caches
+  const int64_t id = a.first + blockIdx.x;
+  const int64_t unit = id / (8 * a.slices) * 8 + id % 8;
+  const int slice = static_cast<int>(id / 8 % a.slices);
+  if (unit >= a.groups) return;
+  const int h = static_cast<int>(unit % a.heads);
+  const int runs = STATES ? a.parts - 1 : a.parts;
+  const int part = static_cast<int>(unit / a.heads % runs);
+  const int64_t b = unit / a.heads / runs;
+  const Seq seq = sequence(a, b);
+  const int live = live_parts(a, seq.n);
+  if (seq.n == 0 || part >= (STATES ? live - 1 : live)) return;
+  const int64_t t0 = seq.first + part * a.part_tokens;
+  const int64_t end = part + 1 < live ? t0 + a.part_tokens : seq.first + seq.n;
+  const int hk = h / (a.heads / a.qk_heads);
+  const int c0 = slice * DVS;  // first column
+  const store* qp = static_cast<const store*>(a.q) + static_cast<int64_t>(hk) * a.dim_k;
+  const store* kp = static_cast<const store*>(a.k) + static_cast<int64_t>(hk) * a.dim_k;
+  const store* vp = static_cast<const store*>(a.v) + static_cast<int64_t>(h) * a.dim_v + c0;
+  const int cols = a.dim_v - c0 < DVS ? a.dim_v - c0 : DVS;
+
+  // ---- a chunk's inputs: asked for one chunk ahead, in registers until their place in LDS is free
+  struct Piece {
+    store v[VEC];
+  };
+  Piece rq[STATES ? 1 : K::KP], rk[K::KP], rv[K::VP];
+  float rg = 0.f;
+  auto ask = [&](int64_t t) __attribute__((always_inline)) {
+    auto get = [&](const store* p, int64_t ld, int i, int per, int width) __attribute__((always_inline)) {
+      const int at = i * 256 + tid, row = at / per, col = at % per * VEC;
+      Piece x;
+      if (t + row < end && col < width) {
+        __builtin_memcpy(x.v, p + (t + row) * ld + col, 16);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x.v[e] = store(0);
+      }
+      return x;
+    };
+    if constexpr (!STATES) {
+#pragma unroll
+      for (int i = 0; i < K::KP; ++i) rq[i] = get(qp, a.ld_q, i, DK / VEC, a.dim_k);
+    }
+#pragma unroll
+    for (int i = 0; i < K::KP; ++i) rk[i] = get(kp, a.ld_k, i, DK / VEC, a.dim_k);
+#pragma unroll
+    for (int i = 0; i < K::VP; ++i) rv[i] = get(vp, a.ld_v, i, DVS / VEC, cols);
+    if (wave == 0) rg = lane < C && t + lane < end ? a.decay[(t + lane) * a.ld_decay + h] : 0.f;
+  };
+  auto put = [&](const Piece& x, int at, int plane, int pitch, int i, int per) __attribute__((always_inline)) {
+    const int p = i * 256 + tid, row = p / per, col = p % per * VEC;
+    unsigned char* to = lds + at + row * pitch + col * 2;
+    if constexpr (NI == 1) {
+      __builtin_memcpy(to, x.v, 16);
+    } else {
+      uint32_t w[NI][VEC / 2];
+#pragma unroll
+      for (int e = 0; e < VEC; e += 2) {
+        uint32_t t[NI];
+        split2<NI>(E::widen(x.v[e]), E::widen(x.v[e + 1]), t);
+#pragma unroll
+        for (int n = 0; n < NI; ++n) w[n][e / 2] = t[n];
+      }
+#pragma unroll
+      for (int n = 0; n < NI; ++n) __builtin_memcpy(__builtin_assume_aligned(to + n * plane, VEC * 2), w[n], VEC * 2);
+    }
+  };
+  auto place = [&]() __attribute__((always_inline)) {
+    if constexpr (!STATES) {
+#pragma unroll
+      for (int i = 0; i < K::KP; ++i) put(rq[i], 0, C * K::QK_PITCH, K::QK_PITCH, i, DK / VEC);
+    }
+#pragma unroll
+    for (int i = 0; i < K::KP; ++i) put(rk[i], K::K_AT, C * K::QK_PITCH, K::QK_PITCH, i, DK / VEC);
+#pragma unroll
+    for (int i = 0; i < K::VP; ++i) put(rv[i], K::V_AT, C * K::V_PITCH, K::V_PITCH, i, DVS / VEC);
+    if (wave == 0) {
+      double s = static_cast<double>(rg < kForget ? kForget : rg) * kLog2e;
+#pragma unroll
+      for (int o = 1; o < C; o <<= 1) {
+        const double up = __shfl_up(s, o);
+        if (lane >= o) s += up;
+      }
+      const double all = __shfl(s, C - 1);
+      if (lane < C) {
+        const float hi = static_cast<float>(s);
+        g_hi[lane] = hi;
+        // a sum that is infinite or NaN has no rest
+        g_lo[lane] = fabsf(hi) < __builtin_inff() ? static_cast<float>(s - static_cast<double>(hi)) : 0.f;
+        w_q[lane] = exp2_of(hi);
+        w_k[lane] = exp2_of(static_cast<float>(all - s));
+        if (lane == 0) *w_all = exp2_of(static_cast<float>(all));
+      }
+    }
+  };
+
+  // ---- S: tile [s][t] of column tile c holds rows 32 s + 8 g + 4 t + e of column 16 c + r
+  const int wc = wave * 16 * CT;  // this wave's first column
+  tok_f32x4 S[KS][2][CT];
+  float factor = 1.f;
+  const int64_t head_size = static_cast<int64_t>(a.dim_k) * a.dim_v;
+  const float* from = STATES                ? nullptr
+                      : a.parts > 1         ? a.part + ((b * a.parts + part) * a.heads + h) * head_size
+                      : seq.fresh           ? nullptr
+                                            : a.state + (seq.slot * a.heads + h) * head_size;
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = 32 * s + 8 * g + 4 * t + e, col = c0 + wc + 16 * c + r;
+          S[s][t][c][e] = from && row < a.dim_k && col < a.dim_v ? from[static_cast<int64_t>(row) * a.dim_v + col] : 0.f;
+        }
+
+  ask(t0);
+  if constexpr (!STATES) {
+    // P above the diagonal, within the 32 keys of a step: zeros that stay
+    for (int i = tid; i < NO * (RT / 2) * 16 * 4; i += 256) {
+      const int piece = i & 3, row = i / 4 % 16, tile = i / 64 % (RT / 2), n = i / 64 / (RT / 2);
+      *reinterpret_cast<uint64_t*>(lds + K::P_AT + (n * C + tile * 32 + row) * K::P_PITCH + (tile * 32 + 16) * 2 + piece * 8) = 0;
+    }
+  }
+  for (int64_t t = t0; t < end; t += C) {
+    place();
+    meet();
+    if (t + C < end) ask(t + C);
+
+    tok_f32x4 O[STATES ? 1 : RT][CT];  // of token 16 rt + r: columns 16 c + 4 g + e
+    if constexpr (!STATES) {
+      // P: tiles of 16 keys x 16 queries on and below the diagonal, in turn
+      constexpr int JOBS = RT * (RT + 1) / 2;
+#pragma unroll
+      for (int j0 = 0; j0 < JOBS; j0 += 4) {
+        const int j = j0 + wave;
+        if (j < JOBS) {
+          const int qt = j < 1 ? 0 : j < 3 ? 1 : j < 6 ? 2 : 3, kt = j - qt * (qt + 1) / 2;
+          tok_f32x4 p = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int s = 0; s < KS; ++s) {
+            tok_bf16x8 fq[NI], fk[NI];
+#pragma unroll
+            for (int n = 0; n < NI; ++n) {
+              const int at = n * C * K::QK_PITCH + r * K::QK_PITCH + s * 64 + g * 16;
+              fq[n] = *reinterpret_cast<const tok_bf16x8*>(lds + at + qt * 16 * K::QK_PITCH);
+              fk[n] = *reinterpret_cast<const tok_bf16x8*>(lds + K::K_AT + at + kt * 16 * K::QK_PITCH);
+            }
+            mfma_terms<LAST, NI, NI>(fk, fq, p);
+          }
+          const int i = qt * 16 + r, key = kt * 16 + 4 * g;
+          const tok_f32x4 hi = *reinterpret_cast<const tok_f32x4*>(g_hi + key), lo = *reinterpret_cast<const tok_f32x4*>(g_lo + key);
+          const float ih = g_hi[i], il = g_lo[i];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[e] = key + e <= i ? p[e] * exp2_of((ih - hi[e]) + (il - lo[e])) : 0.f;
+          uint32_t w0[NO], w1[NO];
+          split2<NO>(p[0], p[1], w0);
+          split2<NO>(p[2], p[3], w1);
+#pragma unroll
+          for (int n = 0; n < NO; ++n)
+            *reinterpret_cast<tok_u32x2*>(lds + K::P_AT + (n * C + i) * K::P_PITCH + key * 2) = tok_u32x2{w0[n], w1[n]};
+        }
+      }
+      // exp(G_i) q_i S
+#pragma unroll
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int c = 0; c < CT; ++c) O[i][c] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        tok_bf16x8 fs[CT][NO];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = S[s][e >> 2][c][e & 3];
+          split8<NO>(f, fs[c]);
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          tok_bf16x8 fq[NI];
+#pragma unroll
+          for (int n = 0; n < NI; ++n)
+            fq[n] = *reinterpret_cast<const tok_bf16x8*>(lds + (n * C + i * 16 + r) * K::QK_PITCH + s * 64 + g * 16);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) mfma_terms<LAST, NO, NI>(fs[c], fq, O[i][c]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const float w = w_q[i * 16 + r];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) O[i][c] *= w;
+      }
+      meet();
+    }
+
+    // P v, and the state
+    {
+      const float all = *w_all;
+      factor *= all;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int c = 0; c < CT; ++c) S[s][u][c] *= all;
+    }
+#pragma unroll
+    for (int j = 0; j < JS; ++j) {
+      const int row = 32 * j + 8 * g;
+      tok_bf16x8 fv[CT][NI], fw[CT][kStateTerms];
+      float weight[8];
+      *reinterpret_cast<tok_f32x4*>(weight) = *reinterpret_cast<const tok_f32x4*>(w_k + row);
+      *reinterpret_cast<tok_f32x4*>(weight + 4) = *reinterpret_cast<const tok_f32x4*>(w_k + row + 4);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        float f[8], zero = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = 0.f;
+#pragma unroll
+        for (int n = NI - 1; n >= 0; --n) {
+          fv[c][n] = column8(lds + K::V_AT + (n * C + row + (r >> 2)) * K::V_PITCH + (wc + 16 * c + 4 * (r & 3)) * 2, K::V_PITCH);
+          const tok_u32x4 u = __builtin_bit_cast(tok_u32x4, fv[c][n]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            f[2 * e] += __uint_as_float(u[e] << 16);
+            f[2 * e + 1] += __uint_as_float(u[e] & 0xffff0000u);
+          }
+        }
+        if constexpr (!STATES) {
+          // a value that is not finite must not meet the zeros of the tokens
+          // before it: it is left out, and makes NaN of those from its own on
+#pragma unroll
+          for (int e = 0; e < 8; ++e) zero = __builtin_fmaf(f[e], 0.f, zero);
+          if (__builtin_expect(__builtin_amdgcn_ballot_w64(zero != zero) != 0, 0)) {
+            int bad = C;
+            tok_u32x4 m;
+#pragma unroll
+            for (int e = 7; e >= 0; --e) {
+              const bool ok = fabsf(f[e]) < __builtin_inff();
+              if (!ok) bad = row + e;
+              const uint32_t half = ok ? 0xffffu : 0u;
+              m[e >> 1] = e & 1 ? half << 16 : m[e >> 1] | half;
+            }
+#pragma unroll
+            for (int n = 0; n < NI; ++n) fv[c][n] = __builtin_bit_cast(tok_bf16x8, __builtin_bit_cast(tok_u32x4, fv[c][n]) & m);
+#pragma unroll
+            for (int o = 16; o < 64; o <<= 1) {
+              const int other = __shfl_xor(bad, o);
+              bad = other < bad ? other : bad;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int from_here = __shfl(bad, 4 * g + e);  // of column 16 c + 4 g + e
+#pragma unroll
+              for (int i = 0; i < RT; ++i)
+                if (i * 16 + r >= from_here) O[i][c][e] = __builtin_nanf("");
+            }
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= weight[e];
+        split8<kStateTerms>(f, fw[c]);
+      }
+      if constexpr (!STATES) {
+#pragma unroll
+        for (int i = 2 * j; i < RT; ++i) {
+          tok_bf16x8 fp[NO];
+#pragma unroll
+          for (int n = 0; n < NO; ++n)
+            fp[n] = *reinterpret_cast<const tok_bf16x8*>(lds + K::P_AT + (n * C + i * 16 + r) * K::P_PITCH + j * 64 + g * 16);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) mfma_terms<LAST, NI, NO>(fv[c], fp, O[i][c]);
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          tok_bf16x8 fk[NI];
+#pragma unroll
+          for (int n = 0; n < NI; ++n)
+            fk[n] = column8(lds + K::K_AT + (n * C + row + (r >> 2)) * K::QK_PITCH + (32 * s + 8 * (r & 3) + 4 * u) * 2, K::QK_PITCH);
+#pragma unroll
+          for (int c = 0; c < CT; ++c) mfma_terms<kStateTerms - 1, NI, kStateTerms>(fk, fw[c], S[s][u][c]);
+        }
+    }
+    if constexpr (!STATES) {
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        const int64_t row = t + i * 16 + r;
+        if (row >= end) continue;
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          const int col = wc + 16 * c + 4 * g;
+          if (col >= cols) continue;
+          store o[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = E::narrow(O[i][c][e] * a.scale);
+          __builtin_memcpy(static_cast<store*>(a.out) + (row * a.heads + h) * a.dim_v + c0 + col, o, sizeof(o));
+        }
+      }
+    }
+    meet();
+  }
+
+  float* to = nullptr;
+  if (STATES)
+    to = a.part + ((b * a.parts + part + 1) * a.heads + h) * head_size;
+  else if (part == live - 1 && seq.slot >= 0)
+    to = a.state + (seq.slot * a.heads + h) * head_size;
+  if (!to) return;
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int row = 32 * s + 8 * g + 4 * t + e, col = c0 + wc + 16 * c + r;
+          if (row < a.dim_k && col < a.dim_v) to[static_cast<int64_t>(row) * a.dim_v + col] = S[s][t][c][e];
+        }
+  if (STATES && slice == 0 && tid == 0) a.factor[(b * a.parts + part + 1) * a.heads + h] = factor;
+}
+
+// The state that each part of a sequence begins with: four elements a thread,
+// in order over the parts.  The first part's is that of the slot, copied, since
+// the last part's workgroup may write the slot before the first one's reads it.
+__global__ __launch_bounds__(256) void join_parts(Args a) {
+  const int64_t head_size = static_cast<int64_t>(a.dim_k) * a.dim_v;
+  const int64_t per = (head_size / 4 + 255) / 256, id = a.first + blockIdx.x;
+  const int64_t at = (id % per * 256 + threadIdx.x) * 4;
+  const int h = static_cast<int>(id / per % a.heads);
+  const int64_t b = id / per / a.heads;
+  const Seq seq = sequence(a, b);
+  if (seq.n == 0 || at >= head_size) return;
+  const int live = live_parts(a, seq.n);
+  tok_f32x4 run = {0.f, 0.f, 0.f, 0.f};
+  if (!seq.fresh) __builtin_memcpy(&run, a.state + (seq.slot * a.heads + h) * head_size + at, 16);
+  for (int p = 0; p < live; ++p) {
+    float* s = a.part + ((b * a.parts + p) * a.heads + h) * head_size + at;
+    if (p > 0) {
+      tok_f32x4 own;
+      __builtin_memcpy(&own, s, 16);
+      run = own + run * a.factor[(b * a.parts + p) * a.heads + h];
+    }
+    __builtin_memcpy(s, &run, 16);
+  }
+}
+
+// The recurrence, W columns of a head's S a workgroup: a thread holds R rows of
+// four columns.
+template <class E, int W, int R>
+__global__ __launch_bounds__(256) void tokens(Args a) {
+  typedef typename E::store store;
+  constexpr int LC = W / 4, RG = 256 / LC;  // threads over columns, over rows
+  __shared__ tok_f32x4 sums[2][4][LC];
+  const int tid = threadIdx.x, lc = tid % LC, rg = tid / LC, wave = tid >> 6;
+  const int64_t id = a.first + blockIdx.x;
+  const int64_t unit = id / (8 * a.slices) * 8 + id % 8;
+  if (unit >= a.groups) return;
+  const int col = static_cast<int>(id / 8 % a.slices) * W + lc * 4;
+  const int h = static_cast<int>(unit % a.heads);
+  const int64_t b = unit / a.heads;
+  const Seq seq = sequence(a, b);
+  if (seq.n == 0) return;
+  const int hk = h / (a.heads / a.qk_heads);
+  const bool in = col < a.dim_v;
+  const int64_t head_size = static_cast<int64_t>(a.dim_k) * a.dim_v;
+  float* st = a.state + (seq.slot * a.heads + h) * head_size + col;
+  tok_f32x4 S[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    const int row = rg + RG * i;
+    S[i] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+    if (!seq.fresh && in && row < a.dim_k) __builtin_memcpy(&S[i], st + static_cast<int64_t>(row) * a.dim_v, 16);
+  }
+  for (int64_t n = 0; n < seq.n; ++n) {
+    const int64_t t = seq.first + n;
+    const store* q = static_cast<const store*>(a.q) + t * a.ld_q + static_cast<int64_t>(hk) * a.dim_k;
+    const store* k = static_cast<const store*>(a.k) + t * a.ld_k + static_cast<int64_t>(hk) * a.dim_k;
+    const store* v = static_cast<const store*>(a.v) + t * a.ld_v + static_cast<int64_t>(h) * a.dim_v + col;
+    const float keep = exp2_of(a.decay[t * a.ld_decay + h] * static_cast<float>(kLog2e));
+    float fq[R], fk[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int row = rg + RG * i < a.dim_k ? rg + RG * i : a.dim_k - 1;
+      fq[i] = E::widen(q[row]);
+      fk[i] = E::widen(k[row]);
+    }
+    store sv[4];
+    if (in) {
+      __builtin_memcpy(sv, v, sizeof(sv));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sv[e] = store(0);
+    }
+    const tok_f32x4 fv = {E::widen(sv[0]), E::widen(sv[1]), E::widen(sv[2]), E::widen(sv[3])};
+    tok_f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      S[i] = S[i] * keep + fv * fk[i];
+      if (rg + RG * i < a.dim_k) o += S[i] * fq[i];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int x = LC; x < 64; x <<= 1) o[e] += __shfl_xor(o[e], x);
+    if ((tid & 63) < LC) sums[n & 1][wave][lc] = o;
+    meet();
+    if (tid < LC && in) {
+      o = (sums[n & 1][0][lc] + sums[n & 1][1][lc]) + (sums[n & 1][2][lc] + sums[n & 1][3][lc]);
+      store out[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[e] = E::narrow(o[e] * a.scale);
+      __builtin_memcpy(static_cast<store*>(a.out) + (t * a.heads + h) * a.dim_v + col, out, sizeof(out));
+    }
+  }
+  if (seq.slot < 0 || !in) return;
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (rg + RG * i < a.dim_k) __builtin_memcpy(st + static_cast<int64_t>(rg + RG * i) * a.dim_v, &S[i], 16);
+}
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// rows of a thread where rg threads share dk of them
+constexpr int rows_each(int dk, int rg) { return dk > rg ? dk / rg : 1; }
+
+constexpr int64_t kFew = 16;  // new tokens of a sequence that take the recurrence
+
+// New tokens that a sequence may have.
+int64_t most_new(const c3c_kv_batch& b) { return b.max_new < b.T ? b.max_new : b.T; }
+
+// The chunk kernel's tile: rows of S, columns of a workgroup, tokens of a chunk.
+struct Tile {
+  int dk, dvs, c;
+};
+Tile tile_of(int dtype, int64_t dim_k, int64_t dim_v) {
+  Tile t;
+  t.dk = dim_k <= 64 ? 64 : dim_k <= 128 ? 128 : 256;
+  t.dvs = dim_v <= 64 || t.dk == 256 || dtype == C3C_DTYPE_F32 ? 64 : 128;
+  t.c = dtype != C3C_DTYPE_BF16 || t.dk == 256 ? 32 : 64;
+  return t;
+}
+
+template <class E, int DK, int DVS, int C>
+hipError_t run_chunks(Args a, hipStream_t s) {
+  const int64_t head_size = static_cast<int64_t>(a.dim_k) * a.dim_v;
+  auto go = [&](void (*k)(Args), int64_t units) {
+    a.groups = units;
+    return in_launches(up(units, 8) * 8 * a.slices, 256, [&](int64_t first, unsigned count) {
+      a.first = first;
+      hipLaunchKernelGGL(k, dim3(count), dim3(256), 0, s, a);
+    });
+  };
+  if (a.parts > 1) {
+    hipError_t e = go(chunks<E, DK, DVS, C, true>, a.B * a.heads * (a.parts - 1));
+    if (e != hipSuccess) return e;
+    e = in_launches(a.B * a.heads * up(head_size / 4, 256), 256, [&](int64_t first, unsigned count) {
+      a.first = first;
+      hipLaunchKernelGGL(join_parts, dim3(count), dim3(256), 0, s, a);
+    });
+    if (e != hipSuccess) return e;
+  }
+  return go(chunks<E, DK, DVS, C, false>, a.B * a.heads * a.parts);
+}
+
+template <class E, int W>
+hipError_t run_tokens(Args a, hipStream_t s) {
+  constexpr int RG = 256 / (W / 4);
+  a.slices = static_cast<int>(up(a.dim_v, W));
+  a.groups = a.B * a.heads;
+  auto k = a.dim_k <= 64 ? tokens<E, W, rows_each(64, RG)> : a.dim_k <= 128 ? tokens<E, W, rows_each(128, RG)> : tokens<E, W, rows_each(256, RG)>;
+  return in_launches(up(a.groups, 8) * 8 * a.slices, 256, [&](int64_t first, unsigned count) {
+    a.first = first;
+    hipLaunchKernelGGL(k, dim3(count), dim3(256), 0, s, a);
+  });
+}
+
+template <class E>
+hipError_t run(Args a, int dtype, int64_t most, hipStream_t s) {
+  if (most <= kFew) {
+    // narrow slices where there are few heads
+    return a.B * a.heads < 256 ? run_tokens<E, 16>(a, s) : run_tokens<E, 32>(a, s);
+  }
+  const Tile t = tile_of(dtype, a.dim_k, a.dim_v);
+  a.slices = static_cast<int>(up(a.dim_v, t.dvs));
+  constexpr bool f32 = E::VEC == 4, bf16 = Terms<E>::IN == 1;
+  constexpr int C = bf16 ? 64 : 32, WIDE = f32 ? 64 : 128;
+  if (t.dk == 256) return run_chunks<E, 256, 64, 32>(a, s);
+  if (t.dvs == 64) return t.dk == 64 ? run_chunks<E, 64, 64, C>(a, s) : run_chunks<E, 128, 64, C>(a, s);
+  return t.dk == 64 ? run_chunks<E, 64, WIDE, C>(a, s) : run_chunks<E, 128, WIDE, C>(a, s);
+}
+
+}  // namespace
+
+RecurPlan plan_recur(const c3c_state_cache& st, const c3c_kv_batch& b, int dtype) {
+  RecurPlan p;
+  const int64_t most = most_new(b);
+  if (most <= kFew || b.B < 1) return p;
+  const Tile t = tile_of(dtype, st.dim_k, st.dim_v);
+  const int64_t chunks = up(most, t.c), units = b.B * st.heads * up(st.dim_v, t.dvs);
+  const int64_t room = 2 * device_compute_units();
+  int64_t parts = room / units;
+  if (parts > chunks / 4) parts = chunks / 4;
+  if (parts < 2) return p;
+  const int64_t each = up(chunks, parts);
+  p.part_tokens = each * t.c;
+  p.parts = static_cast<int>(up(chunks, each));
+  p.state_bytes = b.B * p.parts * st.heads * st.dim_k * st.dim_v * 4;
+  p.bytes = p.state_bytes + b.B * p.parts * st.heads * 4;
+  return p;
+}
+
+hipError_t launch_recur(const RecurArgs& r, int dtype, const RecurPlan& plan, hipStream_t s) {
+  const c3c_state_cache& st = r.st;
+  if (r.b.T == 0 || r.b.B == 0) return hipSuccess;
+  const int64_t most = most_new(r.b);
+  Args a{st.state, r.b.cu, r.b.len, r.slot, r.q, r.k, r.v, r.decay, r.out, r.part, nullptr, st.slots, r.b.B, r.b.T,
+         r.ld_q, r.ld_k, r.ld_v, r.ld_decay, plan.part_tokens, 0, 0, static_cast<int>(st.heads),
+         static_cast<int>(r.qk_heads), static_cast<int>(st.dim_k), static_cast<int>(st.dim_v), plan.parts, 1, r.scale};
+  if (plan.parts > 1) a.factor = r.part + plan.state_bytes / 4;
+  return dtype == C3C_DTYPE_BF16 ? run<ElemBf16>(a, dtype, most, s) : dtype == C3C_DTYPE_F16 ? run<ElemF16>(a, dtype, most, s) : run<ElemF32>(a, dtype, most, s);
+}
+
+}  // namespace c3c

@@ -5,6 +5,12 @@
 // tokens B (columns m), so that a lane's four results are four consecutive n
 // of one token and are stored together.
 //
+// What happens to a result before its rounding is compiled in (EPI): nothing;
+// an activation, a gate and a residual; or, with weights of 2 N rows, the
+// product of an activation of one half and the other (gated).  A gated tile takes
+// its rows half from each half of the weights, so that both results of a
+// channel meet in one lane.
+//
 // skinny: at most 32 tokens.  The weights are read once, straight into
 //   registers (no tile of them is used twice), by 4 waves that share 16 rows
 //   and take every fourth 128-byte piece of K, 8 of them in flight; their sums
@@ -41,45 +47,125 @@ struct is_codes<Codes> {
   static constexpr bool value = true;
 };
 
+enum { PLAIN = LinearEpilogue::kPlain, EPILOGUE = LinearEpilogue::kEpilogue, GATED = LinearEpilogue::kGated };
+
 struct LinArgs {
   const int8_t *x, *w;  // x: also the address of float tokens (linear_skinny)
   const float *x_scale, *w_scale, *bias;
   void* y;
-  int32_t* part;  // [splits][M][N], or NULL: y is written
+  int32_t* part;  // [splits][M][N] (gated: 2 N), or NULL: y is written
   int64_t M, N, K, ldx;
   int tiles_m, tiles_n;
   int splits;     // along K, in stages
   int y_dtype;
   int64_t first;  // workgroup of this launch
+  LinearEpilogue e;
 };
 
-// w_scale and bias of four consecutive channels (the last one's past N)
+// w_scale and bias of four consecutive channels (the last one's past N), gated
+// also of those N further on
+template <int EPI>
 struct Channels {
-  float s[4], b[4];
+  static constexpr int H = EPI == GATED ? 2 : 1;
+  float s[H][4], b[H][4];
 };
-__device__ inline Channels channels(const LinArgs& a, int64_t n) {
-  Channels c;
-  if (n + 4 <= a.N) {
-    __builtin_memcpy(c.s, a.w_scale + n, 16);
-    if (a.bias) __builtin_memcpy(c.b, a.bias + n, 16);
-  } else {
+template <int EPI>
+__device__ inline Channels<EPI> channels(const LinArgs& a, int64_t n) {
+  Channels<EPI> c;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t at = n + i < a.N ? n + i : a.N - 1;
-      c.s[i] = a.w_scale[at];
-      if (a.bias) c.b[i] = a.bias[at];
+  for (int h = 0; h < c.H; ++h) {
+    const float *ws = a.w_scale + h * a.N, *bias = a.bias ? a.bias + h * a.N : nullptr;
+    if (n + 4 <= a.N) {
+      __builtin_memcpy(c.s[h], ws + n, 16);
+      if (bias) __builtin_memcpy(c.b[h], bias + n, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t at = n + i < a.N ? n + i : a.N - 1;
+        c.s[h][i] = ws[at];
+        if (bias) c.b[h][i] = bias[at];
+      }
     }
   }
   return c;
 }
 
-// four results of token m, of which those below N are stored
-__device__ inline void put4(const LinArgs& a, int64_t m, int64_t n, tok_i32x4 v, float s, const Channels& c) {
+// z / (1 + exp(-z))
+__device__ inline float swish(float z) { return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
+__device__ inline float activate(int act, float z) {
+  switch (act) {
+    case C3C_ACT_SILU:
+      return swish(z);
+    case C3C_ACT_GELU:
+      return 0.5f * z * (1.f + erff(0.707106781f * z));
+    case C3C_ACT_GELU_TANH: {
+      // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
+      const float u = 1.59576912f * (z + 0.044715f * z * z * z);
+      return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * u));
+    }
+    default:
+      return z;
+  }
+}
+
+// four values of a row from p, those past N being 0
+__device__ inline void get4(int dtype, const void* p, int64_t at, int64_t left, float (&f)[4]) {
+  if (dtype == C3C_DTYPE_F32) {
+    const float* q = static_cast<const float*>(p) + at;
+    if (left >= 4) {
+      __builtin_memcpy(f, q, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[i] = i < left ? q[i] : 0.f;
+    }
+  } else {
+    const uint16_t* q = static_cast<const uint16_t*>(p) + at;
+    uint16_t h[4];
+    if (left >= 4) {
+      __builtin_memcpy(h, q, 8);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[i] = i < left ? q[i] : uint16_t(0);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = dtype == C3C_DTYPE_BF16 ? ElemBf16::widen(h[i]) : ElemF16::widen(h[i]);
+  }
+}
+
+// What four results meet: the residual and the gates (EPILOGUE).
+struct Beside {
+  float residual[4], gate[4];
+};
+template <int EPI>
+__device__ inline Beside beside(const LinArgs& a, int64_t m, int64_t n) {
+  Beside x;
+  if constexpr (EPI == EPILOGUE) {
+    if (a.e.residual) get4(a.y_dtype, a.e.residual, m * a.N + n, a.N - n, x.residual);
+    if (a.e.gate) get4(a.y_dtype, a.e.gate, static_cast<int64_t>(static_cast<uint32_t>(m) / a.e.rows_per_gate) * a.N + n, a.N - n, x.gate);
+  }
+  return x;
+}
+
+// four results of token m, of which those below N are stored; gated: v[0] those
+// of the first half of the weights, v[1] of the second
+template <int EPI>
+__device__ inline void put4(const LinArgs& a, int64_t m, int64_t n, const tok_i32x4 (&v)[Channels<EPI>::H], float s,
+                            const Channels<EPI>& c, const Beside& x) {
   float f[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    f[i] = static_cast<float>(v[i]) * s * c.s[i];
-    if (a.bias) f[i] += c.b[i];
+    float z[Channels<EPI>::H];
+#pragma unroll
+    for (int h = 0; h < Channels<EPI>::H; ++h) {
+      z[h] = static_cast<float>(v[h][i]) * s * c.s[h][i];
+      if (a.bias) z[h] += c.b[h][i];
+    }
+    f[i] = EPI == PLAIN ? z[0] : activate(a.e.act, z[0]);
+    if constexpr (EPI == GATED) f[i] *= z[1];
+    if constexpr (EPI == EPILOGUE) {
+      if (a.e.gate) f[i] *= x.gate[i];
+      if (a.e.residual) f[i] = __builtin_fmaf(a.e.alpha, x.residual[i], f[i]);
+    }
   }
   const int64_t at = m * a.N + n;
   if (a.y_dtype == C3C_DTYPE_F32) {
@@ -125,10 +211,11 @@ constexpr int kFusedBytes = 32768;  // of quantised rows in LDS
 
 // MT tiles of 16 tokens.  E: int8 for codes, or the type of float tokens that
 // the kernel quantises (MT = 1, at most kFusedBytes of codes).
-template <class E, int MT, bool AL>
+template <class E, int MT, bool AL, int EPI>
 __global__ __launch_bounds__(256) void linear_skinny(LinArgs a) {
   constexpr bool FUSE = !is_codes<E>::value;
-  __shared__ tok_i32x4 sums[3][MT][64];
+  constexpr int H = Channels<EPI>::H;
+  __shared__ tok_i32x4 sums[3][MT][H][64];
   __shared__ __align__(16) int8_t rows[FUSE ? kFusedBytes : 16];
   __shared__ float tops[4][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -136,15 +223,16 @@ __global__ __launch_bounds__(256) void linear_skinny(LinArgs a) {
   const int64_t n0 = (a.first + blockIdx.x) * 16;
   const int64_t nr = n0 + r < a.N ? n0 + r : a.N - 1;
   const int8_t* wp = a.w + nr * a.K;
-  constexpr int U = 8 / MT < 4 ? 4 : 8 / MT;  // stages in flight
-  tok_i32x4 wv[U][2];
+  constexpr int U = H == 2 || 8 / MT < 4 ? 4 : 8 / MT;  // stages in flight
+  tok_i32x4 wv[U][2][H];
   auto fetch = [&](int64_t k0) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
         const int64_t k = k0 + 512 * u + 64 * j + 16 * g;
-        wv[u][j] = piece<AL>(wp + k, a.K - k);
+#pragma unroll
+        for (int h = 0; h < H; ++h) wv[u][j][h] = piece<AL>(wp + h * a.N * a.K + k, a.K - k);
       }
   };
   fetch(wave * 128);
@@ -181,15 +269,19 @@ __global__ __launch_bounds__(256) void linear_skinny(LinArgs a) {
     const int64_t m = t * 16 + r < a.M ? t * 16 + r : a.M - 1;
     xp[t] = FUSE ? rows + m * pitch : a.x + m * a.ldx;
   }
-  tok_i32x4 acc[MT];
+  tok_i32x4 acc[MT][H];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) acc[t] = tok_i32x4{0, 0, 0, 0};
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int h = 0; h < H; ++h) acc[t][h] = tok_i32x4{0, 0, 0, 0};
   for (int64_t k0 = wave * 128; k0 < a.K; k0 += 512 * U) {
-    tok_i32x4 now[U][2];
+    tok_i32x4 now[U][2][H];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) now[u][j] = wv[u][j];
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int h = 0; h < H; ++h) now[u][j][h] = wv[u][j][h];
     if (k0 + 512 * U < a.K) fetch(k0 + 512 * U);
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -199,24 +291,29 @@ __global__ __launch_bounds__(256) void linear_skinny(LinArgs a) {
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
           const tok_i32x4 xv = FUSE ? piece<true>(xp[t] + k, a.K - k) : piece<AL>(xp[t] + k, a.K - k);
-          acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[u][j], xv, acc[t], 0, 0, 0);
+#pragma unroll
+          for (int h = 0; h < H; ++h) acc[t][h] = __builtin_amdgcn_mfma_i32_16x16x64_i8(now[u][j][h], xv, acc[t][h], 0, 0, 0);
         }
       }
   }
   if (wave > 0) {
 #pragma unroll
-    for (int t = 0; t < MT; ++t) sums[wave - 1][t][lane] = acc[t];
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int h = 0; h < H; ++h) sums[wave - 1][t][h][lane] = acc[t][h];
   }
   __syncthreads();
   if (wave > 0) return;
 #pragma unroll
   for (int t = 0; t < MT; ++t) {
 #pragma unroll
-    for (int w = 0; w < 3; ++w) acc[t] += sums[w][t][lane];
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+      for (int h = 0; h < H; ++h) acc[t][h] += sums[w][t][h][lane];
     const int64_t m = t * 16 + r, n = n0 + g * 4;
     if (m >= a.M || n >= a.N) continue;
     const float s = FUSE ? row_scale(fmaxf(fmaxf(tops[0][m], tops[1][m]), fmaxf(tops[2][m], tops[3][m]))) : a.x_scale[m];
-    put4(a, m, n, acc[t], s, channels(a, n));
+    put4<EPI>(a, m, n, acc[t], s, channels<EPI>(a, n), beside<EPI>(a, m, n));
   }
 }
 
@@ -231,8 +328,10 @@ __device__ inline int spread(int r, int c) {
 #define C3C_VMCNT(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | (((n) >> 4) << 14) | (7 << 4) | (15 << 8))
 
 // (BM / WM) * (BN / WN) waves, each with a WM x WN part of the tile.
-template <int BM, int BN, int WM, int WN, int BK, int NS, bool AL>
+// Gated, the rows of w in a wave's part are half of one half, half of the other.
+template <int BM, int BN, int WM, int WN, int BK, int NS, bool AL, int EPI>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinArgs a) {
+  constexpr int H = Channels<EPI>::H, ON = BN / H;  // channels of y
   constexpr int NW = (BM / WM) * (BN / WN);
   constexpr int MT = WM / 16, NT = WN / 16;
   constexpr int ROWS = BM + BN;              // rows of w, then rows of x
@@ -260,19 +359,22 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
   const int colg = b / (COL * a.tiles_n), in = b - colg * COL * a.tiles_n;
   const int high = a.tiles_m - colg * COL < COL ? a.tiles_m - colg * COL : COL;
   const int tm = colg * COL + in % high, tn = in / high;
-  const int64_t m0 = static_cast<int64_t>(tm) * BM, n0 = static_cast<int64_t>(tn) * BN;
+  const int64_t m0 = static_cast<int64_t>(tm) * BM, n0 = static_cast<int64_t>(tn) * ON;
 
   const int stages = static_cast<int>((a.K + BK - 1) / BK);
   const int s0 = static_cast<int>(static_cast<int64_t>(stages) * split / a.splits);
   const int count = static_cast<int>(static_cast<int64_t>(stages) * (split + 1) / a.splits) - s0;
 
-  const int64_t nrows = a.N - n0 < BN ? a.N - n0 : BN, mrows = a.M - m0 < BM ? a.M - m0 : BM;
+  const int64_t nrows = a.N - n0 < ON ? a.N - n0 : ON, mrows = a.M - m0 < BM ? a.M - m0 : BM;
   const int8_t* wb = a.w + n0 * a.K;
   const int8_t* xb = a.x + m0 * a.ldx;
   // the part of a load that this lane brings: row and piece
   const int lrow = lane / (BK / 16), lpiece = spread<BK>(lrow, lane % (BK / 16));
   const __amdgpu_buffer_rsrc_t wrs = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<int8_t*>(wb), 0, static_cast<int>(nrows * a.K), 0x00020000);
+  const int8_t* wb2 = wb + (EPI == GATED ? a.N * a.K : 0);  // the second half's rows
+  const __amdgpu_buffer_rsrc_t wrs2 = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<int8_t*>(wb2), 0, static_cast<int>(nrows * a.K), 0x00020000);
   const __amdgpu_buffer_rsrc_t xrs = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<int8_t*>(xb), 0, static_cast<int>((mrows - 1) * a.ldx + a.K), 0x00020000);
   tok_i32x4 staged[LOADS];  // !AL
@@ -281,17 +383,20 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
     const int k = (s0 + st) * BK + lpiece * 16, buf = st % NS;
     const int row = (i * NW + wave) * LR;  // of ROWS, uniform; whole loads are of w or of x
     const bool isw = row < BN;
-    const int rr = (isw ? row : row - BN) + lrow;
+    // of w: the row within its half, and which half (whole loads are of one half)
+    const bool second = EPI == GATED && row / (WN / 2) % 2 == 1;
+    const int wrow = EPI == GATED ? row / WN * (WN / 2) + row % (WN / 2) : row;
+    const int rr = (isw ? wrow : row - BN) + lrow;
     if (AL) {
       const int ld = static_cast<int>(isw ? a.K : a.ldx);
       // past K: a sign bit takes the offset out of every buffer
       const int off = (rr * ld + k) | ((static_cast<int>(a.K) - 1 - k) & static_cast<int>(0x80000000u));
       lds_void* to = (lds_void*)(lds + buf * ROWS * BK + row * BK);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(isw ? wrs : xrs, to, 16, off, 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(isw ? second ? wrs2 : wrs : xrs, to, 16, off, 0, 0, 0);
     } else {
       const int64_t ld = isw ? a.K : a.ldx;
       const bool ok = rr < (isw ? nrows : mrows);
-      staged[i] = piece<false>((isw ? wb : xb) + (ok ? rr * ld + k : 0), ok ? a.K - k : 0);
+      staged[i] = piece<false>((isw ? second ? wb2 : wb : xb) + (ok ? rr * ld + k : 0), ok ? a.K - k : 0);
     }
   };
   auto settle = [&](int st) __attribute__((always_inline)) {  // !AL
@@ -379,50 +484,75 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
       xs[j] = a.x_scale[m < a.M ? m : a.M - 1];
     }
   }
+  constexpr int OT = NT / H;  // tiles of 16 channels of y
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int64_t n = n0 + wn + i * 16 + g * 4;
+  for (int i = 0; i < OT; ++i) {
+    const int64_t n = n0 + wn / H + i * 16 + g * 4;
     if (n >= a.N) continue;
-    Channels c;
-    if (!a.part) c = channels(a, n);
+    if (a.part) {
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-      const int64_t m = m0 + wm + j * 16 + r;
-      if (m >= a.M) continue;
-      if (a.part) {
-        int32_t* p = a.part + (split * a.M + m) * a.N + n;
-        if (n + 4 <= a.N) {
-          __builtin_memcpy(p, &acc[i][j], 16);
-        } else {
-          for (int e = 0; e < 3; ++e)
-            if (n + e < a.N) p[e] = acc[i][j][e];
+      for (int j = 0; j < MT; ++j) {
+        const int64_t m = m0 + wm + j * 16 + r;
+        if (m >= a.M) continue;
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          int32_t* p = a.part + ((split * a.M + m) * H + h) * a.N + n;
+          if (n + 4 <= a.N) {
+            __builtin_memcpy(p, &acc[i + h * OT][j], 16);
+          } else {
+            for (int e = 0; e < 3; ++e)
+              if (n + e < a.N) p[e] = acc[i + h * OT][j][e];
+          }
         }
-      } else {
-        put4(a, m, n, acc[i][j], xs[j], c);
+      }
+    } else {
+      const Channels<EPI> c = channels<EPI>(a, n);
+      Beside x[MT];  // asked for together: y may be the residual
+#pragma unroll
+      for (int j = 0; j < MT; ++j) {
+        const int64_t m = m0 + wm + j * 16 + r;
+        x[j] = beside<EPI>(a, m < a.M ? m : a.M - 1, n);
+      }
+#pragma unroll
+      for (int j = 0; j < MT; ++j) {
+        const int64_t m = m0 + wm + j * 16 + r;
+        if (m >= a.M) continue;
+        tok_i32x4 v[H];
+#pragma unroll
+        for (int h = 0; h < H; ++h) v[h] = acc[i + h * OT][j];
+        put4<EPI>(a, m, n, v, xs[j], c, x[j]);
       }
     }
   }
 }
 
 // y from the partial sums of a split call: four results a thread.
+template <int EPI>
 __global__ __launch_bounds__(256) void linear_join(LinArgs a) {
+  constexpr int H = Channels<EPI>::H;
   const int64_t quads = (a.N + 3) / 4;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (i >= a.M * quads) return;
   const int64_t m = i / quads, n = i % quads * 4;
-  tok_i32x4 v = {0, 0, 0, 0};
+  const Beside x = beside<EPI>(a, m, n);
+  tok_i32x4 v[H];
+#pragma unroll
+  for (int h = 0; h < H; ++h) v[h] = tok_i32x4{0, 0, 0, 0};
   for (int s = 0; s < a.splits; ++s) {
-    const int32_t* p = a.part + (s * a.M + m) * a.N + n;
-    if (n + 4 <= a.N) {
-      tok_i32x4 t;
-      __builtin_memcpy(&t, p, 16);
-      v += t;
-    } else {
-      for (int e = 0; e < 3; ++e)
-        if (n + e < a.N) v[e] += p[e];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int32_t* p = a.part + ((s * a.M + m) * H + h) * a.N + n;
+      if (n + 4 <= a.N) {
+        tok_i32x4 t;
+        __builtin_memcpy(&t, p, 16);
+        v[h] += t;
+      } else {
+        for (int e = 0; e < 3; ++e)
+          if (n + e < a.N) v[h][e] += p[e];
+      }
     }
   }
-  put4(a, m, n, v, a.x_scale[m], channels(a, n));
+  put4<EPI>(a, m, n, v, a.x_scale[m], channels<EPI>(a, n), x);
 }
 
 // Rows of n bytes, ld apart, to rows of ldd (a multiple of 16), zero past n: 16
@@ -449,12 +579,12 @@ Tile tile_of(int64_t M, int64_t N) {
   return {64, 64};
 }
 
-template <int BM, int BN, int WM, int WN, int BK, int NS, bool AL>
+template <int BM, int BN, int WM, int WN, int BK, int NS, bool AL, int EPI>
 hipError_t run_tiled(LinArgs a, hipStream_t s) {
   constexpr int threads = (BM / WM) * (BN / WN) * 64;
-  auto k = linear_tiled<BM, BN, WM, WN, BK, NS, AL>;
+  auto k = linear_tiled<BM, BN, WM, WN, BK, NS, AL, EPI>;
   a.tiles_m = static_cast<int>(up(a.M, BM));
-  a.tiles_n = static_cast<int>(up(a.N, BN));
+  a.tiles_n = static_cast<int>(up(a.N, BN / Channels<EPI>::H));
   const int64_t blocks = static_cast<int64_t>(a.tiles_m) * a.tiles_n * a.splits;
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   return in_launches(blocks, threads, [&](int64_t first, unsigned count) {
@@ -500,30 +630,48 @@ LinearPlan plan_linear_i8(int64_t M, int64_t N, int64_t K) {
   return p;
 }
 
-hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, int64_t ldx,
-                            const float* x_scale, const int8_t* w, const float* w_scale,
-                            const float* bias, void* y, int y_dtype, const LinearPlan& plan,
-                            int32_t* part, hipStream_t s) {
-  if (M == 0) return hipSuccess;
-  LinArgs a{x, w, x_scale, w_scale, bias, y, part, M, N, K, ldx, 0, 0, part ? plan.splits : 1, y_dtype, 0};
+namespace {
+
+template <int EPI>
+hipError_t run_linear(LinArgs a, hipStream_t s) {
   // 16-byte pieces, and a tile's rows within the 31-bit offsets of a buffer
-  const bool al = K % 16 == 0 && ldx % 16 == 0 && ldx < (1 << 22) && reinterpret_cast<uintptr_t>(x) % 16 == 0 &&
-                  reinterpret_cast<uintptr_t>(w) % 16 == 0;
-  if (M <= kSkinny) {
-    auto k = M <= 16   ? (al ? linear_skinny<Codes, 1, true> : linear_skinny<Codes, 1, false>)
-                       : (al ? linear_skinny<Codes, 2, true> : linear_skinny<Codes, 2, false>);
+  const bool al = a.K % 16 == 0 && a.ldx % 16 == 0 && a.ldx < (1 << 22) && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 &&
+                  reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
+  if (a.M <= kSkinny) {
+    auto k = a.M <= 16   ? (al ? linear_skinny<Codes, 1, true, EPI> : linear_skinny<Codes, 1, false, EPI>)
+                         : (al ? linear_skinny<Codes, 2, true, EPI> : linear_skinny<Codes, 2, false, EPI>);
     return run_skinny(k, a, s);
   }
-  const Tile t = tile_of(M, N);
-  hipError_t e = t.bm == 256   ? (al ? run_tiled<256, 256, 128, 64, 128, 2, true>(a, s) : run_tiled<256, 256, 128, 64, 64, 4, false>(a, s))
-                 : t.bm == 128 ? (al ? run_tiled<128, 128, 64, 64, 64, 4, true>(a, s) : run_tiled<128, 128, 64, 64, 64, 4, false>(a, s))
-                               : (al ? run_tiled<64, 64, 32, 32, 64, 4, true>(a, s) : run_tiled<64, 64, 32, 32, 64, 4, false>(a, s));
-  if (e == hipSuccess && part) {
-    const int64_t blocks = up(M * up(N, 4), 256);  // few: a call of many tiles is not split
-    hipLaunchKernelGGL(linear_join, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
+  const Tile t = tile_of(a.M, a.N * Channels<EPI>::H);
+  hipError_t e = t.bm == 256   ? (al ? run_tiled<256, 256, 128, 64, 128, 2, true, EPI>(a, s) : run_tiled<256, 256, 128, 64, 64, 4, false, EPI>(a, s))
+                 : t.bm == 128 ? (al ? run_tiled<128, 128, 64, 64, 64, 4, true, EPI>(a, s) : run_tiled<128, 128, 64, 64, 64, 4, false, EPI>(a, s))
+                               : (al ? run_tiled<64, 64, 32, 32, 64, 4, true, EPI>(a, s) : run_tiled<64, 64, 32, 32, 64, 4, false, EPI>(a, s));
+  if (e == hipSuccess && a.part) {
+    const int64_t blocks = up(a.M * up(a.N, 4), 256);  // few: a call of many tiles is not split
+    hipLaunchKernelGGL(linear_join<EPI>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, a);
     e = hipGetLastError();
   }
   return e;
+}
+
+template <int EPI>
+hipError_t run_float(const LinArgs& a, int x_dtype, hipStream_t s) {
+  const bool al = a.K % 16 == 0 && reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
+  auto k = x_dtype == C3C_DTYPE_BF16  ? (al ? linear_skinny<ElemBf16, 1, true, EPI> : linear_skinny<ElemBf16, 1, false, EPI>)
+           : x_dtype == C3C_DTYPE_F16 ? (al ? linear_skinny<ElemF16, 1, true, EPI> : linear_skinny<ElemF16, 1, false, EPI>)
+                                      : (al ? linear_skinny<ElemF32, 1, true, EPI> : linear_skinny<ElemF32, 1, false, EPI>);
+  return run_skinny(k, a, s);
+}
+
+}  // namespace
+
+hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, int64_t ldx,
+                            const float* x_scale, const int8_t* w, const float* w_scale,
+                            const float* bias, void* y, int y_dtype, const LinearEpilogue& e,
+                            const LinearPlan& plan, int32_t* part, hipStream_t s) {
+  if (M == 0) return hipSuccess;
+  LinArgs a{x, w, x_scale, w_scale, bias, y, part, M, N, K, ldx, 0, 0, part ? plan.splits : 1, y_dtype, 0, e};
+  return e.kind == EPILOGUE ? run_linear<EPILOGUE>(a, s) : e.kind == GATED ? run_linear<GATED>(a, s) : run_linear<PLAIN>(a, s);
 }
 
 // The copy costs its traffic and a launch, and about halves the products: it
@@ -540,14 +688,10 @@ bool linear_quantises(int64_t M, int64_t K) { return M <= 4 && M * ((K + 15) / 1
 
 hipError_t launch_linear_float(int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, int x_dtype,
                                const int8_t* w, const float* w_scale, const float* bias, void* y, int y_dtype,
-                               hipStream_t s) {
+                               const LinearEpilogue& e, hipStream_t s) {
   if (M == 0) return hipSuccess;
-  LinArgs a{static_cast<const int8_t*>(x), w, nullptr, w_scale, bias, y, nullptr, M, N, K, ldx, 0, 0, 1, y_dtype, 0};
-  const bool al = K % 16 == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
-  auto k = x_dtype == C3C_DTYPE_BF16  ? (al ? linear_skinny<ElemBf16, 1, true> : linear_skinny<ElemBf16, 1, false>)
-           : x_dtype == C3C_DTYPE_F16 ? (al ? linear_skinny<ElemF16, 1, true> : linear_skinny<ElemF16, 1, false>)
-                                      : (al ? linear_skinny<ElemF32, 1, true> : linear_skinny<ElemF32, 1, false>);
-  return run_skinny(k, a, s);
+  LinArgs a{static_cast<const int8_t*>(x), w, nullptr, w_scale, bias, y, nullptr, M, N, K, ldx, 0, 0, 1, y_dtype, 0, e};
+  return e.kind == EPILOGUE ? run_float<EPILOGUE>(a, x_dtype, s) : e.kind == GATED ? run_float<GATED>(a, x_dtype, s) : run_float<PLAIN>(a, x_dtype, s);
 }
 
 }  // namespace c3c

@@ -85,14 +85,16 @@ const char* check_linear(const c3c_linear_desc* d) {
 // scales, which it cannot do without; copies of w and of int8 x in rows of whole
 // 16 bytes; the partial sums.
 struct LinearSpace {
+  int64_t rows_of_w = 0;
   int64_t ldq = 0, scale_at = 0, rows_bytes = 0;  // of float x
   int64_t w_at = 0, x_at = 0, pads_end = 0;       // w_at == x_at: no copy of w; x_at == pads_end: none of x
   int64_t part_at = 0;
   LinearPlan plan;
 };
-LinearSpace linear_space(const c3c_linear_desc& d) {
+LinearSpace linear_space(const c3c_linear_desc& d, int halves) {
   LinearSpace s;
-  s.plan = plan_linear_i8(d.M, d.N, d.K);
+  s.rows_of_w = halves * d.N;
+  s.plan = plan_linear_i8(d.M, s.rows_of_w, d.K);
   const bool i8 = d.x_dtype == C3C_DTYPE_I8;
   s.ldq = round_up(d.K, 16);
   if (!i8 && d.M > 0) {
@@ -100,10 +102,109 @@ LinearSpace linear_space(const c3c_linear_desc& d) {
     s.rows_bytes = s.scale_at + round_up(d.M * 4, 256);
   }
   s.w_at = s.rows_bytes;
-  s.x_at = s.w_at + (linear_pads(d.M, d.K, d.K) ? round_up(d.N * s.ldq, 256) : 0);
+  s.x_at = s.w_at + (linear_pads(d.M, d.K, d.K) ? round_up(s.rows_of_w * s.ldq, 256) : 0);
   s.pads_end = s.x_at + (i8 && linear_pads(d.M, d.K, d.ld_x) ? round_up(d.M * s.ldq, 256) : 0);
   s.part_at = s.pads_end;
   return s;
+}
+
+size_t linear_bytes(const c3c_linear_desc& d, int halves) {
+  const LinearSpace s = linear_space(d, halves);
+  return static_cast<size_t>(s.part_at + s.plan.part_bytes);
+}
+
+const char* check_gated(const c3c_linear_desc* d) {
+  const char* why = check_linear(d);
+  if (why) return why;
+  if (2 * d->N >= kBig) return "2 N exceeds 2^31";
+  if (extent(2 * d->N, d->K, d->K) < 0) return "a tensor exceeds 2^40 elements";
+  return nullptr;
+}
+
+bool known_act(int act) { return act >= C3C_ACT_NONE && act <= C3C_ACT_GELU_TANH; }
+
+// A call whose descriptor and epilogue are checked.
+int run_linear(c3c_ctx* ctx, const c3c_linear_desc& d, const LinearEpilogue& e, const void* x, const float* x_scale,
+               const int8_t* w, const float* w_scale, const float* bias, void* y, void* stream) {
+  const int halves = e.kind == LinearEpilogue::kGated ? 2 : 1;
+  const bool i8 = d.x_dtype == C3C_DTYPE_I8;
+  const int xs = i8 ? 1 : elem_bytes(d.x_dtype), ys = elem_bytes(d.y_dtype);
+  if (i8 ? !x_scale && d.M > 0 : x_scale != nullptr)
+    return fail(ctx, C3C_E_INVAL, "x_scale goes with int8 x, and with it alone");
+  const Span in[] = {{"x", x, extent(d.M, d.K, d.ld_x) * xs, xs},
+                     {"x_scale", x_scale, x_scale ? d.M * 4 : 0, 4},
+                     {"w", w, halves * d.N * d.K, 1},
+                     {"w_scale", w_scale, halves * d.N * 4, 4},
+                     {"bias", bias, bias ? halves * d.N * 4 : 0, 4},
+                     {"gate", e.gate, e.gate && d.M > 0 ? ((d.M - 1) / e.rows_per_gate + 1) * d.N * ys : 0, ys},
+                     // y may be the residual itself
+                     {"residual", e.residual == y ? nullptr : e.residual, e.residual && e.residual != y ? d.M * d.N * ys : 0, ys}};
+  const Span out[] = {{"y", y, d.M * d.N * ys, ys}};
+  const char* why = check_spans(in, 7);
+  if (!why) why = check_spans(out, 1);
+  if (!why) why = check_overlap(in, 7, out, 1, ctx->ws, static_cast<int64_t>(ctx->ws_bytes));
+  if (why) return fail(ctx, C3C_E_INVAL, why);
+  const LinearSpace sp = linear_space(d, halves);
+  const int64_t have = static_cast<int64_t>(ctx->ws_bytes);
+  if (sp.rows_bytes > have)
+    return fail(ctx, C3C_E_INVAL, "the context's workspace is smaller than the quantised rows need");
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  if (!i8 && linear_quantises(d.M, d.K))
+    return done(ctx, launch_linear_float(d.M, d.N, d.K, x, d.ld_x, d.x_dtype, w, w_scale, bias, y, d.y_dtype, e, s));
+  unsigned char* ws = static_cast<unsigned char*>(ctx->ws);
+  const int8_t* rows = static_cast<const int8_t*>(x);
+  int64_t ld = d.ld_x;
+  if (!i8 && d.M > 0) {
+    int8_t* q = reinterpret_cast<int8_t*>(ws);
+    float* scale = reinterpret_cast<float*>(ws + sp.scale_at);
+    const hipError_t err = launch_quantize_rows(d.M, d.K, d.ld_x, d.x_dtype, x, q, sp.ldq, scale, s);
+    if (err != hipSuccess) return done(ctx, err);
+    rows = q;
+    x_scale = scale;
+    ld = sp.ldq;
+  }
+  const int8_t* weights = w;
+  int64_t K = d.K;
+  if (sp.pads_end > sp.w_at && sp.pads_end <= have) {
+    // both operands in rows of whole 16 bytes, zero past K
+    hipError_t err = hipSuccess;
+    if (sp.x_at > sp.w_at) {
+      int8_t* to = reinterpret_cast<int8_t*>(ws + sp.w_at);
+      err = launch_pad_rows(w, sp.rows_of_w, d.K, d.K, to, sp.ldq, s);
+      weights = to;
+      K = sp.ldq;
+    }
+    if (err == hipSuccess && sp.pads_end > sp.x_at) {
+      int8_t* to = reinterpret_cast<int8_t*>(ws + sp.x_at);
+      err = launch_pad_rows(rows, d.M, d.K, ld, to, sp.ldq, s);
+      rows = to;
+      ld = sp.ldq;
+    }
+    if (err != hipSuccess) return done(ctx, err);
+  }
+  int32_t* part = sp.plan.splits > 1 && sp.part_at + sp.plan.part_bytes <= have
+                      ? reinterpret_cast<int32_t*>(ws + sp.part_at)
+                      : nullptr;
+  return done(ctx, launch_linear_i8(d.M, d.N, K, rows, ld, x_scale, weights, w_scale, bias, y, d.y_dtype, e,
+                                    sp.plan, part, s));
+}
+
+// ---------------------------------------------------------------- linear attention
+
+const char* check_recur(const c3c_state_cache* st, const c3c_kv_batch* b, int dtype, int64_t qk_heads) {
+  if (!st || !b) return "states or batch is NULL";
+  if (!elem_bytes(dtype)) return "unknown dtype";
+  if (st->slots < 0 || st->slots >= kBig || st->heads < 1) return "slots must be >= 0 and below 2^31, heads >= 1";
+  if (st->heads > 65535 || b->B > 65535) return "heads and B must be at most 65535";
+  if (st->dim_k < 16 || st->dim_k > 256 || st->dim_k % 16 || st->dim_v < 16 || st->dim_v > 256 || st->dim_v % 16)
+    return "dim_k and dim_v must be multiples of 16, at most 256";
+  if (qk_heads < 1 || st->heads % qk_heads) return "qk_heads must divide heads";
+  if (b->B < 0 || b->T < 0 || b->T >= kBig) return "B and T must be >= 0 and below 2^31";
+  if (b->max_new < 0 || b->max_new >= kBig) return "max_new must be >= 0 and below 2^31";
+  if (b->T > 0 && b->max_new < 1) return "max_new is 0, but there are new tokens";
+  if (b->T > 0 && b->B < 1) return "new tokens of no sequence";
+  if (st->slots > kMaxElems / (st->heads * st->dim_k * st->dim_v)) return "the states exceed 2^40 elements";
+  return nullptr;
 }
 
 // ---------------------------------------------------------------- cache
@@ -170,8 +271,7 @@ int c3c_quantize_rows(c3c_ctx* ctx, int64_t T, int64_t C, int64_t ld_x, int dtyp
 
 int c3c_linear_i8_workspace_bytes(const c3c_linear_desc* d, size_t* bytes) {
   if (!bytes || check_linear(d)) return C3C_E_INVAL;
-  const LinearSpace s = linear_space(*d);
-  *bytes = static_cast<size_t>(s.part_at + s.plan.part_bytes);
+  *bytes = linear_bytes(*d, 1);
   return C3C_OK;
 }
 
@@ -180,63 +280,47 @@ int c3c_linear_i8(c3c_ctx* ctx, const c3c_linear_desc* d, const void* x, const f
   if (!ctx) return C3C_E_INVAL;
   const char* why = check_linear(d);
   if (why) return fail(ctx, C3C_E_INVAL, why);
-  const bool i8 = d->x_dtype == C3C_DTYPE_I8;
-  const int xs = i8 ? 1 : elem_bytes(d->x_dtype), ys = elem_bytes(d->y_dtype);
-  if (i8 ? !x_scale && d->M > 0 : x_scale != nullptr)
-    return fail(ctx, C3C_E_INVAL, "x_scale goes with int8 x, and with it alone");
-  const Span in[] = {{"x", x, extent(d->M, d->K, d->ld_x) * xs, xs},
-                     {"x_scale", x_scale, x_scale ? d->M * 4 : 0, 4},
-                     {"w", w, d->N * d->K, 1},
-                     {"w_scale", w_scale, d->N * 4, 4},
-                     {"bias", bias, bias ? d->N * 4 : 0, 4}};
-  const Span out[] = {{"y", y, d->M * d->N * ys, ys}};
-  why = check_spans(in, 5);
-  if (!why) why = check_spans(out, 1);
-  if (!why) why = check_overlap(in, 5, out, 1, ctx->ws, static_cast<int64_t>(ctx->ws_bytes));
+  return run_linear(ctx, *d, LinearEpilogue(), x, x_scale, w, w_scale, bias, y, stream);
+}
+
+int c3c_linear_i8_epilogue(c3c_ctx* ctx, const c3c_linear_desc* d, const c3c_epilogue* e,
+                           const void* x, const float* x_scale, const int8_t* w,
+                           const float* w_scale, const float* bias, void* y, void* stream) {
+  if (!ctx) return C3C_E_INVAL;
+  const char* why = check_linear(d);
+  if (!why && !e) why = "epilogue is NULL";
+  if (!why && !known_act(e->act)) why = "unknown act";
+  if (!why && !std::isfinite(e->alpha)) why = "alpha must be finite";
+  if (!why && e->gate && e->rows_per_gate < 1) why = "rows_per_gate must be >= 1";
   if (why) return fail(ctx, C3C_E_INVAL, why);
-  const LinearSpace sp = linear_space(*d);
-  const int64_t have = static_cast<int64_t>(ctx->ws_bytes);
-  if (sp.rows_bytes > have)
-    return fail(ctx, C3C_E_INVAL, "the context's workspace is smaller than the quantised rows need");
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  if (!i8 && linear_quantises(d->M, d->K))
-    return done(ctx, launch_linear_float(d->M, d->N, d->K, x, d->ld_x, d->x_dtype, w, w_scale, bias, y, d->y_dtype, s));
-  unsigned char* ws = static_cast<unsigned char*>(ctx->ws);
-  const int8_t* rows = static_cast<const int8_t*>(x);
-  int64_t ld = d->ld_x;
-  if (!i8 && d->M > 0) {
-    int8_t* q = reinterpret_cast<int8_t*>(ws);
-    float* scale = reinterpret_cast<float*>(ws + sp.scale_at);
-    const hipError_t e = launch_quantize_rows(d->M, d->K, d->ld_x, d->x_dtype, x, q, sp.ldq, scale, s);
-    if (e != hipSuccess) return done(ctx, e);
-    rows = q;
-    x_scale = scale;
-    ld = sp.ldq;
-  }
-  const int8_t* weights = w;
-  int64_t K = d->K;
-  if (sp.pads_end > sp.w_at && sp.pads_end <= have) {
-    // both operands in rows of whole 16 bytes, zero past K
-    hipError_t e = hipSuccess;
-    if (sp.x_at > sp.w_at) {
-      int8_t* to = reinterpret_cast<int8_t*>(ws + sp.w_at);
-      e = launch_pad_rows(w, d->N, d->K, d->K, to, sp.ldq, s);
-      weights = to;
-      K = sp.ldq;
-    }
-    if (e == hipSuccess && sp.pads_end > sp.x_at) {
-      int8_t* to = reinterpret_cast<int8_t*>(ws + sp.x_at);
-      e = launch_pad_rows(rows, d->M, d->K, ld, to, sp.ldq, s);
-      rows = to;
-      ld = sp.ldq;
-    }
-    if (e != hipSuccess) return done(ctx, e);
-  }
-  int32_t* part = sp.plan.splits > 1 && sp.part_at + sp.plan.part_bytes <= have
-                      ? reinterpret_cast<int32_t*>(ws + sp.part_at)
-                      : nullptr;
-  return done(ctx, launch_linear_i8(d->M, d->N, K, rows, ld, x_scale, weights, w_scale, bias, y, d->y_dtype,
-                                    sp.plan, part, s));
+  LinearEpilogue le;
+  le.kind = e->act != C3C_ACT_NONE || e->gate || e->residual ? LinearEpilogue::kEpilogue : LinearEpilogue::kPlain;
+  le.act = e->act;
+  le.alpha = e->alpha;
+  // rows of M < 2^31 tokens: as many as that share a row of gates as all
+  le.rows_per_gate = static_cast<uint32_t>(!e->gate ? 1 : e->rows_per_gate < kBig ? e->rows_per_gate : kBig);
+  le.gate = e->gate;
+  le.residual = e->residual;
+  return run_linear(ctx, *d, le, x, x_scale, w, w_scale, bias, y, stream);
+}
+
+int c3c_gated_linear_i8_workspace_bytes(const c3c_linear_desc* d, size_t* bytes) {
+  if (!bytes || check_gated(d)) return C3C_E_INVAL;
+  *bytes = linear_bytes(*d, 2);
+  return C3C_OK;
+}
+
+int c3c_gated_linear_i8(c3c_ctx* ctx, const c3c_linear_desc* d, int act, const void* x,
+                        const float* x_scale, const int8_t* w, const float* w_scale,
+                        const float* bias, void* y, void* stream) {
+  if (!ctx) return C3C_E_INVAL;
+  const char* why = check_gated(d);
+  if (!why && !known_act(act)) why = "unknown act";
+  if (why) return fail(ctx, C3C_E_INVAL, why);
+  LinearEpilogue le;
+  le.kind = LinearEpilogue::kGated;
+  le.act = act;
+  return run_linear(ctx, *d, le, x, x_scale, w, w_scale, bias, y, stream);
 }
 
 int c3c_norm_gate(c3c_ctx* ctx, const c3c_norm_desc* d, const void* h, const void* y,
@@ -354,6 +438,50 @@ int c3c_paged_attention(c3c_ctx* ctx, const c3c_kv_cache* cache, const c3c_kv_ba
   AttendArgs a{*cache, *batch, q, out, lse, static_cast<float*>(ctx->ws), q_heads, ld_q, window, scale, causal};
   if (plan.part_bytes > static_cast<int64_t>(ctx->ws_bytes)) plan = AttendPlan{};
   return done(ctx, launch_attend(a, dtype, plan, static_cast<hipStream_t>(stream)));
+}
+
+int c3c_linear_attention_workspace_bytes(const c3c_state_cache* states, const c3c_kv_batch* batch,
+                                         int dtype, int64_t qk_heads, size_t* bytes) {
+  if (!bytes || check_recur(states, batch, dtype, qk_heads)) return C3C_E_INVAL;
+  *bytes = static_cast<size_t>(plan_recur(*states, *batch, dtype).bytes);
+  return C3C_OK;
+}
+
+int c3c_linear_attention(c3c_ctx* ctx, const c3c_state_cache* states, const c3c_kv_batch* batch,
+                         const int32_t* slot, int dtype, int64_t qk_heads, const void* q,
+                         int64_t ld_q, const void* k, int64_t ld_k, const void* v, int64_t ld_v,
+                         const float* log_decay, int64_t ld_decay, float scale, void* out,
+                         void* stream) {
+  if (!ctx) return C3C_E_INVAL;
+  const char* why = check_recur(states, batch, dtype, qk_heads);
+  if (why) return fail(ctx, C3C_E_INVAL, why);
+  const int es = elem_bytes(dtype);
+  const int64_t T = batch->T, heads = states->heads, qk = qk_heads * states->dim_k, vo = heads * states->dim_v;
+  if (ld_q < qk || ld_k < qk || ld_v < vo || ld_q >= kBig || ld_k >= kBig || ld_v >= kBig)
+    return fail(ctx, C3C_E_INVAL, "a token stride is less than its heads or exceeds 2^31");
+  if (ld_decay != 0 && (ld_decay < heads || ld_decay >= kBig))
+    return fail(ctx, C3C_E_INVAL, "ld_decay must be 0 or at least heads, and below 2^31");
+  if (!std::isfinite(scale)) return fail(ctx, C3C_E_INVAL, "scale must be finite");
+  if (extent(T, qk, ld_q) < 0 || extent(T, qk, ld_k) < 0 || extent(T, vo, ld_v) < 0 || extent(T, vo, vo) < 0)
+    return fail(ctx, C3C_E_INVAL, "a tensor exceeds 2^40 elements");
+  const Span in[] = {{"cu", batch->cu, batch->B > 0 ? (batch->B + 1) * 4 : 0, 4},
+                     {"len", batch->len, batch->B * 4, 4},
+                     {"slot", slot, slot ? batch->B * 4 : 0, 4},
+                     {"q", q, extent(T, qk, ld_q) * es, es},
+                     {"k", k, extent(T, qk, ld_k) * es, es},
+                     {"v", v, extent(T, vo, ld_v) * es, es},
+                     {"log_decay", log_decay, T == 0 ? 0 : ld_decay ? extent(T, heads, ld_decay) * 4 : heads * 4, 4}};
+  const Span o[] = {{"state", states->state, states->slots * heads * states->dim_k * states->dim_v * 4, 4},
+                    {"out", out, T * vo * es, es}};
+  why = check_spans(in, 7);
+  if (!why) why = check_spans(o, 2);
+  if (!why) why = check_overlap(in, 7, o, 2, ctx->ws, static_cast<int64_t>(ctx->ws_bytes));
+  if (why) return fail(ctx, C3C_E_INVAL, why);
+  RecurPlan plan = plan_recur(*states, *batch, dtype);
+  if (plan.bytes > static_cast<int64_t>(ctx->ws_bytes)) plan = RecurPlan{};
+  const RecurArgs a{*states, *batch, slot, q, k, v, log_decay, out, static_cast<float*>(ctx->ws), qk_heads, ld_q, ld_k, ld_v,
+                    ld_decay, scale};
+  return done(ctx, launch_recur(a, dtype, plan, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -9,6 +9,13 @@ chunks the cached Conv3D layers decode (``include/c3c_tokens.h`` states each):
     paged_attention  attention over that cache
     norm_gate        norm after a block, gate, scaled residual, norm before the next
 
+and those that a layer has whose memory is a state of constant size
+(``include/c3c_layers.h``):
+
+    linear_attention  linear attention with a decay for each head
+    linear_i8         also with an activation, a gate and a residual in its epilogue
+    gated_linear_i8   both projections of a gated feed-forward block in one product
+
 As in :mod:`.c3c`, every step runs in the HIP library on torch's current
 stream (or ``stream``), errors are :class:`.c3c.C3CError`, outputs are
 allocated with torch where they are not given, and a call uses the workspace
@@ -32,6 +39,7 @@ DTYPES = dict(c3c.DTYPES, i8=16)
 _NAMES = {torch.bfloat16: "bf16", torch.float16: "f16", torch.float32: "f32"}
 _TORCH = {n: d for d, n in _NAMES.items()}
 PAIRS = {"half": 0, "next": 1}
+ACTS = {"none": 0, "silu": 1, "gelu": 2, "gelu_tanh": 3}
 
 _vp, _i64, _int, _f32, _P = C.c_void_p, C.c_int64, C.c_int, C.c_float, C.POINTER
 
@@ -60,6 +68,14 @@ class _RopeDesc(C.Structure):
                [("pairs", C.c_int32), ("reserved", C.c_int32)]
 
 
+class _StateDesc(C.Structure):
+    _fields_ = [("state", _vp)] + [(n, _i64) for n in ("slots", "heads", "dim_k", "dim_v")]
+
+
+class _Epilogue(C.Structure):
+    _fields_ = [("gate", _vp), ("residual", _vp), ("rows_per_gate", _i64), ("alpha", _f32), ("act", C.c_int32)]
+
+
 lib.c3c_quantize_rows.argtypes = [_vp, _i64, _i64, _i64, _int, _vp, _vp, _vp, _vp]
 lib.c3c_linear_i8_workspace_bytes.argtypes = [_P(LinearDesc), _P(C.c_size_t)]
 lib.c3c_linear_i8.argtypes = [_vp, _P(LinearDesc)] + [_vp] * 7
@@ -70,6 +86,13 @@ lib.c3c_paged_attention_workspace_bytes.argtypes = [_P(_CacheDesc), _P(_BatchDes
                                                     _P(C.c_size_t)]
 lib.c3c_paged_attention.argtypes = [_vp, _P(_CacheDesc), _P(_BatchDesc), _int, _i64, _vp, _i64, _f32, _int, _i64, _vp,
                                     _vp, _vp]
+
+lib.c3c_linear_i8_epilogue.argtypes = [_vp, _P(LinearDesc), _P(_Epilogue)] + [_vp] * 7
+lib.c3c_gated_linear_i8_workspace_bytes.argtypes = [_P(LinearDesc), _P(C.c_size_t)]
+lib.c3c_gated_linear_i8.argtypes = [_vp, _P(LinearDesc), _int] + [_vp] * 7
+lib.c3c_linear_attention_workspace_bytes.argtypes = [_P(_StateDesc), _P(_BatchDesc), _int, _i64, _P(C.c_size_t)]
+lib.c3c_linear_attention.argtypes = [_vp, _P(_StateDesc), _P(_BatchDesc), _vp, _int, _i64, _vp, _i64, _vp, _i64, _vp, _i64,
+                                     _vp, _i64, _f32, _vp, _vp]
 
 
 # A call of a single token takes a few microseconds on the device: what the
@@ -141,28 +164,83 @@ def linear_i8_workspace_bytes(M: int, N: int, K: int, x_dtype: str = "bf16", y_d
     return n.value
 
 
-def linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=None, stream=None):
+def _linear_args(x, x_scale, out, out_dtype):
+    """(M, K, row stride, x's dtype, y's dtype) of a product's activations and output."""
+    xd = "i8" if x.dtype == torch.int8 else _float_dtype(x, "x")
+    ld = _rows(x, "x")
+    yd = out_dtype or (_float_dtype(out, "out") if out is not None else "bf16" if xd == "i8" else xd)
+    return x.shape[0], x.shape[1], ld, xd, yd
+
+
+def _act(act):
+    if act not in ACTS:
+        raise ValueError(f"act is {act!r}, expected one of {', '.join(ACTS)}")
+    return ACTS[act]
+
+
+def linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=None, stream=None, *, act="none",
+              residual=None, gate=None, alpha=1.0, rows_per_gate=1):
     """y (M, N) = x (M, K) times w (N, K) int8 with w_scale (N,) and bias (N,)
     in fp32.  x is bf16, f16 or f32 (quantised in the call; the context needs
     linear_i8_workspace_bytes), or int8 with x_scale (M,).  Rows of x may be
-    strided.  ``out_dtype`` ("bf16", "f16", "f32") defaults to x's, or bf16."""
-    i8 = x.dtype == torch.int8
-    xd = "i8" if i8 else _float_dtype(x, "x")
-    ld = _rows(x, "x")
-    M, K = x.shape
+    strided.  ``out_dtype`` ("bf16", "f16", "f32") defaults to x's, or bf16.
+
+    With an epilogue y = alpha residual + gate act(that), rounded once: ``act``
+    "none", "silu", "gelu" (by erf) or "gelu_tanh"; residual (M, N) and gate
+    (groups, N), one row for ``rows_per_gate`` tokens, of y's dtype.  ``out`` may
+    be the residual."""
+    M, K, ld, xd, yd = _linear_args(x, x_scale, out, out_dtype)
     N = w.shape[0]
-    yd = out_dtype or (_float_dtype(out, "out") if out is not None else "bf16" if i8 else xd)
     ydt = _TORCH[yd]
     if out is None:
         out = x.new_empty((M, N), dtype=ydt)
     d = LinearDesc(M, N, K, ld, DTYPES[xd], DTYPES[yd])
-    st = lib.c3c_linear_i8(
-        ctx._h, C.byref(d), _addr(x, "x"), None if x_scale is None else _check(x_scale, "x_scale", torch.float32, (M,)),
-        _check(w, "w", torch.int8, (N, K)), _check(w_scale, "w_scale", torch.float32, (N,)),
-        None if bias is None else _check(bias, "bias", torch.float32, (N,)), _check(out, "out", ydt, (M, N)),
-        _stream(stream, x))
+    args = (_addr(x, "x"), None if x_scale is None else _check(x_scale, "x_scale", torch.float32, (M,)),
+            _check(w, "w", torch.int8, (N, K)), _check(w_scale, "w_scale", torch.float32, (N,)),
+            None if bias is None else _check(bias, "bias", torch.float32, (N,)), _check(out, "out", ydt, (M, N)),
+            _stream(stream, x))
+    if act == "none" and residual is None and gate is None:
+        st = lib.c3c_linear_i8(ctx._h, C.byref(d), *args)
+        if st:
+            _raise(st, ctx, "c3c_linear_i8")
+        return out
+    groups = -(-M // rows_per_gate) if rows_per_gate > 0 else 0
+    e = _Epilogue(None if gate is None else _check(gate, "gate", ydt, (groups, N)),
+                  None if residual is None else _check(residual, "residual", ydt, (M, N)), rows_per_gate, alpha, _act(act))
+    st = lib.c3c_linear_i8_epilogue(ctx._h, C.byref(d), C.byref(e), *args)
     if st:
-        _raise(st, ctx, "c3c_linear_i8")
+        _raise(st, ctx, "c3c_linear_i8_epilogue")
+    return out
+
+
+def gated_linear_i8_workspace_bytes(M: int, N: int, K: int, x_dtype: str = "bf16", y_dtype: str = "bf16", ld_x=None) -> int:
+    """linear_i8_workspace_bytes of a gated_linear_i8 call of N output channels."""
+    n = C.c_size_t()
+    d = LinearDesc(M, N, K, K if ld_x is None else ld_x, DTYPES[x_dtype], DTYPES[y_dtype])
+    _raise(lib.c3c_gated_linear_i8_workspace_bytes(C.byref(d), C.byref(n)), what="c3c_gated_linear_i8_workspace_bytes")
+    return n.value
+
+
+def gated_linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=None, *, act="silu", stream=None):
+    """y (M, N) = act(x w_g^T + b_g) * (x w_u^T + b_u), the first half of a gated
+    feed-forward block: w (2 N, K) int8 holds the gate's rows, then the others,
+    w_scale and bias (2 N,) fp32.  x, x_scale, out and out_dtype as linear_i8
+    takes them; the context needs gated_linear_i8_workspace_bytes."""
+    M, K, ld, xd, yd = _linear_args(x, x_scale, out, out_dtype)
+    rows = w.shape[0]
+    if rows % 2:
+        raise ValueError(f"w has {rows} rows, expected two halves")
+    N, ydt = rows // 2, _TORCH[yd]
+    if out is None:
+        out = x.new_empty((M, N), dtype=ydt)
+    d = LinearDesc(M, N, K, ld, DTYPES[xd], DTYPES[yd])
+    st = lib.c3c_gated_linear_i8(
+        ctx._h, C.byref(d), _act(act), _addr(x, "x"),
+        None if x_scale is None else _check(x_scale, "x_scale", torch.float32, (M,)), _check(w, "w", torch.int8, (rows, K)),
+        _check(w_scale, "w_scale", torch.float32, (rows,)), None if bias is None else _check(bias, "bias", torch.float32, (rows,)),
+        _check(out, "out", ydt, (M, N)), _stream(stream, x))
+    if st:
+        _raise(st, ctx, "c3c_gated_linear_i8")
     return out
 
 
@@ -336,4 +414,65 @@ def paged_attention(ctx, cache: KVCache, batch: Batch, q, *, scale=None, causal:
         None if lse is None else _check(lse, "lse", torch.float32, (T, qh)), _stream(stream, q))
     if st:
         _raise(st, ctx, "c3c_paged_attention")
+    return out
+
+
+# ---------------------------------------------------------------- linear attention
+
+class StateCache:
+    """The states of linear attention: fp32 (slots, heads, dim_k, dim_v), a slot
+    for each sequence.  Holds its tensor."""
+
+    def __init__(self, state):
+        if state.dim() != 4:
+            raise ValueError("state must be (slots, heads, dim_k, dim_v)")
+        self.state = state
+        slots, self.heads, self.dim_k, self.dim_v = state.shape
+        self._d = _StateDesc(_check(state, "state", torch.float32, state.shape), *state.shape)
+
+    @classmethod
+    def empty(cls, slots: int, heads: int, dim_k: int, dim_v: int, device="cuda"):
+        return cls(torch.zeros((slots, heads, dim_k, dim_v), dtype=torch.float32, device=device))
+
+
+def linear_attention_workspace_bytes(states: StateCache, batch: Batch, q) -> int:
+    """Workspace bytes with which a call on these queries may split its
+    sequences."""
+    n = C.c_size_t()
+    _raise(lib.c3c_linear_attention_workspace_bytes(C.byref(states._d), batch._of(q.shape[0]), DTYPES[_float_dtype(q, "q")],
+                                                    q.shape[1], C.byref(n)), what="c3c_linear_attention_workspace_bytes")
+    return n.value
+
+
+def linear_attention(ctx, states: StateCache, batch: Batch, q, k, v, log_decay, *, slots=None, scale=None, out=None, stream=None):
+    """Linear attention with a decay for each head: for every sequence's new
+    tokens in order S = exp(log_decay) S + k v^T, out = scale q S, with S updated
+    in place.  q, k (T, qk_heads, dim_k), v (T, heads, dim_v), tokens may be
+    strided; groups of heads share a query and key head.  log_decay fp32 (heads,)
+    or (T, heads), rows may be strided.  The batch's page table is not used.
+    ``slots`` (B,) int32: where each sequence's state lies (default: in order); a
+    sequence whose tokens are all in this call begins at zero.  scale defaults to
+    dim_k ** -0.5.  Returns out (T, heads, dim_v)."""
+    dtype = _float_dtype(q, "q")
+    T, qk_heads, _ = q.shape
+    dt, heads = q.dtype, states.heads
+    pq, ldq = _heads(q, "q", dt, T, qk_heads, states.dim_k)
+    pk, ldk = _heads(k, "k", dt, T, qk_heads, states.dim_k)
+    pv, ldv = _heads(v, "v", dt, T, heads, states.dim_v)
+    if log_decay.dtype is not torch.float32:
+        raise ValueError(f"log_decay has dtype {log_decay.dtype}, expected {torch.float32}")
+    if log_decay.dim() == 1:
+        pg, ldg = _check(log_decay, "log_decay", torch.float32, (heads,)), 0
+    else:
+        if log_decay.shape != (T, heads):
+            raise ValueError(f"log_decay has shape {tuple(log_decay.shape)}, expected {(heads,)} or {(T, heads)}")
+        pg, ldg = _addr(log_decay, "log_decay"), _rows(log_decay, "log_decay")
+    if out is None:
+        out = q.new_empty((T, heads, states.dim_v))
+    ps = None if slots is None else _check(slots, "slots", torch.int32, batch.lens.shape)
+    st = lib.c3c_linear_attention(
+        ctx._h, C.byref(states._d), batch._of(T), ps, DTYPES[dtype], qk_heads, pq, ldq, pk, ldk, pv, ldv, pg, ldg,
+        states.dim_k ** -0.5 if scale is None else scale, _check(out, "out", dt, (T, heads, states.dim_v)), _stream(stream, q))
+    if st:
+        _raise(st, ctx, "c3c_linear_attention")
     return out
