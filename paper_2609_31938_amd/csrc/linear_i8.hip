@@ -372,9 +372,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
   const int lrow = lane / (BK / 16), lpiece = spread<BK>(lrow, lane % (BK / 16));
   const __amdgpu_buffer_rsrc_t wrs = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<int8_t*>(wb), 0, static_cast<int>(nrows * a.K), 0x00020000);
-  const int8_t* wb2 = wb + (EPI == GATED ? a.N * a.K : 0);  // the second half's rows
-  const __amdgpu_buffer_rsrc_t wrs2 = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<int8_t*>(wb2), 0, static_cast<int>(nrows * a.K), 0x00020000);
+  const int64_t half = EPI == GATED ? a.N * a.K : 0;  // to the rows of the second half
   const __amdgpu_buffer_rsrc_t xrs = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<int8_t*>(xb), 0, static_cast<int>((mrows - 1) * a.ldx + a.K), 0x00020000);
   tok_i32x4 staged[LOADS];  // !AL
@@ -392,11 +390,20 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
       // past K: a sign bit takes the offset out of every buffer
       const int off = (rr * ld + k) | ((static_cast<int>(a.K) - 1 - k) & static_cast<int>(0x80000000u));
       lds_void* to = (lds_void*)(lds + buf * ROWS * BK + row * BK);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(isw ? second ? wrs2 : wrs : xrs, to, 16, off, 0, 0, 0);
+      if constexpr (EPI == GATED) {
+        // (a choice among three variables is compiled into scratch memory)
+        const int8_t* base = isw ? wb + (second ? half : 0) : xb + 0;
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<int8_t*>(base), 0, static_cast<int>(isw ? nrows * a.K : (mrows - 1) * a.ldx + a.K), 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, to, 16, off, 0, 0, 0);
+      } else {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(isw ? wrs : xrs, to, 16, off, 0, 0, 0);
+      }
     } else {
       const int64_t ld = isw ? a.K : a.ldx;
       const bool ok = rr < (isw ? nrows : mrows);
-      staged[i] = piece<false>((isw ? second ? wb2 : wb : xb) + (ok ? rr * ld + k : 0), ok ? a.K - k : 0);
+      const int8_t* base = isw ? wb + (second ? half : 0) : xb + 0;
+      staged[i] = piece<false>(base + (ok ? rr * ld + k : 0), ok ? a.K - k : 0);
     }
   };
   auto settle = [&](int st) __attribute__((always_inline)) {  // !AL
@@ -477,7 +484,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
   C3C_VMCNT(0);  // nothing is on its way into LDS when the workgroup ends
 
   float xs[MT];
-  if (!a.part) {
+  if (EPI == PLAIN && !a.part) {
 #pragma unroll
     for (int j = 0; j < MT; ++j) {
       const int64_t m = m0 + wm + j * 16 + r;
@@ -488,12 +495,14 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
 #pragma unroll
   for (int i = 0; i < OT; ++i) {
     const int64_t n = n0 + wn / H + i * 16 + g * 4;
-    if (n >= a.N) continue;
-    if (a.part) {
+    if (n >= a.N || (EPI != PLAIN && !a.part)) continue;
+    Channels<EPI> c;
+    if (!a.part) c = channels<EPI>(a, n);
 #pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        const int64_t m = m0 + wm + j * 16 + r;
-        if (m >= a.M) continue;
+    for (int j = 0; j < MT; ++j) {
+      const int64_t m = m0 + wm + j * 16 + r;
+      if (m >= a.M) continue;
+      if (a.part) {
 #pragma unroll
         for (int h = 0; h < H; ++h) {
           int32_t* p = a.part + ((split * a.M + m) * H + h) * a.N + n;
@@ -504,24 +513,62 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
               if (n + e < a.N) p[e] = acc[i + h * OT][j][e];
           }
         }
+      } else if constexpr (EPI == PLAIN) {
+        const tok_i32x4 v[1] = {acc[i][j]};
+        put4<EPI>(a, m, n, v, xs[j], c, Beside());
       }
-    } else {
-      const Channels<EPI> c = channels<EPI>(a, n);
-      Beside x[MT];  // asked for together: y may be the residual
+    }
+  }
+  if constexpr (EPI != PLAIN) {
+    if (a.part) return;
+    // The sums change places in LDS, where a wave now has room for 64 tokens of
+    // its part: a lane takes 8 channels of one token after another, whose
+    // residual, gates and results are whole 16-byte pieces.  In place, four
+    // channels of many tokens a lane, the functions are unrolled 128 times and
+    // the sums end in scratch memory (32760 x 5120 x 5120 onto a residual: 1564 us).
+    constexpr int ROOM = WM < 64 ? WM : 64, OC = WN / H, LPR = OC / 8, RPI = 64 / LPR;
+    constexpr int U = ROOM / RPI < 2 ? 1 : 2;  // tokens of a lane at once
+    static_assert(NW * ROOM * WN * 4 <= static_cast<int>(sizeof(lds)) && ROOM % (RPI * U) == 0, "room, whole rounds");
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // no wave reads a stage any more
+    int8_t* const mine = lds + wave * ROOM * WN * 4;
+    const int c8 = lane % LPR;
+    const int64_t n = n0 + wn / H + c8 * 8;
+    Channels<EPI> c[2] = {channels<EPI>(a, n < a.N ? n : 0), channels<EPI>(a, n + 4 < a.N ? n + 4 : 0)};
 #pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        const int64_t m = m0 + wm + j * 16 + r;
-        x[j] = beside<EPI>(a, m < a.M ? m : a.M - 1, n);
+    for (int first = 0; first < MT; first += ROOM / 16) {
+#pragma unroll
+      for (int j = 0; j < ROOM / 16; ++j)
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+          *reinterpret_cast<tok_i32x4*>(mine + (j * 16 + r) * WN * 4 + ((i * 4 + g) ^ (r & 7)) * 16) = acc[i][first + j];
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+      for (int it = 0; it < ROOM / RPI; it += U) {
+        Beside x[U][2];
+        int64_t m[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          m[u] = m0 + wm + first * 16 + (it + u) * RPI + lane / LPR;
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+            if (m[u] < a.M && n + 4 * p < a.N) x[u][p] = beside<EPI>(a, m[u], n + 4 * p);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (m[u] >= a.M) continue;
+          const float s = a.x_scale[m[u]];
+          const int row = (it + u) * RPI + lane / LPR;
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            tok_i32x4 v[H];
+#pragma unroll
+            for (int h = 0; h < H; ++h)
+              v[h] = *reinterpret_cast<const tok_i32x4*>(mine + row * WN * 4 + ((h * OC / 4 + c8 * 2 + p) ^ (row & 7)) * 16);
+            if (n + 4 * p < a.N) put4<EPI>(a, m[u], n + 4 * p, v, s, c[p], x[u][p]);
+          }
+        }
       }
-#pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        const int64_t m = m0 + wm + j * 16 + r;
-        if (m >= a.M) continue;
-        tok_i32x4 v[H];
-#pragma unroll
-        for (int h = 0; h < H; ++h) v[h] = acc[i + h * OT][j];
-        put4<EPI>(a, m, n, v, xs[j], c, x[j]);
-      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
   }
 }
