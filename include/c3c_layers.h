@@ -49,7 +49,7 @@ typedef struct c3c_state_cache {
  * whose slot is outside [0, slots) begins at zero and its state is not stored.
  * Slots of a call must differ.
  *   q, k: [T][qk_heads][dim_k], v: [T][heads][dim_v]; ld_q, ld_k, ld_v elements
- *   between tokens; head h reads query and key head h / (heads / qk_heads).
+ *   between tokens, below 2^23; head h reads query and key head h / (heads / qk_heads).
  *   log_decay (g): fp32, [heads] with ld_decay 0, or [T][heads] with ld_decay
  *   elements between tokens.  At most 0; -infinity forgets.  A decay is held to
  *   exp(-110), which is 0 in fp32.  Larger ones are taken as they come.

@@ -196,44 +196,47 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
   const int cols = a.dim_v - c0 < DVS ? a.dim_v - c0 : DVS;
 
   // ---- a chunk's inputs: asked for one chunk ahead, in registers until their place in LDS is free
-  struct Piece {
-    store v[VEC];
-  };
-  Piece rq[STATES ? 1 : K::KP], rk[K::KP], rv[K::VP];
+  tok_u32x4 rq[STATES ? 1 : K::KP], rk[K::KP], rv[K::VP];
   float rg = 0.f;
+  // Rows past the last one and columns past the width are read from others, and
+  // made zero when they are placed: a load behind a condition is waited for
+  // before the next.  The offsets in a chunk are 32 bits.
+  auto row_of = [&](int i, int per) __attribute__((always_inline)) { return (i * 256 + tid) / per; };
+  auto col_of = [&](int per) __attribute__((always_inline)) { return tid % per * VEC; };
+  static_assert(256 % (DK / VEC) == 0 && 256 % (DVS / VEC) == 0, "a thread's pieces lie in one column");
+  auto get = [&](const store* p, int64_t ld, int rows, int i, int per, int width) __attribute__((always_inline)) {
+    const int row = row_of(i, per), col = col_of(per);
+    const uint32_t off = static_cast<uint32_t>(row < rows ? row : rows - 1) * (static_cast<uint32_t>(ld) * sizeof(store)) +
+                         (col < width ? col : 0) * sizeof(store);
+    tok_u32x4 x;
+    __builtin_memcpy(&x, reinterpret_cast<const char*>(p) + off, 16);
+    return x;
+  };
   auto ask = [&](int64_t t) __attribute__((always_inline)) {
-    auto get = [&](const store* p, int64_t ld, int i, int per, int width) __attribute__((always_inline)) {
-      const int at = i * 256 + tid, row = at / per, col = at % per * VEC;
-      Piece x;
-      if (t + row < end && col < width) {
-        __builtin_memcpy(x.v, p + (t + row) * ld + col, 16);
-      } else {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) x.v[e] = store(0);
-      }
-      return x;
-    };
+    const int rows = end - t < C ? static_cast<int>(end - t) : C;
     if constexpr (!STATES) {
 #pragma unroll
-      for (int i = 0; i < K::KP; ++i) rq[i] = get(qp, a.ld_q, i, DK / VEC, a.dim_k);
+      for (int i = 0; i < K::KP; ++i) rq[i] = get(qp + t * a.ld_q, a.ld_q, rows, i, DK / VEC, a.dim_k);
     }
 #pragma unroll
-    for (int i = 0; i < K::KP; ++i) rk[i] = get(kp, a.ld_k, i, DK / VEC, a.dim_k);
+    for (int i = 0; i < K::KP; ++i) rk[i] = get(kp + t * a.ld_k, a.ld_k, rows, i, DK / VEC, a.dim_k);
 #pragma unroll
-    for (int i = 0; i < K::VP; ++i) rv[i] = get(vp, a.ld_v, i, DVS / VEC, cols);
-    if (wave == 0) rg = lane < C && t + lane < end ? a.decay[(t + lane) * a.ld_decay + h] : 0.f;
+    for (int i = 0; i < K::VP; ++i) rv[i] = get(vp + t * a.ld_v, a.ld_v, rows, i, DVS / VEC, cols);
+    if (wave == 0) rg = a.decay[(t + (lane < rows ? lane : rows - 1)) * a.ld_decay + h];
   };
-  auto put = [&](const Piece& x, int at, int plane, int pitch, int i, int per) __attribute__((always_inline)) {
+  auto put = [&](tok_u32x4 x, int at, int plane, int pitch, int i, int per) __attribute__((always_inline)) {
     const int p = i * 256 + tid, row = p / per, col = p % per * VEC;
     unsigned char* to = lds + at + row * pitch + col * 2;
     if constexpr (NI == 1) {
-      __builtin_memcpy(to, x.v, 16);
+      *reinterpret_cast<tok_u32x4*>(to) = x;
     } else {
+      store v[VEC];
+      __builtin_memcpy(v, &x, 16);
       uint32_t w[NI][VEC / 2];
 #pragma unroll
       for (int e = 0; e < VEC; e += 2) {
         uint32_t t[NI];
-        split2<NI>(E::widen(x.v[e]), E::widen(x.v[e + 1]), t);
+        split2<NI>(E::widen(v[e]), E::widen(v[e + 1]), t);
 #pragma unroll
         for (int n = 0; n < NI; ++n) w[n][e / 2] = t[n];
       }
@@ -241,7 +244,20 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
       for (int n = 0; n < NI; ++n) __builtin_memcpy(__builtin_assume_aligned(to + n * plane, VEC * 2), w[n], VEC * 2);
     }
   };
-  auto place = [&]() __attribute__((always_inline)) {
+  auto place = [&](int64_t t) __attribute__((always_inline)) {
+    const int rows = end - t < C ? static_cast<int>(end - t) : C;
+    if (rows < C || a.dim_k < DK || cols < DVS) {
+      const tok_u32x4 none = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int i = 0; i < K::KP; ++i) {
+        const bool ok = row_of(i, DK / VEC) < rows && col_of(DK / VEC) < a.dim_k;
+        if constexpr (!STATES) rq[i] = ok ? rq[i] : none;
+        rk[i] = ok ? rk[i] : none;
+      }
+#pragma unroll
+      for (int i = 0; i < K::VP; ++i) rv[i] = row_of(i, DVS / VEC) < rows && col_of(DVS / VEC) < cols ? rv[i] : none;
+      rg = lane < rows ? rg : 0.f;
+    }
     if constexpr (!STATES) {
 #pragma unroll
       for (int i = 0; i < K::KP; ++i) put(rq[i], 0, C * K::QK_PITCH, K::QK_PITCH, i, DK / VEC);
@@ -291,6 +307,8 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
           S[s][t][c][e] = from && row < a.dim_k && col < a.dim_v ? from[static_cast<int64_t>(row) * a.dim_v + col] : 0.f;
         }
 
+  const int64_t lane_out = static_cast<int64_t>(r) * a.heads * a.dim_v + wc + 4 * g;
+
   ask(t0);
   if constexpr (!STATES) {
     // P above the diagonal, within the 32 keys of a step: zeros that stay
@@ -300,7 +318,7 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
     }
   }
   for (int64_t t = t0; t < end; t += C) {
-    place();
+    place(t);
     meet();
     if (t + C < end) ask(t + C);
 
@@ -345,6 +363,7 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
         for (int c = 0; c < CT; ++c) O[i][c] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
+        __builtin_amdgcn_sched_barrier(0);
         tok_bf16x8 fs[CT][NO];
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
@@ -385,6 +404,7 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
     }
 #pragma unroll
     for (int j = 0; j < JS; ++j) {
+      __builtin_amdgcn_sched_barrier(0);
       const int row = 32 * j + 8 * g;
       tok_bf16x8 fv[CT][NI], fw[CT][kStateTerms];
       float weight[8];
@@ -455,6 +475,7 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+          if (u == 0) __builtin_amdgcn_sched_barrier(0);
           tok_bf16x8 fk[NI];
 #pragma unroll
           for (int n = 0; n < NI; ++n)
@@ -466,8 +487,8 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
     if constexpr (!STATES) {
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
-        const int64_t row = t + i * 16 + r;
-        if (row >= end) continue;
+        if (t + i * 16 + r >= end) continue;
+        store* const to = static_cast<store*>(a.out) + ((t + i * 16) * a.heads + h) * a.dim_v + c0 + lane_out;
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
           const int col = wc + 16 * c + 4 * g;
@@ -475,7 +496,7 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
           store o[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) o[e] = E::narrow(O[i][c][e] * a.scale);
-          __builtin_memcpy(static_cast<store*>(a.out) + (row * a.heads + h) * a.dim_v + c0 + col, o, sizeof(o));
+          __builtin_memcpy(to + 16 * c, o, sizeof(o));
         }
       }
     }

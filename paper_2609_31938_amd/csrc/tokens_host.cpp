@@ -14,6 +14,7 @@ namespace {
 
 constexpr int64_t kBig = int64_t(1) << 31;
 constexpr int64_t kMaxElems = int64_t(1) << 40;
+constexpr int64_t kMaxStride = int64_t(1) << 23;  // of a token, in linear attention
 constexpr int64_t kMaxK = 131071;  // 128 * 128 * K stays below 2^31
 
 int elem_bytes(int dtype) {
@@ -457,8 +458,9 @@ int c3c_linear_attention(c3c_ctx* ctx, const c3c_state_cache* states, const c3c_
   if (why) return fail(ctx, C3C_E_INVAL, why);
   const int es = elem_bytes(dtype);
   const int64_t T = batch->T, heads = states->heads, qk = qk_heads * states->dim_k, vo = heads * states->dim_v;
-  if (ld_q < qk || ld_k < qk || ld_v < vo || ld_q >= kBig || ld_k >= kBig || ld_v >= kBig)
-    return fail(ctx, C3C_E_INVAL, "a token stride is less than its heads or exceeds 2^31");
+  // a chunk's offsets are 32 bits
+  if (ld_q < qk || ld_k < qk || ld_v < vo || ld_q >= kMaxStride || ld_k >= kMaxStride || ld_v >= kMaxStride)
+    return fail(ctx, C3C_E_INVAL, "a token stride is less than its heads or not below 2^23");
   if (ld_decay != 0 && (ld_decay < heads || ld_decay >= kBig))
     return fail(ctx, C3C_E_INVAL, "ld_decay must be 0 or at least heads, and below 2^31");
   if (!std::isfinite(scale)) return fail(ctx, C3C_E_INVAL, "scale must be finite");
