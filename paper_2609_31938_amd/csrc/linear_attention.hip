@@ -9,9 +9,8 @@
 // head forgets; the sums G are formed in 64 bits and kept as two floats, since
 // they may be large (a token that resets the state) next to their differences.
 //
-// chunks: a workgroup of 4 waves takes one head and up to 128 columns of S, of
-//   which every wave holds its quarter in the matrix cores' accumulators, all
-//   dim_k rows of it: the layout of an accumulator is that of an operand whose
+// chunks: a workgroup takes one head and up to 128 columns of S, of which every
+//   wave holds 16 in the matrix cores' accumulators, all dim_k rows of them: the layout of an accumulator is that of an operand whose
 //   rows are taken in another order, so S goes into the first product without
 //   passing through LDS, and no two waves share a column of out.  What the waves
 //   share is q, k and the weighted products P of queries and keys, in LDS.
@@ -132,46 +131,86 @@ __device__ inline void mfma_terms(const tok_bf16x8 (&a)[NA], const tok_bf16x8 (&
 // for the stores at the loop's end.)
 __device__ inline void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
-// The operand of 8 tokens (rows from t0 + 8 g on) by the column of this lane:
-// ds_read_b64_tr_b16 gives lane i of 16 element i % 4 of what lanes 4 e + i / 4
-// address, e = 0 .. 3.  at: where this lane reads, in the first row's place.
+// v, of which the compiler knows nothing: what is computed from it in a loop
+// stays there.  (Left to itself it forms all addresses of a chunk before the loop,
+// and keeps them in scratch memory.)
+__device__ inline int unknown(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// Operands of the matrix cores hold 8 of 32 rows a lane, in any order that both
+// share: here rows 4 g .. 4 g + 3 and those 16 further on, g = lane / 16, as an
+// accumulator's two tiles lie.  By columns (a row is a token, the lane's column
+// its lane % 16): ds_read_b64_tr_b16 gives lane i of 16 element i % 4 of what
+// lanes 4 e + i / 4 address, e = 0 .. 3.  at: where this lane reads, in the first
+// row's place.
 __device__ inline tok_bf16x8 column8(const unsigned char* at, int pitch) {
   const tok_i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
-  const tok_i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 4 * pitch));
+  const tok_i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(at + 16 * pitch));
   return __builtin_bit_cast(tok_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// By rows (the row of this lane, 8 of 32 channels from at on) ...
+__device__ inline tok_bf16x8 row8(const unsigned char* at) {
+  const tok_i16x4 lo = *reinterpret_cast<const tok_i16x4*>(at), hi = *reinterpret_cast<const tok_i16x4*>(at + 32);
+  return __builtin_bit_cast(tok_bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// ... or where a row keeps these 8 side by side (q, P): 16-byte pieces, whose
+// places change from row to row so that neither 16 rows of one piece nor a mixture
+// of two pieces, as the lanes of a 16-byte read are served, meet in a bank.
+// Place of piece g of the first 32 channels in a row; that of the s-th is the same
+// ^ 64 s.
+template <int PITCH>
+__device__ inline int piece_at(int row, int g) {
+  const int h = PITCH >= 256 ? row & 15 : PITCH == 128 ? row >> 1 & 7 : -(row >> 2) & 3;
+  return row * PITCH + ((h >> 2) << 6) + ((g ^ (h & 3)) << 4);
+}
+// Place of the four channels that are the c-th in order.
+template <int PITCH>
+__device__ inline int four_at(int row, int c) {
+  return (piece_at<PITCH>(row, c & 3) ^ ((c >> 3) << 6)) + (c >> 2 & 1) * 8;
 }
 
 // E: input type.  DK: rows of S (dim_k, filled up with zeros).  DVS: columns of
-// this workgroup.  C: tokens of a chunk.  STATES: only the state of a part.
-template <class E, int DK, int DVS, int C, bool STATES>
+// this workgroup, CT tiles of 16 a wave.  C: tokens of a chunk.  STATES: only the state of a
+// part.
+template <class E, int DK, int DVS, int CT, int C, bool STATES>
 struct Chunk {
   static constexpr int NI = Terms<E>::IN, NO = Terms<E>::OUT;
-  static constexpr int QK_PITCH = DK * 2 + 16, V_PITCH = DVS * 2 + 16, P_PITCH = C * 2 + 16;
-  static constexpr int QK_BYTES = NI * C * QK_PITCH, V_BYTES = NI * C * V_PITCH;
+  static constexpr int THREADS = DVS * 4 / CT;
+  // Bytes between rows.  Of k and v, read by columns, 8 rows of 32 bytes meet in
+  // no bank: an odd number of 32 bytes; their second 8 of 16 rows begin 16 bytes
+  // further on, so that 16 rows of 8 or 16 bytes don't either.
+  static constexpr int Q_PITCH = DK * 2, K_PITCH = DK * 2 + 32, V_PITCH = DVS * 2 + 32, P_PITCH = C * 2;
+  static constexpr int Q_BYTES = STATES ? 0 : NI * C * Q_PITCH, K_BYTES = NI * C * K_PITCH, V_BYTES = NI * C * V_PITCH;
   static constexpr int P_BYTES = STATES ? 0 : NO * C * P_PITCH;
-  static constexpr int K_AT = STATES ? 0 : QK_BYTES, V_AT = K_AT + QK_BYTES, P_AT = V_AT + V_BYTES;
-  static constexpr int W_AT = P_AT + P_BYTES;  // weights: 4 floats a token, and the chunk's
-  static constexpr int BYTES = W_AT + 4 * C * 4 + 16;
-  static constexpr int EVEC = E::VEC;
-  static constexpr int KP = C * DK / EVEC / 256, VP = C * DVS / EVEC / 256;  // 16-byte pieces a thread
-  static constexpr int CT = DVS / 64;                                         // column tiles of 16 of a wave
+  static constexpr int K_AT = Q_BYTES, V_AT = K_AT + K_BYTES;
+  static constexpr int W_AT = V_AT + V_BYTES;  // weights: 4 floats a token, and the chunk's
+  static constexpr int BUFFER = (W_AT + 4 * C * 4 + 4 + 255) / 256 * 256;
+  // Eight waves a compute unit, in one workgroup or two.  Two buffers where they
+  // fit: the products of a chunk's queries and keys are then formed beside the
+  // chunk before.
+  static constexpr int LDS = 160 * 1024 / (512 / THREADS);  // of a workgroup
+  static constexpr int BUFS = STATES || 2 * (BUFFER + P_BYTES) > LDS ? 1 : 2;
+  static constexpr int P_AT = BUFS * BUFFER, BYTES = P_AT + BUFS * P_BYTES;
+  // 16-byte pieces of q or k, of v, and how many a thread takes
+  static constexpr int K_ALL = C * DK / E::VEC, V_ALL = C * DVS / E::VEC;
+  static constexpr int KP = (K_ALL + THREADS - 1) / THREADS, VP = (V_ALL + THREADS - 1) / THREADS;
+  // waves of a SIMD: two (256 registers), for a part's state alone four (128)
+  static constexpr int MOST = STATES ? 4 : 2, FIT = 160 * 1024 / BYTES * THREADS / 256;
+  static constexpr int WAVES = FIT < MOST ? FIT : MOST;
 };
 
-template <class E, int DK, int DVS, int C, bool STATES>
-__global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1024 ? 2 : 1)) void chunks(Args a) {
-  typedef Chunk<E, DK, DVS, C, STATES> K;
+template <class E, int DK, int DVS, int CT, int C, bool STATES>
+__global__ __launch_bounds__((Chunk<E, DK, DVS, CT, C, STATES>::THREADS), (Chunk<E, DK, DVS, CT, C, STATES>::WAVES)) void chunks(Args a) {
+  typedef Chunk<E, DK, DVS, CT, C, STATES> K;
   typedef typename E::store store;
-  constexpr int NI = K::NI, NO = K::NO, CT = K::CT, VEC = E::VEC;
+  constexpr int NI = K::NI, NO = K::NO, VEC = E::VEC, THREADS = K::THREADS, NW = THREADS / 64;
   constexpr int LAST = NO - 1;
   constexpr int KS = DK / 32, JS = C / 32, RT = C / 16;
   __shared__ __align__(16) unsigned char lds[K::BYTES];
-  float* const g_hi = reinterpret_cast<float*>(lds + K::W_AT);  // G in units of log 2: its float and the rest
-  float* const g_lo = g_hi + C;
-  float* const w_q = g_lo + C;  // exp(G_i)
-  float* const w_k = w_q + C;   // exp(G_C - G_i)
-  float* const w_all = w_k + C;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int r = lane & 15, g = lane >> 4;
+  int tid = threadIdx.x;
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
 
   // workgroup -> (sequence, part, head) and slice: the slices of a head, which
   // read the same q and k, run on the same one of the 8 L2 caches
@@ -201,9 +240,9 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
   // Rows past the last one and columns past the width are read from others, and
   // made zero when they are placed: a load behind a condition is waited for
   // before the next.  The offsets in a chunk are 32 bits.
-  auto row_of = [&](int i, int per) __attribute__((always_inline)) { return (i * 256 + tid) / per; };
+  auto row_of = [&](int i, int per) __attribute__((always_inline)) { return (i * THREADS + tid) / per % C; };
   auto col_of = [&](int per) __attribute__((always_inline)) { return tid % per * VEC; };
-  static_assert(256 % (DK / VEC) == 0 && 256 % (DVS / VEC) == 0, "a thread's pieces lie in one column");
+  static_assert(THREADS % (DK / VEC) == 0 && THREADS % (DVS / VEC) == 0, "a thread's pieces lie in one column");
   auto get = [&](const store* p, int64_t ld, int rows, int i, int per, int width) __attribute__((always_inline)) {
     const int row = row_of(i, per), col = col_of(per);
     const uint32_t off = static_cast<uint32_t>(row < rows ? row : rows - 1) * (static_cast<uint32_t>(ld) * sizeof(store)) +
@@ -224,11 +263,18 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
     for (int i = 0; i < K::VP; ++i) rv[i] = get(vp + t * a.ld_v, a.ld_v, rows, i, DVS / VEC, cols);
     if (wave == 0) rg = a.decay[(t + (lane < rows ? lane : rows - 1)) * a.ld_decay + h];
   };
-  auto put = [&](tok_u32x4 x, int at, int plane, int pitch, int i, int per) __attribute__((always_inline)) {
-    const int p = i * 256 + tid, row = p / per, col = p % per * VEC;
-    unsigned char* to = lds + at + row * pitch + col * 2;
+  auto put = [&](tok_u32x4 x, unsigned char* at, int plane, int pitch, int i, int per, int all, bool q) __attribute__((always_inline)) {
+    if (all % THREADS != 0 && i * THREADS + tid >= all) return;
+    const int row = row_of(i, per), col = col_of(per);
+    unsigned char* to = at + (q ? four_at<K::Q_PITCH>(row, col / 4) : row * pitch + (row & 8) * 2 + col * 2);
+    unsigned char* to2 = at + (q ? four_at<K::Q_PITCH>(row, col / 4 + 1) : 0);
     if constexpr (NI == 1) {
-      *reinterpret_cast<tok_u32x4*>(to) = x;
+      if (q) {
+        *reinterpret_cast<tok_u32x2*>(to) = tok_u32x2{x[0], x[1]};
+        *reinterpret_cast<tok_u32x2*>(to2) = tok_u32x2{x[2], x[3]};
+      } else {
+        *reinterpret_cast<tok_u32x4*>(to) = x;
+      }
     } else {
       store v[VEC];
       __builtin_memcpy(v, &x, 16);
@@ -241,10 +287,17 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
         for (int n = 0; n < NI; ++n) w[n][e / 2] = t[n];
       }
 #pragma unroll
-      for (int n = 0; n < NI; ++n) __builtin_memcpy(__builtin_assume_aligned(to + n * plane, VEC * 2), w[n], VEC * 2);
+      for (int n = 0; n < NI; ++n) {
+        if (VEC == 8 && q) {
+          __builtin_memcpy(__builtin_assume_aligned(to + n * plane, 8), w[n], 8);
+          __builtin_memcpy(__builtin_assume_aligned(to2 + n * plane, 8), w[n] + 2, 8);
+        } else {
+          __builtin_memcpy(__builtin_assume_aligned(to + n * plane, VEC * 2), w[n], VEC * 2);
+        }
+      }
     }
   };
-  auto place = [&](int64_t t) __attribute__((always_inline)) {
+  auto place = [&](unsigned char* buf, int64_t t) __attribute__((always_inline)) {
     const int rows = end - t < C ? static_cast<int>(end - t) : C;
     if (rows < C || a.dim_k < DK || cols < DVS) {
       const tok_u32x4 none = {0u, 0u, 0u, 0u};
@@ -260,12 +313,12 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
     }
     if constexpr (!STATES) {
 #pragma unroll
-      for (int i = 0; i < K::KP; ++i) put(rq[i], 0, C * K::QK_PITCH, K::QK_PITCH, i, DK / VEC);
+      for (int i = 0; i < K::KP; ++i) put(rq[i], buf, C * K::Q_PITCH, K::Q_PITCH, i, DK / VEC, K::K_ALL, true);
     }
 #pragma unroll
-    for (int i = 0; i < K::KP; ++i) put(rk[i], K::K_AT, C * K::QK_PITCH, K::QK_PITCH, i, DK / VEC);
+    for (int i = 0; i < K::KP; ++i) put(rk[i], buf + K::K_AT, C * K::K_PITCH, K::K_PITCH, i, DK / VEC, K::K_ALL, false);
 #pragma unroll
-    for (int i = 0; i < K::VP; ++i) put(rv[i], K::V_AT, C * K::V_PITCH, K::V_PITCH, i, DVS / VEC);
+    for (int i = 0; i < K::VP; ++i) put(rv[i], buf + K::V_AT, C * K::V_PITCH, K::V_PITCH, i, DVS / VEC, K::V_ALL, false);
     if (wave == 0) {
       double s = static_cast<double>(rg < kForget ? kForget : rg) * kLog2e;
 #pragma unroll
@@ -275,20 +328,24 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
       }
       const double all = __shfl(s, C - 1);
       if (lane < C) {
+        // for each token G in units of log 2 (its float and the rest), scale
+        // exp(G_i), exp(G_C - G_i); exp(G_C)
+        float* const w = reinterpret_cast<float*>(buf + K::W_AT) + lane;
         const float hi = static_cast<float>(s);
-        g_hi[lane] = hi;
+        w[0] = hi;
         // a sum that is infinite or NaN has no rest
-        g_lo[lane] = fabsf(hi) < __builtin_inff() ? static_cast<float>(s - static_cast<double>(hi)) : 0.f;
-        w_q[lane] = exp2_of(hi);
-        w_k[lane] = exp2_of(static_cast<float>(all - s));
-        if (lane == 0) *w_all = exp2_of(static_cast<float>(all));
+        w[C] = fabsf(hi) < __builtin_inff() ? static_cast<float>(s - static_cast<double>(hi)) : 0.f;
+        w[2 * C] = a.scale * exp2_of(hi);
+        w[3 * C] = exp2_of(static_cast<float>(all - s));
+        if (lane == 0) w[4 * C] = exp2_of(static_cast<float>(all));
       }
     }
   };
 
-  // ---- S: tile [s][t] of column tile c holds rows 32 s + 8 g + 4 t + e of column 16 c + r
-  const int wc = wave * 16 * CT;  // this wave's first column
-  tok_f32x4 S[KS][2][CT];
+  // ---- S: tile [s][t] holds rows 32 s + 16 t + 4 g + e of this wave's column
+  // 16 c + r
+  const int wc = wave * 16 * CT, col = c0 + wc + r;
+  tok_f32x4 S[CT][KS][2];
   float factor = 1.f;
   const int64_t head_size = static_cast<int64_t>(a.dim_k) * a.dim_v;
   const float* from = STATES                ? nullptr
@@ -300,143 +357,143 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
+      for (int e = 0; e < 4; ++e) {
+        const int row = 32 * s + 16 * t + 4 * g + e;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = 32 * s + 8 * g + 4 * t + e, col = c0 + wc + 16 * c + r;
-          S[s][t][c][e] = from && row < a.dim_k && col < a.dim_v ? from[static_cast<int64_t>(row) * a.dim_v + col] : 0.f;
-        }
-
+        for (int c = 0; c < CT; ++c)
+          S[c][s][t][e] = from && row < a.dim_k && col + 16 * c < a.dim_v ? from[static_cast<int64_t>(row) * a.dim_v + col + 16 * c] : 0.f;
+      }
   const int64_t lane_out = static_cast<int64_t>(r) * a.heads * a.dim_v + wc + 4 * g;
 
-  ask(t0);
-  if constexpr (!STATES) {
-    // P above the diagonal, within the 32 keys of a step: zeros that stay
-    for (int i = tid; i < NO * (RT / 2) * 16 * 4; i += 256) {
-      const int piece = i & 3, row = i / 4 % 16, tile = i / 64 % (RT / 2), n = i / 64 / (RT / 2);
-      *reinterpret_cast<uint64_t*>(lds + K::P_AT + (n * C + tile * 32 + row) * K::P_PITCH + (tile * 32 + 16) * 2 + piece * 8) = 0;
-    }
-  }
-  for (int64_t t = t0; t < end; t += C) {
-    place(t);
-    meet();
-    if (t + C < end) ask(t + C);
-
-    tok_f32x4 O[STATES ? 1 : RT][CT];  // of token 16 rt + r: columns 16 c + 4 g + e
-    if constexpr (!STATES) {
-      // P: tiles of 16 keys x 16 queries on and below the diagonal, in turn
-      constexpr int JOBS = RT * (RT + 1) / 2;
+  // P of a chunk: tiles of 16 keys x 16 queries on and below the diagonal, in turn
+  auto weigh = [&](const unsigned char* buf, unsigned char* P) __attribute__((always_inline)) {
+    constexpr int JOBS = RT * (RT + 1) / 2;
+    const int r = tid & 15, g = tid >> 4 & 3, q_at = piece_at<K::Q_PITCH>(r, g);
+    const float *g_hi = reinterpret_cast<const float*>(buf + K::W_AT), *g_lo = g_hi + C;
 #pragma unroll
-      for (int j0 = 0; j0 < JOBS; j0 += 4) {
-        const int j = j0 + wave;
-        if (j < JOBS) {
-          const int qt = j < 1 ? 0 : j < 3 ? 1 : j < 6 ? 2 : 3, kt = j - qt * (qt + 1) / 2;
-          tok_f32x4 p = {0.f, 0.f, 0.f, 0.f};
+    for (int j0 = 0; j0 < JOBS; j0 += NW) {
+      const int j = j0 + wave;
+      if (j < JOBS) {
+        const int qt = j < 1 ? 0 : j < 3 ? 1 : j < 6 ? 2 : 3, kt = j - qt * (qt + 1) / 2;
+        tok_f32x4 p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int s = 0; s < KS; ++s) {
-            tok_bf16x8 fq[NI], fk[NI];
+        for (int s = 0; s < KS; ++s) {
+          tok_bf16x8 fq[NI], fk[NI];
 #pragma unroll
-            for (int n = 0; n < NI; ++n) {
-              const int at = n * C * K::QK_PITCH + r * K::QK_PITCH + s * 64 + g * 16;
-              fq[n] = *reinterpret_cast<const tok_bf16x8*>(lds + at + qt * 16 * K::QK_PITCH);
-              fk[n] = *reinterpret_cast<const tok_bf16x8*>(lds + K::K_AT + at + kt * 16 * K::QK_PITCH);
-            }
-            mfma_terms<LAST, NI, NI>(fk, fq, p);
+          for (int n = 0; n < NI; ++n) {
+            fq[n] = *reinterpret_cast<const tok_bf16x8*>(buf + (n * C + qt * 16) * K::Q_PITCH + (q_at ^ s * 64));
+            fk[n] = row8(buf + K::K_AT + (n * C + kt * 16 + r) * K::K_PITCH + (r & 8) * 2 + s * 64 + g * 8);
           }
-          const int i = qt * 16 + r, key = kt * 16 + 4 * g;
-          const tok_f32x4 hi = *reinterpret_cast<const tok_f32x4*>(g_hi + key), lo = *reinterpret_cast<const tok_f32x4*>(g_lo + key);
-          const float ih = g_hi[i], il = g_lo[i];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) p[e] = key + e <= i ? p[e] * exp2_of((ih - hi[e]) + (il - lo[e])) : 0.f;
-          uint32_t w0[NO], w1[NO];
-          split2<NO>(p[0], p[1], w0);
-          split2<NO>(p[2], p[3], w1);
-#pragma unroll
-          for (int n = 0; n < NO; ++n)
-            *reinterpret_cast<tok_u32x2*>(lds + K::P_AT + (n * C + i) * K::P_PITCH + key * 2) = tok_u32x2{w0[n], w1[n]};
+          mfma_terms<LAST, NI, NI>(fk, fq, p);
         }
+        const int i = qt * 16 + r, key = kt * 16 + 4 * g;
+        const tok_f32x4 hi = *reinterpret_cast<const tok_f32x4*>(g_hi + key), lo = *reinterpret_cast<const tok_f32x4*>(g_lo + key);
+        const float ih = g_hi[i], il = g_lo[i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = key + e <= i ? p[e] * a.scale * exp2_of((ih - hi[e]) + (il - lo[e])) : 0.f;
+        uint32_t w0[NO], w1[NO];
+        split2<NO>(p[0], p[1], w0);
+        split2<NO>(p[2], p[3], w1);
+#pragma unroll
+        for (int n = 0; n < NO; ++n)
+          *reinterpret_cast<tok_u32x2*>(P + n * C * K::P_PITCH + four_at<K::P_PITCH>(i, kt * 4 + g)) = tok_u32x2{w0[n], w1[n]};
       }
+    }
+  };
+
+  // out of a chunk, and S after it
+  tok_f32x4 O[CT][STATES ? 1 : RT];  // of token 16 i + r: columns wc + 16 c + 4 g + e
+  auto chunk = [&](const unsigned char* buf, const unsigned char* P) __attribute__((always_inline)) {
+    const int r = tid & 15, g = tid >> 4 & 3, q_at = piece_at<K::Q_PITCH>(r, g), p_at = piece_at<K::P_PITCH>(r, g);
+    const float *w_q = reinterpret_cast<const float*>(buf + K::W_AT) + 2 * C, *w_k = w_q + C;
+    if constexpr (!STATES) {
       // exp(G_i) q_i S
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int c = 0; c < CT; ++c) O[i][c] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < RT; ++i) O[c][i] = tok_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         __builtin_amdgcn_sched_barrier(0);
-        tok_bf16x8 fs[CT][NO];
+        tok_bf16x8 fs[CT][NO], fq[RT][NI];
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int n = 0; n < NI; ++n)
+            fq[i][n] = *reinterpret_cast<const tok_bf16x8*>(buf + (n * C + i * 16) * K::Q_PITCH + (q_at ^ s * 64));
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
           float f[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = S[s][e >> 2][c][e & 3];
+          for (int e = 0; e < 8; ++e) f[e] = S[c][s][e >> 2][e & 3];
           split8<NO>(f, fs[c]);
         }
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-          tok_bf16x8 fq[NI];
+        for (int x = 0; x < NO; ++x)
 #pragma unroll
-          for (int n = 0; n < NI; ++n)
-            fq[n] = *reinterpret_cast<const tok_bf16x8*>(lds + (n * C + i * 16 + r) * K::QK_PITCH + s * 64 + g * 16);
+          for (int y = 0; y < NI; ++y)
 #pragma unroll
-          for (int c = 0; c < CT; ++c) mfma_terms<LAST, NO, NI>(fs[c], fq, O[i][c]);
-        }
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+              for (int i = 0; i < RT; ++i)
+                if (x + y <= LAST) O[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fs[c][x], fq[i][y], O[c][i], 0, 0, 0);
       }
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
         const float w = w_q[i * 16 + r];
 #pragma unroll
-        for (int c = 0; c < CT; ++c) O[i][c] *= w;
+        for (int c = 0; c < CT; ++c) O[c][i] *= w;
       }
-      meet();
     }
-
-    // P v, and the state
     {
-      const float all = *w_all;
+      const float all = w_k[C];
       factor *= all;
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int c = 0; c < CT; ++c) S[s][u][c] *= all;
+          for (int c = 0; c < CT; ++c) S[c][s][u] *= all;
     }
 #pragma unroll
     for (int j = 0; j < JS; ++j) {
       __builtin_amdgcn_sched_barrier(0);
-      const int row = 32 * j + 8 * g;
-      tok_bf16x8 fv[CT][NI], fw[CT][kStateTerms];
+      const int row = 32 * j + 4 * g;  // the first of this lane's tokens; four more 16 further on
+      tok_bf16x8 fv[CT][NI], fw[CT][kStateTerms], fp[STATES ? 1 : RT][NO];
       float weight[8];
       *reinterpret_cast<tok_f32x4*>(weight) = *reinterpret_cast<const tok_f32x4*>(w_k + row);
-      *reinterpret_cast<tok_f32x4*>(weight + 4) = *reinterpret_cast<const tok_f32x4*>(w_k + row + 4);
+      *reinterpret_cast<tok_f32x4*>(weight + 4) = *reinterpret_cast<const tok_f32x4*>(w_k + row + 16);
 #pragma unroll
       for (int c = 0; c < CT; ++c) {
-        float f[8], zero = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = 0.f;
+        float f[8], x[8];
 #pragma unroll
         for (int n = NI - 1; n >= 0; --n) {
-          fv[c][n] = column8(lds + K::V_AT + (n * C + row + (r >> 2)) * K::V_PITCH + (wc + 16 * c + 4 * (r & 3)) * 2, K::V_PITCH);
+          fv[c][n] = column8(buf + K::V_AT + (n * C + row + (r >> 2)) * K::V_PITCH + (g & 2) * 8 + (wc + 16 * c + 4 * (r & 3)) * 2, K::V_PITCH);
           const tok_u32x4 u = __builtin_bit_cast(tok_u32x4, fv[c][n]);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            f[2 * e] += __uint_as_float(u[e] << 16);
-            f[2 * e + 1] += __uint_as_float(u[e] & 0xffff0000u);
+            const float lo = __uint_as_float(u[e] << 16), hi = __uint_as_float(u[e] & 0xffff0000u);
+            f[2 * e] = n == NI - 1 ? lo : f[2 * e] + lo;
+            f[2 * e + 1] = n == NI - 1 ? hi : f[2 * e + 1] + hi;
           }
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = f[e] * weight[e];
+        split8<kStateTerms>(x, fw[c]);
         if constexpr (!STATES) {
           // a value that is not finite must not meet the zeros of the tokens
-          // before it: it is left out, and makes NaN of those from its own on
-#pragma unroll
-          for (int e = 0; e < 8; ++e) zero = __builtin_fmaf(f[e], 0.f, zero);
-          if (__builtin_expect(__builtin_amdgcn_ballot_w64(zero != zero) != 0, 0)) {
+          // before it: it is left out, and makes NaN of those from its own on.
+          // The last term of such a value is NaN; of others it is below 2, but
+          // for values beyond 2^17, which are looked at as well.
+          const tok_u32x4 last = __builtin_bit_cast(tok_u32x4, fw[c][kStateTerms - 1]);
+          const uint32_t any = last[0] | last[1] | last[2] | last[3];
+          if (__builtin_expect(__builtin_amdgcn_ballot_w64((any & 0x40004000u) != 0) != 0, 0)) {
             int bad = C;
             tok_u32x4 m;
 #pragma unroll
             for (int e = 7; e >= 0; --e) {
               const bool ok = fabsf(f[e]) < __builtin_inff();
-              if (!ok) bad = row + e;
+              if (!ok) bad = row + (e < 4 ? e : 12 + e);
               const uint32_t half = ok ? 0xffffu : 0u;
               m[e >> 1] = e & 1 ? half << 16 : m[e >> 1] | half;
             }
@@ -449,58 +506,116 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int from_here = __shfl(bad, 4 * g + e);  // of column 16 c + 4 g + e
+              const int from_here = __shfl(bad, 4 * g + e);  // of column wc + 16 c + 4 g + e
 #pragma unroll
               for (int i = 0; i < RT; ++i)
-                if (i * 16 + r >= from_here) O[i][c][e] = __builtin_nanf("");
+                if (i * 16 + r >= from_here) O[c][i][e] = __builtin_nanf("");
             }
           }
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] *= weight[e];
-        split8<kStateTerms>(f, fw[c]);
       }
       if constexpr (!STATES) {
 #pragma unroll
-        for (int i = 2 * j; i < RT; ++i) {
-          tok_bf16x8 fp[NO];
+        for (int i = 2 * j; i < RT; ++i)
 #pragma unroll
           for (int n = 0; n < NO; ++n)
-            fp[n] = *reinterpret_cast<const tok_bf16x8*>(lds + K::P_AT + (n * C + i * 16 + r) * K::P_PITCH + j * 64 + g * 16);
+            fp[i][n] = *reinterpret_cast<const tok_bf16x8*>(P + (n * C + i * 16) * K::P_PITCH + (p_at ^ j * 64));
+      }
+      if constexpr (!STATES) {
 #pragma unroll
-          for (int c = 0; c < CT; ++c) mfma_terms<LAST, NI, NO>(fv[c], fp, O[i][c]);
-        }
+        for (int x = 0; x < NI; ++x)
+#pragma unroll
+          for (int y = 0; y < NO; ++y)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+              for (int i = 2 * j; i < RT; ++i)
+                if (x + y <= LAST) O[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv[c][x], fp[i][y], O[c][i], 0, 0, 0);
       }
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
+      for (int s = 0; s < KS; s += 2) {
+        __builtin_amdgcn_sched_barrier(0);
+        tok_bf16x8 fk[4][NI];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          if (u == 0) __builtin_amdgcn_sched_barrier(0);
-          tok_bf16x8 fk[NI];
+        for (int u = 0; u < 4; ++u)
 #pragma unroll
           for (int n = 0; n < NI; ++n)
-            fk[n] = column8(lds + K::K_AT + (n * C + row + (r >> 2)) * K::QK_PITCH + (32 * s + 8 * (r & 3) + 4 * u) * 2, K::QK_PITCH);
+            fk[u][n] = column8(buf + K::K_AT + (n * C + row + (r >> 2)) * K::K_PITCH + (g & 2) * 8 + (32 * s + 16 * u + 4 * (r & 3)) * 2, K::K_PITCH);
 #pragma unroll
-          for (int c = 0; c < CT; ++c) mfma_terms<kStateTerms - 1, NI, kStateTerms>(fk, fw[c], S[s][u][c]);
-        }
+        for (int x = 0; x < NI; ++x)
+#pragma unroll
+          for (int y = 0; y < kStateTerms; ++y)
+#pragma unroll
+            for (int c = 0; c < CT; ++c)
+#pragma unroll
+              for (int u = 0; u < 4; ++u)
+                if (x + y < kStateTerms)
+                  S[c][s + u / 2][u & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fk[u][x], fw[c][y], S[c][s + u / 2][u & 1], 0, 0, 0);
+      }
     }
+  };
+  auto store_out = [&](int64_t t) __attribute__((always_inline)) {
     if constexpr (!STATES) {
+      store* const to = static_cast<store*>(a.out) + (t * a.heads + h) * a.dim_v + c0 + lane_out;
+      const int64_t tile = static_cast<int64_t>(16) * a.heads * a.dim_v;
+      const int rows = end - t < C ? static_cast<int>(end - t) : C;
 #pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        if (t + i * 16 + r >= end) continue;
-        store* const to = static_cast<store*>(a.out) + ((t + i * 16) * a.heads + h) * a.dim_v + c0 + lane_out;
+      for (int c = 0; c < CT; ++c) {
+        if (wc + 16 * c >= cols) return;
 #pragma unroll
-        for (int c = 0; c < CT; ++c) {
-          const int col = wc + 16 * c + 4 * g;
-          if (col >= cols) continue;
+        for (int i = 0; i < RT; ++i) {
           store o[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[e] = E::narrow(O[i][c][e] * a.scale);
-          __builtin_memcpy(to + 16 * c, o, sizeof(o));
+          for (int e = 0; e < 4; ++e) o[e] = E::narrow(O[c][i][e]);
+          if (rows == C || i * 16 + (lane & 15) < rows) __builtin_memcpy(to + i * tile + 16 * c, o, sizeof(o));
         }
       }
     }
+  };
+
+  if constexpr (!STATES) {
+    // P above the diagonal, within the 32 keys of a step: zeros that stay
+    for (int i = tid; i < K::BUFS * NO * (RT / 2) * 16 * 4; i += THREADS) {
+      const int piece = i & 3, row = i / 4 % 16, tile = i / 64 % (RT / 2), n = i / 64 / (RT / 2);  // n: of all buffers
+      *reinterpret_cast<uint64_t*>(lds + K::P_AT + n * C * K::P_PITCH + four_at<K::P_PITCH>(tile * 32 + row, tile * 8 + 4 + piece)) = 0;
+    }
+  }
+  ask(t0);
+  place(lds, t0);
+  if (t0 + C < end) ask(t0 + C);
+  meet();
+  if constexpr (K::BUFS == 2) {
+    weigh(lds, lds + K::P_AT);
+    if (t0 + C < end) place(lds + K::BUFFER, t0 + C);
+    if (t0 + 2 * C < end) ask(t0 + 2 * C);
     meet();
+    int cur = 0;
+    for (int64_t t = t0; t < end; t += C, cur ^= 1) {
+      tid = unknown(tid);
+      unsigned char *const buf = lds + cur * K::BUFFER, *const next = lds + (cur ^ 1) * K::BUFFER;
+      unsigned char *const P = lds + K::P_AT + cur * K::P_BYTES, *const Pn = lds + K::P_AT + (cur ^ 1) * K::P_BYTES;
+      if (t + C < end) weigh(next, Pn);
+      chunk(buf, P);
+      store_out(t);
+      meet();
+      if (t + 2 * C < end) place(buf, t + 2 * C);
+      if (t + 3 * C < end) ask(t + 3 * C);
+      meet();
+    }
+  } else {
+    for (int64_t t = t0; t < end; t += C) {
+      tid = unknown(tid);
+      if constexpr (!STATES) {
+        weigh(lds, lds + K::P_AT);
+        meet();
+      }
+      chunk(lds, lds + K::P_AT);
+      store_out(t);
+      meet();
+      if (t + C < end) place(lds, t + C);
+      if (t + 2 * C < end) ask(t + 2 * C);
+      meet();
+    }
   }
 
   float* to = nullptr;
@@ -514,12 +629,12 @@ __global__ __launch_bounds__(256, (Chunk<E, DK, DVS, C, STATES>::BYTES <= 80 * 1
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
+      for (int e = 0; e < 4; ++e) {
+        const int row = 32 * s + 16 * t + 4 * g + e;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int row = 32 * s + 8 * g + 4 * t + e, col = c0 + wc + 16 * c + r;
-          if (row < a.dim_k && col < a.dim_v) to[static_cast<int64_t>(row) * a.dim_v + col] = S[s][t][c][e];
-        }
+        for (int c = 0; c < CT; ++c)
+          if (row < a.dim_k && col + 16 * c < a.dim_v) to[static_cast<int64_t>(row) * a.dim_v + col + 16 * c] = S[c][s][t][e];
+      }
   if (STATES && slice == 0 && tid == 0) a.factor[(b * a.parts + part + 1) * a.heads + h] = factor;
 }
 
@@ -639,23 +754,23 @@ struct Tile {
 Tile tile_of(int dtype, int64_t dim_k, int64_t dim_v) {
   Tile t;
   t.dk = dim_k <= 64 ? 64 : dim_k <= 128 ? 128 : 256;
-  t.dvs = dim_v <= 64 || t.dk == 256 || dtype == C3C_DTYPE_F32 ? 64 : 128;
-  t.c = dtype != C3C_DTYPE_BF16 || t.dk == 256 ? 32 : 64;
+  t.dvs = dim_v <= 64 ? 64 : 128;
+  t.c = 32;
   return t;
 }
 
-template <class E, int DK, int DVS, int C>
+template <class E, int DK, int DVS, int CT, int C>
 hipError_t run_chunks(Args a, hipStream_t s) {
   const int64_t head_size = static_cast<int64_t>(a.dim_k) * a.dim_v;
-  auto go = [&](void (*k)(Args), int64_t units) {
+  auto go = [&](void (*k)(Args), int64_t units, int threads) {
     a.groups = units;
-    return in_launches(up(units, 8) * 8 * a.slices, 256, [&](int64_t first, unsigned count) {
+    return in_launches(up(units, 8) * 8 * a.slices, threads, [&](int64_t first, unsigned count) {
       a.first = first;
-      hipLaunchKernelGGL(k, dim3(count), dim3(256), 0, s, a);
+      hipLaunchKernelGGL(k, dim3(count), dim3(threads), 0, s, a);
     });
   };
   if (a.parts > 1) {
-    hipError_t e = go(chunks<E, DK, DVS, C, true>, a.B * a.heads * (a.parts - 1));
+    hipError_t e = go(chunks<E, DK, DVS, 1, C, true>, a.B * a.heads * (a.parts - 1), DVS * 4);
     if (e != hipSuccess) return e;
     e = in_launches(a.B * a.heads * up(head_size / 4, 256), 256, [&](int64_t first, unsigned count) {
       a.first = first;
@@ -663,7 +778,7 @@ hipError_t run_chunks(Args a, hipStream_t s) {
     });
     if (e != hipSuccess) return e;
   }
-  return go(chunks<E, DK, DVS, C, false>, a.B * a.heads * a.parts);
+  return go(chunks<E, DK, DVS, CT, C, false>, a.B * a.heads * a.parts, DVS * 4 / CT);
 }
 
 template <class E, int W>
@@ -686,11 +801,10 @@ hipError_t run(Args a, int dtype, int64_t most, hipStream_t s) {
   }
   const Tile t = tile_of(dtype, a.dim_k, a.dim_v);
   a.slices = static_cast<int>(up(a.dim_v, t.dvs));
-  constexpr bool f32 = E::VEC == 4, bf16 = Terms<E>::IN == 1;
-  constexpr int C = bf16 ? 64 : 32, WIDE = f32 ? 64 : 128;
-  if (t.dk == 256) return run_chunks<E, 256, 64, 32>(a, s);
-  if (t.dvs == 64) return t.dk == 64 ? run_chunks<E, 64, 64, C>(a, s) : run_chunks<E, 128, 64, C>(a, s);
-  return t.dk == 64 ? run_chunks<E, 64, WIDE, C>(a, s) : run_chunks<E, 128, WIDE, C>(a, s);
+  constexpr int C = 32, CT = Terms<E>::IN < 3 ? 2 : 1;
+  if (t.dvs == 64)
+    return t.dk == 64 ? run_chunks<E, 64, 64, 1, C>(a, s) : t.dk == 128 ? run_chunks<E, 128, 64, 1, C>(a, s) : run_chunks<E, 256, 64, 1, 32>(a, s);
+  return t.dk == 64 ? run_chunks<E, 64, 128, CT, C>(a, s) : t.dk == 128 ? run_chunks<E, 128, 128, CT, C>(a, s) : run_chunks<E, 256, 128, 1, 32>(a, s);
 }
 
 }  // namespace
@@ -701,7 +815,7 @@ RecurPlan plan_recur(const c3c_state_cache& st, const c3c_kv_batch& b, int dtype
   if (most <= kFew || b.B < 1) return p;
   const Tile t = tile_of(dtype, st.dim_k, st.dim_v);
   const int64_t chunks = up(most, t.c), units = b.B * st.heads * up(st.dim_v, t.dvs);
-  const int64_t room = 2 * device_compute_units();
+  const int64_t room = device_compute_units() * (t.dvs == 128 ? 2 : 4);
   int64_t parts = room / units;
   if (parts > chunks / 4) parts = chunks / 4;
   if (parts < 2) return p;
