@@ -90,22 +90,13 @@ __device__ inline Channels<EPI> channels(const LinArgs& a, int64_t n) {
   return c;
 }
 
-// z / (1 + exp(-z))
-__device__ inline float swish(float z) { return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * z)); }
 __device__ inline float activate(int act, float z) {
-  switch (act) {
-    case C3C_ACT_SILU:
-      return swish(z);
-    case C3C_ACT_GELU:
-      return 0.5f * z * (1.f + erff(0.707106781f * z));
-    case C3C_ACT_GELU_TANH: {
-      // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
-      const float u = 1.59576912f * (z + 0.044715f * z * z * z);
-      return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * u));
-    }
-    default:
-      return z;
-  }
+  if (act == C3C_ACT_NONE) return z;
+  if (act == C3C_ACT_GELU) return 0.5f * z * (1.f + erff(0.707106781f * z));
+  // z / (1 + exp(-u)); u = z, or 2 sqrt(2 / pi) (z + 0.044715 z^3), since
+  // (1 + tanh v) / 2 = 1 / (1 + exp(-2 v))
+  const float u = act == C3C_ACT_SILU ? z : 1.59576912f * (z + 0.044715f * z * z * z);
+  return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * u));
 }
 
 // four values of a row from p, those past N being 0
@@ -130,6 +121,59 @@ __device__ inline void get4(int dtype, const void* p, int64_t at, int64_t left, 
 #pragma unroll
     for (int i = 0; i < 4; ++i) f[i] = dtype == C3C_DTYPE_BF16 ? ElemBf16::widen(h[i]) : ElemF16::widen(h[i]);
   }
+}
+
+// eight values of a row as they are stored, those past N being 0
+struct Stored8 {
+  tok_u32x4 a, b;  // 16-bit types: a alone
+};
+__device__ inline Stored8 stored8(int dtype, const void* p, int64_t at, int64_t left) {
+  Stored8 x = {{0u, 0u, 0u, 0u}, {0u, 0u, 0u, 0u}};
+  if (dtype == C3C_DTYPE_F32) {
+    const float* q = static_cast<const float*>(p) + at;
+    if (left >= 8) {
+      __builtin_memcpy(&x.a, q, 16);
+      __builtin_memcpy(&x.b, q + 4, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (i < left) (i < 4 ? x.a : x.b)[i & 3] = __float_as_uint(q[i]);
+    }
+  } else {
+    const uint16_t* q = static_cast<const uint16_t*>(p) + at;
+    if (left >= 8) {
+      __builtin_memcpy(&x.a, q, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (i < left) x.a[i >> 1] |= static_cast<uint32_t>(q[i]) << (16 * (i & 1));
+    }
+  }
+  return x;
+}
+// the same of U rows; whole: they all have eight (loads behind conditions of
+// single lanes are waited for one by one)
+template <int U>
+__device__ inline void stored_rows(int dtype, const void* p, const int64_t (&at)[U], int64_t left, bool whole, Stored8 (&x)[U]) {
+  if (whole && dtype == C3C_DTYPE_F32) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      __builtin_memcpy(&x[u].a, static_cast<const float*>(p) + at[u], 16);
+      __builtin_memcpy(&x[u].b, static_cast<const float*>(p) + at[u] + 4, 16);
+    }
+  } else if (whole) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) __builtin_memcpy(&x[u].a, static_cast<const uint16_t*>(p) + at[u], 16);
+  } else {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (left > 0) x[u] = stored8(dtype, p, at[u], left);
+  }
+}
+__device__ inline float value(int dtype, const Stored8& x, int i) {
+  if (dtype == C3C_DTYPE_F32) return __uint_as_float((i < 4 ? x.a : x.b)[i & 3]);
+  const uint16_t h = static_cast<uint16_t>(x.a[i >> 1] >> (16 * (i & 1)));
+  return dtype == C3C_DTYPE_BF16 ? ElemBf16::widen(h) : ElemF16::widen(h);
 }
 
 // What four results meet: the residual and the gates (EPILOGUE).
@@ -519,6 +563,57 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
       }
     }
   }
+  if constexpr (EPI == EPILOGUE) {
+    // Onto a residual without an activation (of 16 bits, a whole tile, its tokens
+    // under one row of gates): everything is read before anything is stored, since
+    // a load is waited for with every store before it, and all workgroups are
+    // here at once.
+    const uint32_t group = static_cast<uint32_t>(m0) / a.e.rows_per_gate;
+    if (!a.part && a.e.act == C3C_ACT_NONE && a.e.residual && a.y_dtype != C3C_DTYPE_F32 && n0 + BN <= a.N &&
+        static_cast<uint32_t>(m0 + mrows - 1) / a.e.rows_per_gate == group) {
+      const uint16_t* from = static_cast<const uint16_t*>(a.e.residual) + m0 * a.N + n0 + wn + g * 4;
+      tok_u32x2 res[NT][MT];
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          const int64_t row = wm + j * 16 + r < mrows ? wm + j * 16 + r : mrows - 1;
+          __builtin_memcpy(&res[i][j], from + row * a.N + i * 16, 8);
+        }
+#pragma unroll
+      for (int j = 0; j < MT; ++j) xs[j] = a.x_scale[m0 + (wm + j * 16 + r < mrows ? wm + j * 16 + r : mrows - 1)];
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const int64_t n = n0 + wn + i * 16 + g * 4;
+        const Channels<EPI> c = channels<EPI>(a, n);
+        float gate[4];
+        if (a.e.gate) get4(a.y_dtype, a.e.gate, group * a.N + n, 4, gate);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          uint16_t h[4];
+          __builtin_memcpy(h, &res[i][j], 8);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float z = static_cast<float>(acc[i][j][e]) * xs[j] * c.s[0][e];
+            if (a.bias) z += c.b[0][e];
+            if (a.e.gate) z *= gate[e];
+            const float f = a.y_dtype == C3C_DTYPE_BF16 ? ElemBf16::widen(h[e]) : ElemF16::widen(h[e]);
+            z = __builtin_fmaf(a.e.alpha, f, z);
+            h[e] = a.y_dtype == C3C_DTYPE_BF16 ? ElemBf16::narrow(z) : ElemF16::narrow(z);
+          }
+          __builtin_memcpy(&res[i][j], h, 8);
+        }
+      }
+      uint16_t* to = static_cast<uint16_t*>(a.y) + m0 * a.N + n0 + wn + g * 4;
+#pragma unroll
+      for (int j = 0; j < MT; ++j)
+        if (wm + j * 16 + r < mrows) {
+#pragma unroll
+          for (int i = 0; i < NT; ++i) __builtin_memcpy(to + (wm + j * 16 + r) * a.N + i * 16, &res[i][j], 8);
+        }
+      return;
+    }
+  }
   if constexpr (EPI != PLAIN) {
     if (a.part) return;
     // The sums change places in LDS, where a wave now has room for 64 tokens of
@@ -527,12 +622,13 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
     // channels of many tokens a lane, the functions are unrolled 128 times and
     // the sums end in scratch memory (32760 x 5120 x 5120 onto a residual: 1564 us).
     constexpr int ROOM = WM < 64 ? WM : 64, OC = WN / H, LPR = OC / 8, RPI = 64 / LPR;
-    constexpr int U = ROOM / RPI < 2 ? 1 : 2;  // tokens of a lane at once
+    constexpr int U = ROOM / RPI < 2 ? ROOM / RPI : 2;  // tokens of a lane at once
     static_assert(NW * ROOM * WN * 4 <= static_cast<int>(sizeof(lds)) && ROOM % (RPI * U) == 0, "room, whole rounds");
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");  // no wave reads a stage any more
     int8_t* const mine = lds + wave * ROOM * WN * 4;
     const int c8 = lane % LPR;
     const int64_t n = n0 + wn / H + c8 * 8;
+    const bool whole = n0 + ON <= a.N;
     Channels<EPI> c[2] = {channels<EPI>(a, n < a.N ? n : 0), channels<EPI>(a, n + 4 < a.N ? n + 4 : 0)};
 #pragma unroll
     for (int first = 0; first < MT; first += ROOM / 16) {
@@ -544,14 +640,20 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll 1
       for (int it = 0; it < ROOM / RPI; it += U) {
-        Beside x[U][2];
+        // asked for together, as they are stored: y may be the residual
+        Stored8 res[U], gate[U];
         int64_t m[U];
+        int64_t at[U], gate_at[U];  // of rows that exist
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           m[u] = m0 + wm + first * 16 + (it + u) * RPI + lane / LPR;
-#pragma unroll
-          for (int p = 0; p < 2; ++p)
-            if (m[u] < a.M && n + 4 * p < a.N) x[u][p] = beside<EPI>(a, m[u], n + 4 * p);
+          const int64_t row = m[u] < a.M ? m[u] : a.M - 1;
+          at[u] = row * a.N + n;
+          if constexpr (EPI == EPILOGUE) gate_at[u] = static_cast<int64_t>(static_cast<uint32_t>(row) / a.e.rows_per_gate) * a.N + n;
+        }
+        if constexpr (EPI == EPILOGUE) {
+          if (a.e.residual) stored_rows(a.y_dtype, a.e.residual, at, a.N - n, whole, res);
+          if (a.e.gate) stored_rows(a.y_dtype, a.e.gate, gate_at, a.N - n, whole, gate);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -564,7 +666,15 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
 #pragma unroll
             for (int h = 0; h < H; ++h)
               v[h] = *reinterpret_cast<const tok_i32x4*>(mine + row * WN * 4 + ((h * OC / 4 + c8 * 2 + p) ^ (row & 7)) * 16);
-            if (n + 4 * p < a.N) put4<EPI>(a, m[u], n + 4 * p, v, s, c[p], x[u][p]);
+            Beside x;
+            if constexpr (EPI == EPILOGUE) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                if (a.e.residual) x.residual[i] = value(a.y_dtype, res[u], 4 * p + i);
+                if (a.e.gate) x.gate[i] = value(a.y_dtype, gate[u], 4 * p + i);
+              }
+            }
+            if (n + 4 * p < a.N) put4<EPI>(a, m[u], n + 4 * p, v, s, c[p], x);
           }
         }
       }
