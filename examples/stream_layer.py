@@ -4,9 +4,11 @@ frame after another, and a cached causal Conv3D layer that decodes them.
 Every frame's tokens run through the layers in one call each (a frame sees
 itself and the frames that its window still holds), or token by token; the
 layers keep keys and values in paged 8-bit caches, the decoder keeps its last
-two frames.  Weights and inputs are synthetic.
+two frames.  Every n-th layer may be a recurrent one (--recurrent n), which
+remembers the stream in a state of constant size and sees it token by token.
+Weights and inputs are synthetic.
 
-    python examples/stream_layer.py [--frames 6] [--channels 1536] [--layers 2]
+    python examples/stream_layer.py [--frames 6] [--channels 1536] [--layers 2] [--recurrent 0]
 """
 import argparse
 import os
@@ -28,8 +30,8 @@ class Weights:
         w = torch.randn(N, K, generator=gen, device="cuda") / K ** 0.5
         self.w, self.scale = tokens.quantize_rows(ctx, w)
 
-    def __call__(self, ctx, x, x_scale=None):
-        return tokens.linear_i8(ctx, x, self.w, self.scale, x_scale=x_scale, out_dtype="bf16")
+    def __call__(self, ctx, x, x_scale=None, **epilogue):
+        return tokens.linear_i8(ctx, x, self.w, self.scale, x_scale=x_scale, out_dtype="bf16", **epilogue)
 
 
 class Layer:
@@ -42,6 +44,7 @@ class Layer:
         self.up = Weights(ctx, gen, 4 * channels, channels)
         self.down = Weights(ctx, gen, channels, 4 * channels)
         self.cache = tokens.KVCache.empty(pages, kv_heads, PAGE, self.dim)
+        self.products = self.qkv, self.out, self.up, self.down
 
         def gain():
             return 1 + 0.1 * torch.randn(channels, generator=gen, device="cuda")
@@ -50,6 +53,11 @@ class Layer:
         # one row of gates for the whole stream (a layer scale)
         self.gate_a, self.gate_f = (0.3 * torch.randn(1, channels, generator=gen, device="cuda").bfloat16()
                                     for _ in range(2))
+
+    def workspace(self, T, batch, window):
+        """Bytes that the calls of T tokens ask for."""
+        q = torch.empty(T, self.heads, self.dim, dtype=torch.bfloat16, device="cuda")
+        return [tokens.paged_attention_workspace_bytes(self.cache, q, batch, causal, window) for causal in (False, True)]
 
     def __call__(self, ctx, h, x, x_scale, batch, angles, causal, window, pre_next):
         """h (T, channels): the residual stream; x, x_scale: the layer's input
@@ -66,18 +74,54 @@ class Layer:
         return tokens.norm_gate(ctx, h, y, self.gate_f, post=self.post_f, pre=pre_next, rows_per_gate=T, quantize=True)
 
 
+class RecurrentLayer:
+    """Linear attention with a decay for each head and a gated feed-forward block,
+    each added to the residual stream by its last product."""
+
+    def __init__(self, ctx, gen, channels, heads, kv_heads):
+        self.heads, self.kv_heads, self.dim = heads, kv_heads, channels // heads
+        # heads share queries and keys in groups
+        self.qkv = Weights(ctx, gen, (heads + 2 * kv_heads) * self.dim, channels)
+        self.out = Weights(ctx, gen, channels, channels)
+        self.gate_up = Weights(ctx, gen, 2 * 3 * channels, channels)
+        self.down = Weights(ctx, gen, channels, 3 * channels)
+        self.products = self.qkv, self.out, self.down
+        self.states = tokens.StateCache.empty(1, heads, self.dim, self.dim)
+        # a head forgets half of what it holds within some 20 to 600 tokens
+        self.log_decay = torch.log1p(-torch.exp2(-5 - 5 * torch.arange(heads, device="cuda") / heads))
+        self.pre_a, self.pre_f = (1 + 0.1 * torch.randn(channels, generator=gen, device="cuda") for _ in range(2))
+
+    def workspace(self, T, batch, window):
+        q = torch.empty(T, self.kv_heads, self.dim, dtype=torch.bfloat16, device="cuda")
+        return [tokens.linear_attention_workspace_bytes(self.states, batch, q),
+                tokens.gated_linear_i8_workspace_bytes(T, self.gate_up.w.shape[0] // 2, self.gate_up.w.shape[1], "i8")]
+
+    def __call__(self, ctx, h, x, x_scale, batch, angles, causal, window, pre_next):
+        T = h.shape[0]
+        qkv = self.qkv(ctx, x, x_scale).view(T, 2 * self.kv_heads + self.heads, self.dim)
+        q, k, v = qkv.split([self.kv_heads, self.kv_heads, self.heads], 1)
+        a = tokens.linear_attention(ctx, self.states, batch, q, k, v, self.log_decay)
+        h = self.out(ctx, a.view(T, -1), residual=h, out=h)
+        _, x, x_scale = tokens.norm_gate(ctx, h, pre=self.pre_f, h_out=h, quantize=True)
+        u = tokens.gated_linear_i8(ctx, x, self.gate_up.w, self.gate_up.scale, x_scale=x_scale, out_dtype="bf16", act="silu")
+        h = self.down(ctx, u, residual=h, out=h)
+        return tokens.norm_gate(ctx, h, pre=pre_next, h_out=h, quantize=True)
+
+
 class WorldModel:
-    """`layers` layers over frames of H x W latent pixels in 2 x 2 patches, and
-    the decoder's first convolution."""
+    """`layers` layers over frames of H x W latent pixels in 2 x 2 patches, every
+    `recurrent`-th of them a recurrent one (0: none), and the decoder's first
+    convolution."""
 
     def __init__(self, channels=1536, heads=12, kv_heads=4, layers=2, H=60, W=104, latent=32, max_frames=8,
-                 window_frames=0, seed=0):
+                 window_frames=0, seed=0, recurrent=0):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         self.ctx = c3c.Context()
         self.H, self.W, self.latent, self.per_frame = H, W, latent, H // 2 * (W // 2)
         self.max_len = max_frames * self.per_frame
         cols = -(-self.max_len // PAGE)
-        self.layers = [Layer(self.ctx, gen, channels, heads, kv_heads, cols) for _ in range(layers)]
+        self.layers = [RecurrentLayer(self.ctx, gen, channels, heads, kv_heads) if recurrent and i % recurrent == recurrent - 1
+                       else Layer(self.ctx, gen, channels, heads, kv_heads, cols) for i in range(layers)]
         self.embed = Weights(self.ctx, gen, channels, 4 * latent)
         self.head = Weights(self.ctx, gen, 4 * latent, channels)
         self.last = torch.ones(channels, device="cuda")
@@ -102,11 +146,8 @@ class WorldModel:
             cu = torch.tensor([0, T], dtype=torch.int32, device="cuda")
             batch = tokens.Batch(self.table, cu, self.length, max_new=T, max_len=self.max_len)
             # the largest workspace that a call of T tokens asks for
-            layer = self.layers[0]
-            q = torch.empty(T, layer.heads, layer.dim, dtype=torch.bfloat16, device="cuda")
-            need = [tokens.paged_attention_workspace_bytes(layer.cache, q, batch, False, self.window),
-                    tokens.paged_attention_workspace_bytes(layer.cache, q, batch, True, self.window)]
-            for m in [m for x in self.layers for m in (x.qkv, x.out, x.up, x.down)] + [self.embed, self.head]:
+            need = [n for layer in self.layers for n in layer.workspace(T, batch, self.window)]
+            for m in [m for x in self.layers for m in x.products] + [self.embed, self.head]:
                 need.append(tokens.linear_i8_workspace_bytes(T, *m.w.shape))
             need.append(c3c.workspace_bytes(self.spec, "bf16"))
             self._batches[T] = batch, max(need)
@@ -141,9 +182,10 @@ def main():
     ap.add_argument("--frames", type=int, default=6)
     ap.add_argument("--channels", type=int, default=1536)
     ap.add_argument("--layers", type=int, default=2)
+    ap.add_argument("--recurrent", type=int, default=0)
     a = ap.parse_args()
     model = WorldModel(channels=a.channels, heads=a.channels // 128, kv_heads=max(1, a.channels // 384), layers=a.layers,
-                       max_frames=a.frames + 1, window_frames=4)
+                       max_frames=a.frames + 1, window_frames=4, recurrent=a.recurrent)
     x = torch.randn(model.per_frame, 4 * model.latent, device="cuda").bfloat16()
     for f in range(a.frames):
         torch.cuda.synchronize()

@@ -107,6 +107,16 @@ def _stream(stream, t):
     return _raw_stream(t.get_device()) if stream is None else getattr(stream, "cuda_stream", stream)
 
 
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _here(t):
+    """Refuses a call whose tensors are not on the current device: a stream given
+    as 0 is the current device's."""
+    if t.is_cuda and t.get_device() != _device():
+        raise ValueError(f"the tensors are on device {t.get_device()}, the current one is {_device()}")
+
+
 def _addr(t, name):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
@@ -164,7 +174,7 @@ def linear_i8_workspace_bytes(M: int, N: int, K: int, x_dtype: str = "bf16", y_d
     return n.value
 
 
-def _linear_args(x, x_scale, out, out_dtype):
+def _linear_args(x, out, out_dtype):
     """(M, K, row stride, x's dtype, y's dtype) of a product's activations and output."""
     xd = "i8" if x.dtype == torch.int8 else _float_dtype(x, "x")
     ld = _rows(x, "x")
@@ -189,7 +199,7 @@ def linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=N
     "none", "silu", "gelu" (by erf) or "gelu_tanh"; residual (M, N) and gate
     (groups, N), one row for ``rows_per_gate`` tokens, of y's dtype.  ``out`` may
     be the residual."""
-    M, K, ld, xd, yd = _linear_args(x, x_scale, out, out_dtype)
+    M, K, ld, xd, yd = _linear_args(x, out, out_dtype)
     N = w.shape[0]
     ydt = _TORCH[yd]
     if out is None:
@@ -204,6 +214,7 @@ def linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=N
         if st:
             _raise(st, ctx, "c3c_linear_i8")
         return out
+    _here(x)
     groups = -(-M // rows_per_gate) if rows_per_gate > 0 else 0
     e = _Epilogue(None if gate is None else _check(gate, "gate", ydt, (groups, N)),
                   None if residual is None else _check(residual, "residual", ydt, (M, N)), rows_per_gate, alpha, _act(act))
@@ -226,7 +237,8 @@ def gated_linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_d
     feed-forward block: w (2 N, K) int8 holds the gate's rows, then the others,
     w_scale and bias (2 N,) fp32.  x, x_scale, out and out_dtype as linear_i8
     takes them; the context needs gated_linear_i8_workspace_bytes."""
-    M, K, ld, xd, yd = _linear_args(x, x_scale, out, out_dtype)
+    _here(x)
+    M, K, ld, xd, yd = _linear_args(x, out, out_dtype)
     rows = w.shape[0]
     if rows % 2:
         raise ValueError(f"w has {rows} rows, expected two halves")
@@ -453,6 +465,7 @@ def linear_attention(ctx, states: StateCache, batch: Batch, q, k, v, log_decay, 
     ``slots`` (B,) int32: where each sequence's state lies (default: in order); a
     sequence whose tokens are all in this call begins at zero.  scale defaults to
     dim_k ** -0.5.  Returns out (T, heads, dim_v)."""
+    _here(q)
     dtype = _float_dtype(q, "q")
     T, qk_heads, _ = q.shape
     dt, heads = q.dtype, states.heads

@@ -85,6 +85,17 @@ def test_split_and_unsplit_give_the_same_bits():
     assert torch.equal(epilogue_call(M, N, K, "bf16", "bf16", **kw), epilogue_call(M, N, K, "bf16", "bf16", ws=rows, **kw))
 
 
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N,K", [(4200, 4100, 256), (4200, 4128, 95), (2100, 2050, 128)])
+@pytest.mark.parametrize("rows", [0, 1, 300, 5000])
+def test_large_tiles_onto_a_residual(act, dtype, M, N, K, rows):
+    """Tiles of 256 and 128, whole ones and the last; tokens of a tile under one
+    row of gates, and under several."""
+    kw = dict(act=act, residual=True, rows=rows)
+    assert torch.equal(epilogue_call(M, N, K, "i8", dtype, **kw), epilogue_call(M, N, K, "i8", dtype, in_place=True, **kw))
+
+
 @pytest.mark.parametrize("M,N,K,ld", [(40, 130, 97, 99), (70, 130, 97, 99), (300, 257, 96, 112)])
 def test_strided_rows(M, N, K, ld):
     epilogue_call(M, N, K, "f16", "f32", "silu", residual=True, ld=ld)
@@ -148,7 +159,7 @@ def test_gated(act, dtype, M, N, K):
 
 @pytest.mark.parametrize("yd", DTYPES)
 @pytest.mark.parametrize("M,N,K,ld", [(1, 48, 100, 100), (5, 48, 96, 112), (40, 130, 97, 99), (70, 130, 97, 99), (600, 515, 1024, 1024),
-                                      (2100, 1030, 128, 128)])
+                                      (2100, 1030, 128, 128), (4200, 2050, 256, 256), (4200, 2064, 95, 95)])
 def test_gated_8_bit_activations(yd, M, N, K, ld):
     gated_call(M, N, K, "i8", yd, bias=False, ld=ld)
 
