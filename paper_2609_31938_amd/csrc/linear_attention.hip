@@ -9,16 +9,31 @@
 // head forgets; the sums G are formed in 64 bits and kept as two floats, since
 // they may be large (a token that resets the state) next to their differences.
 //
-// chunks: a workgroup takes one head and up to 128 columns of S, of which every
-//   wave holds 16 in the matrix cores' accumulators, all dim_k rows of them: the layout of an accumulator is that of an operand whose
-//   rows are taken in another order, so S goes into the first product without
-//   passing through LDS, and no two waves share a column of out.  What the waves
-//   share is q, k and the weighted products P of queries and keys, in LDS.
+// Precision: an operand of the matrix cores is a sum of bf16 terms.  Inputs are
+// exact in 1 (bf16), 2 (f16) or 3 (f32) of them; S and the weighted products P of
+// queries and keys, which meet outputs of 16 bits, take 2 (2^-18 of a value; one
+// would add an error as large as the output's own rounding), for f32 3; weighted
+// values, which end in the fp32 states, take 3.
+//
+// chunks: a workgroup takes one head and up to 128 columns of S, of which a wave
+//   holds 16 or 32 in the matrix cores' accumulators, all dim_k rows of them: the
+//   layout of an accumulator is that of an operand whose rows are taken in
+//   another order, so S goes into the first product without passing through LDS,
+//   and no two waves share a column of out.  What the waves share is q, k and P,
+//   in LDS.  A clip of 32760 tokens x 32 heads of 128 (bf16) takes 350 us, and its
+//   loads and stores alone 211; two waves a SIMD (of 247 registers) wait for LDS,
+//   products and barriers in turn: without loads and stores it takes 291, without
+//   any one of the products 300 to 350.  Tried, and slower or no faster there: 16
+//   columns a wave with four waves a SIMD (registers in scratch memory, 410),
+//   chunks of 64 tokens (340 to 400; a frame of 1560 tokens 31 us, 23 so), one
+//   term in place of two or three (370), S scaled only where it has to be.
 // parts: few heads and sequences leave compute units idle.  Their sequences
 //   are split into parts of whole chunks: one launch forms each part's own
-//   state, one joins them in order, one forms the outputs of all parts.
-// tokens: few new tokens (single ones, drafted ones) take the recurrence
-//   as it stands, S in registers: it is bound by reading and writing S.
+//   state (160 us there; it reads k and v once more, whose loads alone take 110),
+//   one joins them in order (13 us), one forms the outputs of all parts.
+// tokens: few new tokens (single ones, drafted ones) take the recurrence as it
+//   stands, S in registers: it is bound by reading and writing S (64 sequences x
+//   32 heads of 128: 268 MB in 42 to 56 us by what the caches hold).
 #include "token_dev.h"
 #include "tokens_internal.h"
 
@@ -28,6 +43,7 @@ namespace {
 typedef short tok_i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) tok_i16x4 lds_i16x4;
 
+constexpr int C = 32;  // tokens of a chunk: a step of the matrix cores
 constexpr double kLog2e = 1.4426950408889634;
 constexpr float kForget = -110.f;  // exp of it is 0 in fp32
 
@@ -174,7 +190,7 @@ __device__ inline int four_at(int row, int c) {
 // E: input type.  DK: rows of S (dim_k, filled up with zeros).  DVS: columns of
 // this workgroup, CT tiles of 16 a wave.  C: tokens of a chunk.  STATES: only the state of a
 // part.
-template <class E, int DK, int DVS, int CT, int C, bool STATES>
+template <class E, int DK, int DVS, int CT, bool STATES>
 struct Chunk {
   static constexpr int NI = Terms<E>::IN, NO = Terms<E>::OUT;
   static constexpr int THREADS = DVS * 4 / CT;
@@ -201,13 +217,13 @@ struct Chunk {
   static constexpr int WAVES = FIT < MOST ? FIT : MOST;
 };
 
-template <class E, int DK, int DVS, int CT, int C, bool STATES>
-__global__ __launch_bounds__((Chunk<E, DK, DVS, CT, C, STATES>::THREADS), (Chunk<E, DK, DVS, CT, C, STATES>::WAVES)) void chunks(Args a) {
-  typedef Chunk<E, DK, DVS, CT, C, STATES> K;
+template <class E, int DK, int DVS, int CT, bool STATES>
+__global__ __launch_bounds__((Chunk<E, DK, DVS, CT, STATES>::THREADS), (Chunk<E, DK, DVS, CT, STATES>::WAVES)) void chunks(Args a) {
+  typedef Chunk<E, DK, DVS, CT, STATES> K;
   typedef typename E::store store;
   constexpr int NI = K::NI, NO = K::NO, VEC = E::VEC, THREADS = K::THREADS, NW = THREADS / 64;
   constexpr int LAST = NO - 1;
-  constexpr int KS = DK / 32, JS = C / 32, RT = C / 16;
+  constexpr int KS = DK / 32, RT = C / 16;
   __shared__ __align__(16) unsigned char lds[K::BYTES];
   int tid = threadIdx.x;
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
@@ -367,38 +383,35 @@ __global__ __launch_bounds__((Chunk<E, DK, DVS, CT, C, STATES>::THREADS), (Chunk
 
   // P of a chunk: tiles of 16 keys x 16 queries on and below the diagonal, in turn
   auto weigh = [&](const unsigned char* buf, unsigned char* P) __attribute__((always_inline)) {
-    constexpr int JOBS = RT * (RT + 1) / 2;
+    constexpr int JOBS = 3;
     const int r = tid & 15, g = tid >> 4 & 3, q_at = piece_at<K::Q_PITCH>(r, g);
     const float *g_hi = reinterpret_cast<const float*>(buf + K::W_AT), *g_lo = g_hi + C;
+    static_assert(NW >= JOBS && RT == 2, "a tile a wave");
+    const int j = wave;
+    if (j >= JOBS) return;
+    const int qt = j > 0, kt = j > 1;
+    tok_f32x4 p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j0 = 0; j0 < JOBS; j0 += NW) {
-      const int j = j0 + wave;
-      if (j < JOBS) {
-        const int qt = j < 1 ? 0 : j < 3 ? 1 : j < 6 ? 2 : 3, kt = j - qt * (qt + 1) / 2;
-        tok_f32x4 p = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < KS; ++s) {
+      tok_bf16x8 fq[NI], fk[NI];
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          tok_bf16x8 fq[NI], fk[NI];
-#pragma unroll
-          for (int n = 0; n < NI; ++n) {
-            fq[n] = *reinterpret_cast<const tok_bf16x8*>(buf + (n * C + qt * 16) * K::Q_PITCH + (q_at ^ s * 64));
-            fk[n] = row8(buf + K::K_AT + (n * C + kt * 16 + r) * K::K_PITCH + (r & 8) * 2 + s * 64 + g * 8);
-          }
-          mfma_terms<LAST, NI, NI>(fk, fq, p);
-        }
-        const int i = qt * 16 + r, key = kt * 16 + 4 * g;
-        const tok_f32x4 hi = *reinterpret_cast<const tok_f32x4*>(g_hi + key), lo = *reinterpret_cast<const tok_f32x4*>(g_lo + key);
-        const float ih = g_hi[i], il = g_lo[i];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = key + e <= i ? p[e] * a.scale * exp2_of((ih - hi[e]) + (il - lo[e])) : 0.f;
-        uint32_t w0[NO], w1[NO];
-        split2<NO>(p[0], p[1], w0);
-        split2<NO>(p[2], p[3], w1);
-#pragma unroll
-        for (int n = 0; n < NO; ++n)
-          *reinterpret_cast<tok_u32x2*>(P + n * C * K::P_PITCH + four_at<K::P_PITCH>(i, kt * 4 + g)) = tok_u32x2{w0[n], w1[n]};
+      for (int n = 0; n < NI; ++n) {
+        fq[n] = *reinterpret_cast<const tok_bf16x8*>(buf + (n * C + qt * 16) * K::Q_PITCH + (q_at ^ s * 64));
+        fk[n] = row8(buf + K::K_AT + (n * C + kt * 16 + r) * K::K_PITCH + (r & 8) * 2 + s * 64 + g * 8);
       }
+      mfma_terms<LAST, NI, NI>(fk, fq, p);
     }
+    const int i = qt * 16 + r, key = kt * 16 + 4 * g;
+    const tok_f32x4 hi = *reinterpret_cast<const tok_f32x4*>(g_hi + key), lo = *reinterpret_cast<const tok_f32x4*>(g_lo + key);
+    const float ih = g_hi[i], il = g_lo[i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = key + e <= i ? p[e] * a.scale * exp2_of((ih - hi[e]) + (il - lo[e])) : 0.f;
+    uint32_t w0[NO], w1[NO];
+    split2<NO>(p[0], p[1], w0);
+    split2<NO>(p[2], p[3], w1);
+#pragma unroll
+    for (int n = 0; n < NO; ++n)
+      *reinterpret_cast<tok_u32x2*>(P + n * C * K::P_PITCH + four_at<K::P_PITCH>(i, kt * 4 + g)) = tok_u32x2{w0[n], w1[n]};
   };
 
   // out of a chunk, and S after it
@@ -455,10 +468,9 @@ __global__ __launch_bounds__((Chunk<E, DK, DVS, CT, C, STATES>::THREADS), (Chunk
 #pragma unroll
           for (int c = 0; c < CT; ++c) S[c][s][u] *= all;
     }
-#pragma unroll
-    for (int j = 0; j < JS; ++j) {
+    {
       __builtin_amdgcn_sched_barrier(0);
-      const int row = 32 * j + 4 * g;  // the first of this lane's tokens; four more 16 further on
+      const int row = 4 * g;  // the first of this lane's tokens; four more 16 further on
       tok_bf16x8 fv[CT][NI], fw[CT][kStateTerms], fp[STATES ? 1 : RT][NO];
       float weight[8];
       *reinterpret_cast<tok_f32x4*>(weight) = *reinterpret_cast<const tok_f32x4*>(w_k + row);
@@ -516,10 +528,10 @@ __global__ __launch_bounds__((Chunk<E, DK, DVS, CT, C, STATES>::THREADS), (Chunk
       }
       if constexpr (!STATES) {
 #pragma unroll
-        for (int i = 2 * j; i < RT; ++i)
+        for (int i = 0; i < RT; ++i)
 #pragma unroll
           for (int n = 0; n < NO; ++n)
-            fp[i][n] = *reinterpret_cast<const tok_bf16x8*>(P + (n * C + i * 16) * K::P_PITCH + (p_at ^ j * 64));
+            fp[i][n] = *reinterpret_cast<const tok_bf16x8*>(P + (n * C + i * 16) * K::P_PITCH + p_at);
       }
       if constexpr (!STATES) {
 #pragma unroll
@@ -529,7 +541,7 @@ __global__ __launch_bounds__((Chunk<E, DK, DVS, CT, C, STATES>::THREADS), (Chunk
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
-              for (int i = 2 * j; i < RT; ++i)
+              for (int i = 0; i < RT; ++i)
                 if (x + y <= LAST) O[c][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv[c][x], fp[i][y], O[c][i], 0, 0, 0);
       }
 #pragma unroll
@@ -575,9 +587,9 @@ __global__ __launch_bounds__((Chunk<E, DK, DVS, CT, C, STATES>::THREADS), (Chunk
 
   if constexpr (!STATES) {
     // P above the diagonal, within the 32 keys of a step: zeros that stay
-    for (int i = tid; i < K::BUFS * NO * (RT / 2) * 16 * 4; i += THREADS) {
-      const int piece = i & 3, row = i / 4 % 16, tile = i / 64 % (RT / 2), n = i / 64 / (RT / 2);  // n: of all buffers
-      *reinterpret_cast<uint64_t*>(lds + K::P_AT + n * C * K::P_PITCH + four_at<K::P_PITCH>(tile * 32 + row, tile * 8 + 4 + piece)) = 0;
+    for (int i = tid; i < K::BUFS * NO * 16 * 4; i += THREADS) {
+      const int four = i & 3, row = i / 4 % 16, n = i / 64;  // n: terms of all buffers
+      *reinterpret_cast<uint64_t*>(lds + K::P_AT + n * C * K::P_PITCH + four_at<K::P_PITCH>(row, 4 + four)) = 0;
     }
   }
   ask(t0);
@@ -742,24 +754,24 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // rows of a thread where rg threads share dk of them
 constexpr int rows_each(int dk, int rg) { return dk > rg ? dk / rg : 1; }
 
-constexpr int64_t kFew = 16;  // new tokens of a sequence that take the recurrence
+// New tokens of a sequence that take the recurrence.  A token takes about 1.1 us
+// there, a chunk 10: 16 sequences x 16 heads of 128 (bf16) 10.3 us for 4 tokens, 12.5
+// for 6, in chunks 11.2; 64 x 32 heads 51 for 4 and 60 for 6, in chunks 55; of 256
+// rows and columns, or in f32, the two meet at 8 to 12 tokens.
+constexpr int64_t kFew = 5;
 
 // New tokens that a sequence may have.
 int64_t most_new(const c3c_kv_batch& b) { return b.max_new < b.T ? b.max_new : b.T; }
 
-// The chunk kernel's tile: rows of S, columns of a workgroup, tokens of a chunk.
+// The chunk kernel's tile: rows of S, columns of a workgroup.
 struct Tile {
-  int dk, dvs, c;
+  int dk, dvs;
 };
-Tile tile_of(int dtype, int64_t dim_k, int64_t dim_v) {
-  Tile t;
-  t.dk = dim_k <= 64 ? 64 : dim_k <= 128 ? 128 : 256;
-  t.dvs = dim_v <= 64 ? 64 : 128;
-  t.c = 32;
-  return t;
+Tile tile_of(int64_t dim_k, int64_t dim_v) {
+  return {dim_k <= 64 ? 64 : dim_k <= 128 ? 128 : 256, dim_v <= 64 ? 64 : 128};
 }
 
-template <class E, int DK, int DVS, int CT, int C>
+template <class E, int DK, int DVS, int CT>
 hipError_t run_chunks(Args a, hipStream_t s) {
   const int64_t head_size = static_cast<int64_t>(a.dim_k) * a.dim_v;
   auto go = [&](void (*k)(Args), int64_t units, int threads) {
@@ -770,7 +782,7 @@ hipError_t run_chunks(Args a, hipStream_t s) {
     });
   };
   if (a.parts > 1) {
-    hipError_t e = go(chunks<E, DK, DVS, 1, C, true>, a.B * a.heads * (a.parts - 1), DVS * 4);
+    hipError_t e = go(chunks<E, DK, DVS, 1, true>, a.B * a.heads * (a.parts - 1), DVS * 4);
     if (e != hipSuccess) return e;
     e = in_launches(a.B * a.heads * up(head_size / 4, 256), 256, [&](int64_t first, unsigned count) {
       a.first = first;
@@ -778,7 +790,7 @@ hipError_t run_chunks(Args a, hipStream_t s) {
     });
     if (e != hipSuccess) return e;
   }
-  return go(chunks<E, DK, DVS, CT, C, false>, a.B * a.heads * a.parts, DVS * 4 / CT);
+  return go(chunks<E, DK, DVS, CT, false>, a.B * a.heads * a.parts, DVS * 4 / CT);
 }
 
 template <class E, int W>
@@ -794,33 +806,36 @@ hipError_t run_tokens(Args a, hipStream_t s) {
 }
 
 template <class E>
-hipError_t run(Args a, int dtype, int64_t most, hipStream_t s) {
+hipError_t run(Args a, int64_t most, hipStream_t s) {
   if (most <= kFew) {
-    // narrow slices where there are few heads
+    // narrow slices where there are few heads: as many workgroups as compute units
     return a.B * a.heads < 256 ? run_tokens<E, 16>(a, s) : run_tokens<E, 32>(a, s);
   }
-  const Tile t = tile_of(dtype, a.dim_k, a.dim_v);
+  const Tile t = tile_of(a.dim_k, a.dim_v);
   a.slices = static_cast<int>(up(a.dim_v, t.dvs));
-  constexpr int C = 32, CT = Terms<E>::IN < 3 ? 2 : 1;
-  if (t.dvs == 64)
-    return t.dk == 64 ? run_chunks<E, 64, 64, 1, C>(a, s) : t.dk == 128 ? run_chunks<E, 128, 64, 1, C>(a, s) : run_chunks<E, 256, 64, 1, 32>(a, s);
-  return t.dk == 64 ? run_chunks<E, 64, 128, CT, C>(a, s) : t.dk == 128 ? run_chunks<E, 128, 128, CT, C>(a, s) : run_chunks<E, 256, 128, 1, 32>(a, s);
+  // two column tiles a wave where the registers hold them
+  constexpr int CT = Terms<E>::IN < 3 ? 2 : 1;
+  if (t.dvs == 64) return t.dk == 64 ? run_chunks<E, 64, 64, 1>(a, s) : t.dk == 128 ? run_chunks<E, 128, 64, 1>(a, s) : run_chunks<E, 256, 64, 1>(a, s);
+  return t.dk == 64 ? run_chunks<E, 64, 128, CT>(a, s) : t.dk == 128 ? run_chunks<E, 128, 128, CT>(a, s) : run_chunks<E, 256, 128, 1>(a, s);
 }
 
 }  // namespace
 
-RecurPlan plan_recur(const c3c_state_cache& st, const c3c_kv_batch& b, int dtype) {
+RecurPlan plan_recur(const c3c_state_cache& st, const c3c_kv_batch& b) {
   RecurPlan p;
   const int64_t most = most_new(b);
   if (most <= kFew || b.B < 1) return p;
-  const Tile t = tile_of(dtype, st.dim_k, st.dim_v);
-  const int64_t chunks = up(most, t.c), units = b.B * st.heads * up(st.dim_v, t.dvs);
+  const Tile t = tile_of(st.dim_k, st.dim_v);
+  const int64_t chunks = up(most, C), units = b.B * st.heads * up(st.dim_v, t.dvs);
+  // As many parts as there is room for at once, of two chunks at least (6 heads
+  // of 80 x 112 in f32, four sequences of up to 701 tokens: 37 us, of four chunks
+  // 51; twice the room: the same).
   const int64_t room = device_compute_units() * (t.dvs == 128 ? 2 : 4);
   int64_t parts = room / units;
-  if (parts > chunks / 4) parts = chunks / 4;
+  if (parts > chunks / 2) parts = chunks / 2;
   if (parts < 2) return p;
   const int64_t each = up(chunks, parts);
-  p.part_tokens = each * t.c;
+  p.part_tokens = each * C;
   p.parts = static_cast<int>(up(chunks, each));
   p.state_bytes = b.B * p.parts * st.heads * st.dim_k * st.dim_v * 4;
   p.bytes = p.state_bytes + b.B * p.parts * st.heads * 4;
@@ -835,7 +850,7 @@ hipError_t launch_recur(const RecurArgs& r, int dtype, const RecurPlan& plan, hi
          r.ld_q, r.ld_k, r.ld_v, r.ld_decay, plan.part_tokens, 0, 0, static_cast<int>(st.heads),
          static_cast<int>(r.qk_heads), static_cast<int>(st.dim_k), static_cast<int>(st.dim_v), plan.parts, 1, r.scale};
   if (plan.parts > 1) a.factor = r.part + plan.state_bytes / 4;
-  return dtype == C3C_DTYPE_BF16 ? run<ElemBf16>(a, dtype, most, s) : dtype == C3C_DTYPE_F16 ? run<ElemF16>(a, dtype, most, s) : run<ElemF32>(a, dtype, most, s);
+  return dtype == C3C_DTYPE_BF16 ? run<ElemBf16>(a, most, s) : dtype == C3C_DTYPE_F16 ? run<ElemF16>(a, most, s) : run<ElemF32>(a, most, s);
 }
 
 }  // namespace c3c

@@ -444,7 +444,7 @@ int c3c_paged_attention(c3c_ctx* ctx, const c3c_kv_cache* cache, const c3c_kv_ba
 int c3c_linear_attention_workspace_bytes(const c3c_state_cache* states, const c3c_kv_batch* batch,
                                          int dtype, int64_t qk_heads, size_t* bytes) {
   if (!bytes || check_recur(states, batch, dtype, qk_heads)) return C3C_E_INVAL;
-  *bytes = static_cast<size_t>(plan_recur(*states, *batch, dtype).bytes);
+  *bytes = static_cast<size_t>(plan_recur(*states, *batch).bytes);
   return C3C_OK;
 }
 
@@ -479,7 +479,7 @@ int c3c_linear_attention(c3c_ctx* ctx, const c3c_state_cache* states, const c3c_
   if (!why) why = check_spans(o, 2);
   if (!why) why = check_overlap(in, 7, o, 2, ctx->ws, static_cast<int64_t>(ctx->ws_bytes));
   if (why) return fail(ctx, C3C_E_INVAL, why);
-  RecurPlan plan = plan_recur(*states, *batch, dtype);
+  RecurPlan plan = plan_recur(*states, *batch);
   if (plan.bytes > static_cast<int64_t>(ctx->ws_bytes)) plan = RecurPlan{};
   const RecurArgs a{*states, *batch, slot, q, k, v, log_decay, out, static_cast<float*>(ctx->ws), qk_heads, ld_q, ld_k, ld_v,
                     ld_decay, scale};

@@ -110,7 +110,7 @@ struct RecurPlan {
   int64_t part_tokens = int64_t(1) << 40;     // of each part but the last
   int64_t state_bytes = 0, bytes = 0;         // of workspace: the parts' states, and with their factors
 };
-RecurPlan plan_recur(const c3c_state_cache& st, const c3c_kv_batch& b, int dtype);
+RecurPlan plan_recur(const c3c_state_cache& st, const c3c_kv_batch& b);
 hipError_t launch_recur(const RecurArgs& a, int dtype, const RecurPlan& plan, hipStream_t s);
 
 }  // namespace c3c
