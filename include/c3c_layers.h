@@ -60,7 +60,8 @@ typedef struct c3c_state_cache {
  * States and sums are fp32.  Products of a chunk of tokens run on the matrix
  * cores with operands split into bf16 terms of 8 bits: inputs into as many as
  * hold them exactly (1 for bf16, 2 for f16, 3 for f32); what multiplies them in
- * out into 2 (3 for f32) terms; in the state into 3.
+ * out into 2 (3 for f32) terms; in the state into 3.  A value beyond 3.38e38, the
+ * largest of bf16, counts as infinite.
  *
  * max_new bounds the new tokens of a sequence; it only plans the work.
  * Workspace (c3c_linear_attention_workspace_bytes): the states between the
@@ -84,6 +85,9 @@ int c3c_linear_attention(c3c_ctx* ctx, const c3c_state_cache* states, const c3c_
 enum { C3C_ACT_NONE = 0, C3C_ACT_SILU = 1, C3C_ACT_GELU = 2, C3C_ACT_GELU_TANH = 3 };
 
 /* z = c3c_linear_i8's result, before its rounding; for token m and channel n
+ * (with float activations' codes, here and in c3c_gated_linear_i8, the integers
+ * nearest to 127 x / max|x| themselves: c3c_quantize_rows rounds the scale first,
+ * which differs by one step for the few values next to a half)
  *   y = alpha * residual[m][n] + gate[m / rows_per_gate][n] * act(z)
  * residual [M][N], gate [ceil(M / rows_per_gate)][N], both of y_dtype and
  * contiguous; NULL: no residual, a gate of ones.  y may be the residual itself.

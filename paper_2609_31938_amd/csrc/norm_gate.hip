@@ -240,6 +240,7 @@ struct QuantArgs {
   float* scale;
   int64_t T, C, ld_x, ld_q;  // q's rows are zero from C to ld_q
   int64_t first;             // workgroup of this launch
+  int exact;                 // codes nearest to 127 x / max|x| itself
 };
 
 template <class E, int NV, bool WAVE>
@@ -261,12 +262,13 @@ __global__ __launch_bounds__(WAVE ? 256 : 1024) void quantize_regs(QuantArgs a) 
   for (int i = 0; i < NV; ++i)
 #pragma unroll
     for (int e = 0; e < V; ++e) top = fmaxf(top, magnitude(v[i][e]));
-  const float s = row_scale(row.max(top, 0));
+  top = row.max(top, 0);
+  const float s = row_scale(top);
   int8_t* q = a.q + t * a.ld_q;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
     const int c = (lane + i * per) * V;
-    if (c < Q) store_codes<V>(q + c, Q - c, v[i], s);
+    if (c < Q) store_codes<V>(q + c, Q - c, v[i], s, a.exact ? top : 0.f);
   }
   if (lane == 0) a.scale[t] = s;
 }
@@ -279,9 +281,12 @@ __global__ __launch_bounds__(1024) void quantize_loop(QuantArgs a) {
   const typename E::store* x = static_cast<const typename E::store*>(a.x) + t * a.ld_x;
   float top = 0.f;
   for (int64_t c = threadIdx.x; c < a.C; c += blockDim.x) top = fmaxf(top, magnitude(E::widen(x[c])));
-  const float s = row_scale(row.max(top, 0));
-  for (int64_t c = threadIdx.x; c < a.ld_q; c += blockDim.x)
-    a.q[t * a.ld_q + c] = static_cast<int8_t>(c < a.C ? code(E::widen(x[c]), s) : 0);
+  top = row.max(top, 0);
+  const float s = row_scale(top);
+  for (int64_t c = threadIdx.x; c < a.ld_q; c += blockDim.x) {
+    const float v = c < a.C ? E::widen(x[c]) : 0.f;
+    a.q[t * a.ld_q + c] = static_cast<int8_t>(a.exact && near_half(v, s) ? true_code(v, s, top) : code(v, s));
+  }
   if (threadIdx.x == 0) a.scale[t] = s;
 }
 
@@ -345,9 +350,9 @@ hipError_t launch_norm_gate(const c3c_norm_desc& d, const void* h, const void* y
 }
 
 hipError_t launch_quantize_rows(int64_t T, int64_t C, int64_t ld_x, int dtype, const void* x,
-                                int8_t* q, int64_t ld_q, float* scale, hipStream_t s) {
+                                int8_t* q, int64_t ld_q, float* scale, bool exact, hipStream_t s) {
   if (T == 0) return hipSuccess;
-  const QuantArgs a{x, q, scale, T, C, ld_x, ld_q, 0};
+  const QuantArgs a{x, q, scale, T, C, ld_x, ld_q, 0, exact};
   return dtype == C3C_DTYPE_BF16  ? quantize_typed<ElemBf16>(a, s)
          : dtype == C3C_DTYPE_F16 ? quantize_typed<ElemF16>(a, s)
                                   : quantize_typed<ElemF32>(a, s);

@@ -119,13 +119,36 @@ __device__ inline int code(float v, float s) {
   return s > 0.f ? static_cast<int>(fminf(fmaxf(q, -127.f), 127.f)) : 0;
 }
 
+// The integer nearest to 127 v / top itself (top: the row's largest magnitude), not
+// to v / s with its rounded scale: the two differ only next to a half, as near_half
+// says (v / s errs by less than 2^-16).
+__device__ inline bool near_half(float v, float s) {
+  const float t = v / s;
+  return fabsf(fabsf(t - rintf(t)) - 0.5f) < 0x1p-15f;
+}
+__device__ inline int true_code(float v, float s, float top) {
+  return s > 0.f ? static_cast<int>(rint(static_cast<double>(v) * 127.0 / static_cast<double>(top))) : 0;
+}
+
+// top: 0, or the row's largest magnitude for codes by true_code
 template <int N>
-__device__ inline void store_codes(int8_t* p, int m, const float (&v)[N], float s) {
+__device__ inline void store_codes(int8_t* p, int m, const float (&v)[N], float s, float top = 0.f) {
   uint32_t w[(N + 3) / 4];
 #pragma unroll
   for (int i = 0; i < (N + 3) / 4; ++i) w[i] = 0;
 #pragma unroll
   for (int e = 0; e < N; ++e) w[e >> 2] |= (static_cast<uint32_t>(code(v[e], s)) & 255u) << (8 * (e & 3));
+  if (top > 0.f) {
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < N; ++e) any |= near_half(v[e], s);
+    if (__builtin_expect(any, 0)) {
+#pragma unroll
+      for (int i = 0; i < (N + 3) / 4; ++i) w[i] = 0;
+#pragma unroll
+      for (int e = 0; e < N; ++e) w[e >> 2] |= (static_cast<uint32_t>(true_code(v[e], s, top)) & 255u) << (8 * (e & 3));
+    }
+  }
   if (m >= N) {
     __builtin_memcpy(p, w, N);
   } else {

@@ -158,7 +158,7 @@ int run_linear(c3c_ctx* ctx, const c3c_linear_desc& d, const LinearEpilogue& e, 
   if (!i8 && d.M > 0) {
     int8_t* q = reinterpret_cast<int8_t*>(ws);
     float* scale = reinterpret_cast<float*>(ws + sp.scale_at);
-    const hipError_t err = launch_quantize_rows(d.M, d.K, d.ld_x, d.x_dtype, x, q, sp.ldq, scale, s);
+    const hipError_t err = launch_quantize_rows(d.M, d.K, d.ld_x, d.x_dtype, x, q, sp.ldq, scale, e.kind != LinearEpilogue::kPlain, s);
     if (err != hipSuccess) return done(ctx, err);
     rows = q;
     x_scale = scale;
@@ -267,7 +267,7 @@ int c3c_quantize_rows(c3c_ctx* ctx, int64_t T, int64_t C, int64_t ld_x, int dtyp
   if (!why) why = check_spans(out, 2);
   if (!why) why = check_overlap(in, 1, out, 2, nullptr, 0);
   if (why) return fail(ctx, C3C_E_INVAL, why);
-  return done(ctx, launch_quantize_rows(T, C, ld_x, dtype, x, q, C, scale, static_cast<hipStream_t>(stream)));
+  return done(ctx, launch_quantize_rows(T, C, ld_x, dtype, x, q, C, scale, false, static_cast<hipStream_t>(stream)));
 }
 
 int c3c_linear_i8_workspace_bytes(const c3c_linear_desc* d, size_t* bytes) {

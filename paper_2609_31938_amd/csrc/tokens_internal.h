@@ -24,9 +24,10 @@ hipError_t in_launches(int64_t workgroups, int64_t threads, F launch) {
   return e;
 }
 
-// quantize_rows and norm_gate (norm_gate.hip)
+// quantize_rows and norm_gate (norm_gate.hip).  exact: codes nearest to
+// 127 x / max|x| itself, not to x over the rounded scale
 hipError_t launch_quantize_rows(int64_t T, int64_t C, int64_t ld_x, int dtype, const void* x,
-                                int8_t* q, int64_t ld_q, float* scale, hipStream_t s);
+                                int8_t* q, int64_t ld_q, float* scale, bool exact, hipStream_t s);
 hipError_t launch_norm_gate(const c3c_norm_desc& d, const void* h, const void* y, const void* gate,
                             const float* post, const float* pre, void* h_out, void* u, int8_t* u_q,
                             float* u_scale, hipStream_t s);

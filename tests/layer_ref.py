@@ -48,6 +48,16 @@ def state_tolerance(n, sizes):
     return EPS32 * (n + 6 * (n / 32 + 1) + 16) * sizes[0] + 4 * EPS32 * sizes[1]
 
 
+def quantize(x):
+    """(codes, scale fp32) of x (rows, n): the integers nearest to 127 x / max|x|."""
+    x = f64(x)
+    top = np.abs(x).max(1)
+    s = (top.astype(np.float32) / np.float32(127)).astype(np.float32)
+    with np.errstate(all="ignore"):
+        q = np.where(s[:, None] > 0, np.rint(x * 127 / top[:, None]), 0)
+    return q.astype(np.int8), s
+
+
 def act(z, name):
     """(act(z), bound on the relative error of its fp32 form without the
     argument's, bound on the absolute one)"""

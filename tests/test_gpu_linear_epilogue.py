@@ -33,10 +33,10 @@ def weights(N, K, seed=3):
 def epilogue_call(M, N, K, xd, yd, act="none", bias=True, residual=False, rows=0, alpha=0.9, in_place=False, ws=None, ld=None):
     """Runs the call and checks it."""
     x = ref.randn(5, M, ld or K)[:, :K]
-    q, s = ref.quantize(x) if xd == "i8" else (None, None)
+    q, s = layer_ref.quantize(x) if xd == "i8" else (None, None)
     if xd != "i8":
         x = x.to(ref.TORCH[xd])
-        q, s = ref.quantize(x)
+        q, s = layer_ref.quantize(x)
         xs = None
     else:
         x, xs = torch.from_numpy(q).cuda(), torch.from_numpy(s).cuda()
@@ -131,11 +131,11 @@ def test_nan_and_infinities_stay_where_they_are():
 def gated_call(M, N, K, xd, yd, act="silu", bias=True, ws=None, ld=None):
     x = ref.randn(5, M, ld or K)[:, :K]
     if xd == "i8":
-        q, s = ref.quantize(x)
+        q, s = layer_ref.quantize(x)
         x, xs = torch.from_numpy(q).cuda(), torch.from_numpy(s).cuda()
     else:
         x, xs = x.to(ref.TORCH[xd]), None
-        q, s = ref.quantize(x)
+        q, s = layer_ref.quantize(x)
     w, wscale, b = weights(2 * N, K)
     b = b if bias else None
     z, err = layer_ref.product(q, s, w, wscale, b)
@@ -176,9 +176,10 @@ def test_gated_halves_are_those_of_plain_products(M):
     """Without an activation, the product of two plain products in fp32, to a rounding."""
     N, K = 1100, 304
     x, (w, ws, b) = ref.randn(5, M, K).bfloat16(), weights(2 * N, K)
-    ctx = context(tokens.gated_linear_i8_workspace_bytes(M, N, K))
-    got = tokens.gated_linear_i8(ctx, x, w, ws, b, act="none", out_dtype="f32")
-    a, u = (tokens.linear_i8(ctx, x, w[s], ws[s], b[s], out_dtype="f32") for s in (slice(0, N), slice(N, 2 * N)))
+    ctx = context(tokens.gated_linear_i8_workspace_bytes(M, N, K, "i8"))
+    x, xs = tokens.quantize_rows(ctx, x)
+    got = tokens.gated_linear_i8(ctx, x, w, ws, b, x_scale=xs, act="none", out_dtype="f32")
+    a, u = (tokens.linear_i8(ctx, x, w[s], ws[s], b[s], x_scale=xs, out_dtype="f32") for s in (slice(0, N), slice(N, 2 * N)))
     assert torch.equal(got, a * u)
 
 
@@ -220,6 +221,25 @@ def test_gated_large_offsets():
     y = tokens.gated_linear_i8(c3c.Context(), x, w, ws, x_scale=s, act="silu")
     want = tokens.gated_linear_i8(c3c.Context(), x[-300:], w, ws, x_scale=s[-300:], act="silu")
     assert torch.equal(y[-300:], want) and (y[0] == 0).all()
+
+
+@pytest.mark.parametrize("M", [3, 50])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_codes_next_to_a_half(M, dtype):
+    """Values whose quotient by the rounded scale falls on the other side of a half
+    take the code of the true quotient: identity weights give the codes back."""
+    K = 1024
+    g = torch.Generator().manual_seed(8)
+    top = (1 + torch.rand(M, 1, generator=g)).to(ref.TORCH[dtype]).double()
+    k = torch.randint(-126, 126, (M, K), generator=g).double() + 0.5
+    x = (top * k / 127).to(ref.TORCH[dtype])
+    x[:, 0] = top[:, 0].to(x.dtype)
+    x = x.cuda()
+    w, one = torch.eye(K, dtype=torch.int8, device="cuda"), torch.ones(K, device="cuda")
+    ctx = context(tokens.linear_i8_workspace_bytes(M, K, K, dtype, "f32"))
+    y = tokens.linear_i8(ctx, x, w, one, out_dtype="f32", gate=torch.ones(1, K, device="cuda"), rows_per_gate=M)
+    q, s = layer_ref.quantize(x)
+    assert np.array_equal(y.cpu().numpy(), q.astype(np.float32) * s[:, None])
 
 
 def test_no_rows():
