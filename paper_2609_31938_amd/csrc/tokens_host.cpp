@@ -298,8 +298,8 @@ int c3c_linear_i8_epilogue(c3c_ctx* ctx, const c3c_linear_desc* d, const c3c_epi
   le.kind = e->act != C3C_ACT_NONE || e->gate || e->residual ? LinearEpilogue::kEpilogue : LinearEpilogue::kPlain;
   le.act = e->act;
   le.alpha = e->alpha;
-  // rows of M < 2^31 tokens: as many as that share a row of gates as all
-  le.rows_per_gate = static_cast<uint32_t>(!e->gate ? 1 : e->rows_per_gate < kBig ? e->rows_per_gate : kBig);
+  // M < 2^31 tokens: without gates, or with so many under one row, all are alike
+  le.rows_per_gate = static_cast<uint32_t>(e->gate && e->rows_per_gate < kBig ? e->rows_per_gate : kBig);
   le.gate = e->gate;
   le.residual = e->residual;
   return run_linear(ctx, *d, le, x, x_scale, w, w_scale, bias, y, stream);

@@ -266,3 +266,49 @@ def test_no_tokens():
     c = Case([0, 0], [3, 0], extra=0)
     out, state = c.run(max_new=1)
     assert out.shape[0] == 0 and torch.equal(state, c.state)
+
+
+@pytest.mark.parametrize("n", [1, 6])
+def test_more_workgroups_than_one_launch_takes(n):
+    """65535 sequences x 260 heads, a workgroup of 256 threads each: 2^32 threads
+    and more; all but two of the states outside of the slots."""
+    B, H = 65535, 260
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, k = (torch.randn(B * n, 1, 16, generator=g, device="cuda").bfloat16() for _ in range(2))
+    v = torch.randn(B * n, H, 16, generator=g, device="cuda").bfloat16()
+    decay = torch.full((H,), -0.25, device="cuda")
+    cu = torch.arange(B + 1, device="cuda").int() * n
+    b = tokens.Batch(torch.empty(B, 0, dtype=torch.int32, device="cuda"), cu, torch.full((B,), n + 1, dtype=torch.int32, device="cuda"),
+                     max_new=n, max_len=n + 1)
+    slots = torch.full((B,), -1, dtype=torch.int32, device="cuda")
+    slots[3], slots[B - 1] = 1, 0
+    first = ref.randn(6, 2, H, 16, 16)
+    st = tokens.StateCache(first.clone())
+    out = tokens.linear_attention(c3c.Context(), st, b, q, k, v, decay, slots=slots)
+    for s in (0, 3, 32000, 64000, 65000, B - 2, B - 1):
+        rows, slot = slice(s * n, s * n + n), int(slots[s])
+        S = ref.f64(first[slot]) if slot >= 0 else np.zeros((H, 16, 16))
+        args = [ref.f64(x[rows]) for x in (q, k, v)] + [np.broadcast_to(ref.f64(decay), (n, H))]
+        want, end, so, se = layer_ref.linear_attention(*args, S, 0.25)
+        ref.assert_within(out[rows], want, layer_ref.attention_tolerance("bf16", want, so, n, 16), s)
+        if slot >= 0:
+            ref.assert_within(st.state[slot], end, layer_ref.state_tolerance(n, se), s)
+
+
+@pytest.mark.parametrize("new", [[3, 1], [40, 90]])
+def test_two_streams_with_contexts_of_their_own(new):
+    """Calls that overlap in time, each with its workspace and states."""
+    c = Case(new, [3, 0], 4, 2, 64, 64)
+    want, batch = c.run(), c.batch()
+    n = max(tokens.linear_attention_workspace_bytes(tokens.StateCache(c.state), batch, c.q), 256)
+    jobs = []
+    for _ in range(2):
+        ctx, st, s = c3c.Context(), tokens.StateCache(c.state.clone()), torch.cuda.Stream()
+        ctx.set_workspace(torch.empty(n, dtype=torch.uint8, device="cuda"))
+        jobs.append((ctx, st, s, torch.empty_like(c.v)))
+    torch.cuda.synchronize()
+    for ctx, st, s, out in jobs:
+        tokens.linear_attention(ctx, st, batch, c.q, c.k, c.v, c.g, slots=c.slot, out=out, stream=s)
+    torch.cuda.synchronize()
+    for _, st, _, out in jobs:
+        assert torch.equal(out[:c.T], want[0][:c.T]) and torch.equal(st.state, want[1])
