@@ -569,7 +569,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
     // Onto a residual without an activation (of 16 bits, a whole tile, its tokens
     // under one row of gates): everything is read before anything is stored, since
     // a load is waited for with every store before it, and all workgroups are
-    // here at once.
+    // here at once (32760 x 5120 x 5120: 905 us, through LDS 1017, without a residual
+    // 790; loads past the caches 926).
     const uint32_t group = static_cast<uint32_t>(m0) / a.e.rows_per_gate;
     if (!a.part && a.e.act == C3C_ACT_NONE && a.e.residual && a.y_dtype != C3C_DTYPE_F32 && n0 + BN <= a.N &&
         static_cast<uint32_t>(m0 + mrows - 1) / a.e.rows_per_gate == group) {

@@ -58,6 +58,8 @@ class Case:
                 seen.add(s)
                 first = S[s] if o else np.zeros_like(S[s])
                 want, end, so, se = layer_ref.linear_attention(q[rows], k[rows], v[rows], g[rows], first, scale)
+                if self.dtype == "f16":  # 65520 and more are nearer to 2^16, which is infinite, than to 65504
+                    want = np.where(np.abs(want) >= 65520, np.copysign(np.inf, want), want)
                 ref.assert_within(out[rows], want, layer_ref.attention_tolerance(self.dtype, want, so, n, q.shape[2]), b)
                 ref.assert_within(state[s], end, layer_ref.state_tolerance(n, se), ("state", b))
             at += n
@@ -312,3 +314,38 @@ def test_two_streams_with_contexts_of_their_own(new):
     torch.cuda.synchronize()
     for _, st, _, out in jobs:
         assert torch.equal(out[:c.T], want[0][:c.T]) and torch.equal(st.state, want[1])
+
+
+@pytest.mark.parametrize("dtype,size", [("bf16", 2.0 ** 20), ("bf16", 2.0 ** 90), ("f16", 2.0 ** 12), ("f32", 2.0 ** 40), ("f32", 2.0 ** -60)])
+@pytest.mark.parametrize("new", [[4], [70, 3]])
+def test_large_and_small_values(dtype, size, new):
+    """Powers of two of ordinary values: the same results times that power."""
+    c = Case(new, [2] * len(new), 2, 1, 64, 80, dtype)
+    c.v, c.state = c.v * size, c.state * size
+    assert c.v.isfinite().all()
+    out, state = c.run()
+    c.check((torch.where(torch.arange(len(out), device="cuda")[:, None, None] < c.T, out, 7), state))
+
+
+@pytest.mark.parametrize("new", [[1], [3, 2], [50, 20]])
+def test_decays_in_strided_rows_and_one_row_for_all(new):
+    c = Case(new, [2] * len(new), 4, 2, 32, 32)
+    want = c.run()
+    wide = torch.full((c.g.shape[0], 9), float("nan"), device="cuda")
+    wide[:, 3:7] = c.g
+    c.g = wide[:, 3:7]
+    got = c.run()
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+    c.g = c.g[1].contiguous()
+    want = c.run()
+    c.g = c.g.expand(c.q.shape[0], 4)
+    got = c.run()
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+def test_no_sequences():
+    st = tokens.StateCache.empty(2, 2, 16, 16)
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32, device="cuda")  # noqa: E731
+    b = tokens.Batch(i32(0, 0), i32(1), i32(0), max_new=1, max_len=1)
+    e = torch.empty(0, 2, 16, device="cuda")
+    assert tokens.linear_attention(c3c.Context(), st, b, e, e, e, torch.zeros(2, device="cuda")).shape == (0, 2, 16)
