@@ -285,7 +285,7 @@ __global__ __launch_bounds__(1024) void quantize_loop(QuantArgs a) {
   const float s = row_scale(top);
   for (int64_t c = threadIdx.x; c < a.ld_q; c += blockDim.x) {
     const float v = c < a.C ? E::widen(x[c]) : 0.f;
-    a.q[t * a.ld_q + c] = static_cast<int8_t>(a.exact && near_half(v, s) ? true_code(v, s, top) : code(v, s));
+    a.q[t * a.ld_q + c] = static_cast<int8_t>(a.exact && doubtful(v, s) ? true_code(v, s, top) : code(v, s));
   }
   if (threadIdx.x == 0) a.scale[t] = s;
 }

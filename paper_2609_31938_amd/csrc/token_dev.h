@@ -120,11 +120,12 @@ __device__ inline int code(float v, float s) {
 }
 
 // The integer nearest to 127 v / top itself (top: the row's largest magnitude), not
-// to v / s with its rounded scale: the two differ only next to a half, as near_half
-// says (v / s errs by less than 2^-16).
-__device__ inline bool near_half(float v, float s) {
+// to v / s with its rounded scale.  The two differ only where a code is doubtful:
+// next to a half (v / s errs by less than 2^-16), or anywhere under a subnormal
+// scale, which has few bits.
+__device__ inline bool doubtful(float v, float s) {
   const float t = v / s;
-  return fabsf(fabsf(t - rintf(t)) - 0.5f) < 0x1p-15f;
+  return s < 0x1p-126f || fabsf(fabsf(t - rintf(t)) - 0.5f) < 0x1p-15f;
 }
 __device__ inline int true_code(float v, float s, float top) {
   return s > 0.f ? static_cast<int>(rint(static_cast<double>(v) * 127.0 / static_cast<double>(top))) : 0;
@@ -141,7 +142,7 @@ __device__ inline void store_codes(int8_t* p, int m, const float (&v)[N], float 
   if (top > 0.f) {
     bool any = false;
 #pragma unroll
-    for (int e = 0; e < N; ++e) any |= near_half(v[e], s);
+    for (int e = 0; e < N; ++e) any |= doubtful(v[e], s);
     if (__builtin_expect(any, 0)) {
 #pragma unroll
       for (int i = 0; i < (N + 3) / 4; ++i) w[i] = 0;

@@ -57,3 +57,38 @@ def test_gelu_keeps_its_relative_accuracy(yd, M, N, K, gated):
         y = tokens.linear_i8(ctx, x, w, ws, bias, x_scale=one, out_dtype=yd, act="gelu")
     assert torch.equal(y, y[:1].expand(M, N))
     ref.assert_within(y[0], want, (ref.UNIT[yd] + rel) * np.abs(want) + ref.TINY[yd])
+
+
+# ---------------------------------------------------------------- rows of tiny values
+
+# quantised by the product itself, in a wave's registers, in a workgroup's, in a loop
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K", [(3, 500), (50, 500), (9, 4000), (6, 33000)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_codes_of_rows_whose_scale_is_subnormal(dtype, M, K, gated):
+    """They are those of the true quotient, however few bits the scale has; a row
+    whose scale rounds to 0 is 0.  Weights of a single 1 give codes back, times the
+    row's scale and a power of two: nothing but that product is rounded."""
+    N, unit = 64, 2.0 ** (-149 if dtype == "f32" else -133)
+    g = torch.Generator().manual_seed(4)
+    top = torch.tensor([1, 63, 64, 100, 190, 191, 300, 1000, 12345, 2.0 ** 20])[torch.arange(M) % 10] * unit
+    x = ((2 * torch.rand(M, K, generator=g, dtype=torch.float64) - 1) * top.double()[:, None]).to(ref.TORCH[dtype])
+    x[:, 0] = top.to(x.dtype)
+    q, s = layer_ref.quantize(x)
+    normal = s >= 2.0 ** -126
+    assert not normal[np.arange(M) % 10 < 9].any() and (dtype == "bf16" or not normal.any())
+    at = torch.randperm(K - 1, generator=g)[:N] + 1
+    at[0] = 0
+    w = torch.zeros(N, K, dtype=torch.int8)
+    w[torch.arange(N), at] = 1
+    scale = np.float32(2.0 ** 100)
+    z = (q[:, at.numpy()].astype(np.float32) * s[:, None]) * scale
+    ws = torch.full((N,), float(scale), device="cuda")
+    if gated:
+        ctx = context(tokens.gated_linear_i8_workspace_bytes(M, N // 2, K, dtype, "f32"))
+        y = tokens.gated_linear_i8(ctx, x.cuda(), w.cuda(), ws, out_dtype="f32", act="none")
+        z = z[:, :N // 2] * z[:, N // 2:]
+    else:
+        ctx = context(tokens.linear_i8_workspace_bytes(M, N, K, dtype, "f32"))
+        y = tokens.linear_i8(ctx, x.cuda(), w.cuda(), ws, out_dtype="f32", gate=torch.ones(1, N, device="cuda"), rows_per_gate=M)
+    assert np.array_equal(y.cpu().numpy(), z)
