@@ -85,12 +85,19 @@ int c3c_linear_attention(c3c_ctx* ctx, const c3c_state_cache* states, const c3c_
 enum { C3C_ACT_NONE = 0, C3C_ACT_SILU = 1, C3C_ACT_GELU = 2, C3C_ACT_GELU_TANH = 3 };
 
 /* z = c3c_linear_i8's result, before its rounding; for token m and channel n
- * (with float activations' codes, here and in c3c_gated_linear_i8, the integers
- * nearest to 127 x / max|x| themselves: c3c_quantize_rows rounds the scale first,
- * which differs by one step for the few values next to a half)
  *   y = alpha * residual[m][n] + gate[m / rows_per_gate][n] * act(z)
  * residual [M][N], gate [ceil(M / rows_per_gate)][N], both of y_dtype and
  * contiguous; NULL: no residual, a gate of ones.  y may be the residual itself.
+ * Codes of float activations, here and in c3c_gated_linear_i8: the integers
+ * nearest to 127 x / max|x| themselves, ties to even; 0 in rows whose scale
+ * rounds to 0.  c3c_linear_i8 and c3c_quantize_rows divide by the rounded scale
+ * instead, which differs by one step for the few values next to a half, by more
+ * where the scale is subnormal: a caller who needs one set of codes for several
+ * products quantises once and passes int8.  With C3C_ACT_NONE, no gate and no
+ * residual the call is c3c_linear_i8, its codes included; every call of
+ * c3c_gated_linear_i8 takes the codes stated here.
+ * Activations are relatively accurate where they tend to 0 as well, down to
+ * magnitudes of 2^-118, below which they may be 0.
  * The workspace is that of c3c_linear_i8 (c3c_linear_i8_workspace_bytes).
  * EINVAL: as c3c_linear_i8; NULL e; unknown act; alpha not finite;
  * rows_per_gate < 1 with a gate; y overlapping a residual that it is not. */

@@ -198,7 +198,12 @@ def linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=N
     With an epilogue y = alpha residual + gate act(that), rounded once: ``act``
     "none", "silu", "gelu" (by erf) or "gelu_tanh"; residual (M, N) and gate
     (groups, N), one row for ``rows_per_gate`` tokens, of y's dtype.  ``out`` may
-    be the residual."""
+    be the residual.
+
+    Float activations are quantised by quantize_rows' rule, which divides by the
+    rounded scale; with an epilogue the codes are the integers nearest to 127 x /
+    max|x| themselves.  The two differ by a step for the few values next to a
+    half: quantise once and pass int8 where several products have to share codes."""
     M, K, ld, xd, yd = _linear_args(x, out, out_dtype)
     N = w.shape[0]
     ydt = _TORCH[yd]
@@ -236,7 +241,7 @@ def gated_linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_d
     """y (M, N) = act(x w_g^T + b_g) * (x w_u^T + b_u), the first half of a gated
     feed-forward block: w (2 N, K) int8 holds the gate's rows, then the others,
     w_scale and bias (2 N,) fp32.  x, x_scale, out and out_dtype as linear_i8
-    takes them; the context needs gated_linear_i8_workspace_bytes."""
+    with an epilogue takes them; the context needs gated_linear_i8_workspace_bytes."""
     _here(x)
     M, K, ld, xd, yd = _linear_args(x, out, out_dtype)
     rows = w.shape[0]

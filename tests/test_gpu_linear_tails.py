@@ -59,6 +59,25 @@ def test_gelu_keeps_its_relative_accuracy(yd, M, N, K, gated):
     ref.assert_within(y[0], want, (ref.UNIT[yd] + rel) * np.abs(want) + ref.TINY[yd])
 
 
+@pytest.mark.parametrize("M,N,K", [(2, 300, 64), (80, 300, 64)])
+@pytest.mark.parametrize("act,low", [("silu", -80), ("gelu_tanh", -9.5)])
+def test_silu_and_gelu_tanh_keep_theirs(M, N, K, act, low):
+    """z / (1 + exp(-u)): the roundings of u log2(e) (two where u is z; two of
+    constants and products, a sum's and four of the cube where it is a polynomial)
+    enter times |u|; the exponential's and the reciprocal's ulp, a sum and a
+    product."""
+    z = np.linspace(low, 3, N).astype(np.float32)
+    x, one = torch.zeros(M, K, dtype=torch.int8, device="cuda"), torch.ones(M, device="cuda")
+    w, ws = torch.ones(N, K, dtype=torch.int8, device="cuda"), torch.ones(N, device="cuda")
+    ctx = context(tokens.linear_i8_workspace_bytes(M, N, K, "i8", "f32"))
+    y = tokens.linear_i8(ctx, x, w, ws, torch.from_numpy(z).cuda(), x_scale=one, out_dtype="f32", act=act)
+    z = z.astype(np.float64)
+    u, n = (z, 2) if act == "silu" else (2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3), 9)
+    want = z / (1 + np.exp(-u))
+    assert torch.equal(y, y[:1].expand(M, N))
+    ref.assert_within(y[0], want, (n * np.abs(u) + 7) * ref.EPS32 * np.abs(want))
+
+
 # ---------------------------------------------------------------- rows of tiny values
 
 # quantised by the product itself, in a wave's registers, in a workgroup's, in a loop
@@ -92,3 +111,36 @@ def test_codes_of_rows_whose_scale_is_subnormal(dtype, M, K, gated):
         ctx = context(tokens.linear_i8_workspace_bytes(M, N, K, dtype, "f32"))
         y = tokens.linear_i8(ctx, x.cuda(), w.cuda(), ws, out_dtype="f32", gate=torch.ones(1, N, device="cuda"), rows_per_gate=M)
     assert np.array_equal(y.cpu().numpy(), z)
+
+
+# ---------------------------------------------------------------- whose codes
+
+@pytest.mark.parametrize("M", [3, 50])
+def test_each_call_takes_the_codes_that_its_documentation_says(M):
+    """Values next to a half, where the two rules differ: the plain product has
+    quantize_rows' codes, an epilogue (a residual of zeros is one) and a gated
+    product those of the true quotient, and int8 codes are taken as they are."""
+    K = 1024
+    g = torch.Generator().manual_seed(8)
+    top = 1 + torch.rand(M, 1, generator=g).double()
+    x = (top * (torch.randint(-126, 126, (M, K), generator=g).double() + 0.5) / 127).float()
+    x[:, 0] = top[:, 0].float()
+    (by_scale, s), (true, _) = ref.quantize(x), layer_ref.quantize(x)
+    assert (by_scale != true).any()
+    x, w, one = x.cuda(), torch.eye(K, dtype=torch.int8, device="cuda"), torch.ones(K, device="cuda")
+    ctx = context(tokens.gated_linear_i8_workspace_bytes(M, K, K, "f32", "f32"))
+
+    def same(y, codes):
+        return np.array_equal(y.cpu().numpy(), codes.astype(np.float32) * s[:, None])
+
+    zero = torch.zeros(M, K, device="cuda")
+    q, xs = tokens.quantize_rows(ctx, x)
+    assert np.array_equal(q.cpu().numpy(), by_scale)
+    assert same(tokens.linear_i8(ctx, x, w, one), by_scale)
+    assert same(tokens.linear_i8(ctx, x, w, one, residual=zero), true)
+    assert same(tokens.linear_i8(ctx, q, w, one, x_scale=xs, out_dtype="f32", residual=zero), by_scale)
+    # the second half of the gated product is 1 in every channel
+    both, bias = torch.cat([w, torch.zeros_like(w)]), torch.cat([0 * one, one])
+    args = both, torch.cat([one, one]), bias
+    assert same(tokens.gated_linear_i8(ctx, x, *args, act="none"), true)
+    assert same(tokens.gated_linear_i8(ctx, q, *args, x_scale=xs, out_dtype="f32", act="none"), by_scale)
