@@ -117,6 +117,18 @@ def _here(t):
         raise ValueError(f"the tensors are on device {t.get_device()}, the current one is {_device()}")
 
 
+def _together(ctx, t, *others):
+    """Refuses a call one of whose tensors (None: not given), or whose context's
+    workspace, is on another device than t: a kernel does not reach it."""
+    device = t.get_device()
+    for o in others:
+        if o is not None and o.get_device() != device:
+            raise ValueError(f"the tensors of a call are on devices {device} and {o.get_device()}")
+    ws = getattr(ctx, "_ws", None)
+    if ws is not None and ws.get_device() != device:
+        raise ValueError(f"the tensors are on device {device}, the context's workspace on {ws.get_device()}")
+
+
 def _addr(t, name):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
@@ -223,6 +235,7 @@ def linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=N
     groups = -(-M // rows_per_gate) if rows_per_gate > 0 else 0
     e = _Epilogue(None if gate is None else _check(gate, "gate", ydt, (groups, N)),
                   None if residual is None else _check(residual, "residual", ydt, (M, N)), rows_per_gate, alpha, _act(act))
+    _together(ctx, x, w, w_scale, bias, x_scale, out, residual, gate)
     st = lib.c3c_linear_i8_epilogue(ctx._h, C.byref(d), C.byref(e), *args)
     if st:
         _raise(st, ctx, "c3c_linear_i8_epilogue")
@@ -251,11 +264,11 @@ def gated_linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_d
     if out is None:
         out = x.new_empty((M, N), dtype=ydt)
     d = LinearDesc(M, N, K, ld, DTYPES[xd], DTYPES[yd])
-    st = lib.c3c_gated_linear_i8(
-        ctx._h, C.byref(d), _act(act), _addr(x, "x"),
-        None if x_scale is None else _check(x_scale, "x_scale", torch.float32, (M,)), _check(w, "w", torch.int8, (rows, K)),
-        _check(w_scale, "w_scale", torch.float32, (rows,)), None if bias is None else _check(bias, "bias", torch.float32, (rows,)),
-        _check(out, "out", ydt, (M, N)), _stream(stream, x))
+    args = (_act(act), _addr(x, "x"), None if x_scale is None else _check(x_scale, "x_scale", torch.float32, (M,)),
+            _check(w, "w", torch.int8, (rows, K)), _check(w_scale, "w_scale", torch.float32, (rows,)),
+            None if bias is None else _check(bias, "bias", torch.float32, (rows,)), _check(out, "out", ydt, (M, N)))
+    _together(ctx, x, w, w_scale, bias, x_scale, out)
+    st = lib.c3c_gated_linear_i8(ctx._h, C.byref(d), *args, _stream(stream, x))
     if st:
         _raise(st, ctx, "c3c_gated_linear_i8")
     return out
@@ -488,9 +501,11 @@ def linear_attention(ctx, states: StateCache, batch: Batch, q, k, v, log_decay, 
     if out is None:
         out = q.new_empty((T, heads, states.dim_v))
     ps = None if slots is None else _check(slots, "slots", torch.int32, batch.lens.shape)
+    po = _check(out, "out", dt, (T, heads, states.dim_v))
+    _together(ctx, q, k, v, log_decay, out, slots, states.state, batch.cu, batch.lens)
     st = lib.c3c_linear_attention(
         ctx._h, C.byref(states._d), batch._of(T), ps, DTYPES[dtype], qk_heads, pq, ldq, pk, ldk, pv, ldv, pg, ldg,
-        states.dim_k ** -0.5 if scale is None else scale, _check(out, "out", dt, (T, heads, states.dim_v)), _stream(stream, q))
+        states.dim_k ** -0.5 if scale is None else scale, po, _stream(stream, q))
     if st:
         _raise(st, ctx, "c3c_linear_attention")
     return out

@@ -1,0 +1,103 @@
+"""A recurrent layer's operators refuse tensors of several devices: a kernel would
+read or write memory that it does not reach.  On the CPU, with tensors that say
+where they are; a call that were not refused would end in the library's refusal
+of its missing workspace or NULL tensor, before any device access."""
+import pytest
+import torch
+
+from paper_2609_31938_amd import c3c, tokens
+
+no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="fake-device argument tests run on CPU-only hosts")
+
+
+class On:
+    """A tensor of no address that says it is on a device."""
+
+    def __init__(self, t, device=0):
+        self.t, self.device = t, device
+
+    def __getattr__(self, name):
+        return {"is_cuda": True, "get_device": lambda: self.device, "data_ptr": lambda: 0}.get(name) or getattr(self.t, name)
+
+
+def refused(name, call, args, match="devices 0 and 1"):
+    args = dict(args)
+    args[name] = On(args[name].t, 1)
+    with pytest.raises(ValueError, match=match):
+        call(args)
+
+
+@pytest.fixture
+def ctx(monkeypatch):
+    monkeypatch.setattr(tokens, "_device", lambda: 0)
+    monkeypatch.setattr(tokens, "_raw_stream", lambda device: None)
+    return c3c.Context()
+
+
+def elsewhere(ctx):
+    ctx._ws = On(torch.zeros(16, dtype=torch.uint8), 1)
+
+
+@no_gpu
+@pytest.mark.parametrize("name", ["w", "w_scale", "bias", "x_scale", "out", "residual", "gate", "workspace"])
+def test_product_with_an_epilogue(ctx, name):
+    M, N, K = 4, 6, 16
+    args = dict(x=On(torch.zeros(M, K, dtype=torch.int8)), w=On(torch.zeros(N, K, dtype=torch.int8)), w_scale=On(torch.zeros(N)),
+                bias=On(torch.zeros(N)), x_scale=On(torch.zeros(M)), out=On(torch.zeros(M, N)), residual=On(torch.zeros(M, N)),
+                gate=On(torch.zeros(M, N)))
+
+    def call(a):
+        return tokens.linear_i8(ctx, **a)
+
+    with pytest.raises(c3c.C3CError):
+        call(args)
+    if name == "workspace":
+        elsewhere(ctx)
+        with pytest.raises(ValueError, match="workspace on 1"):
+            call(args)
+    else:
+        refused(name, call, args)
+
+
+@no_gpu
+@pytest.mark.parametrize("name", ["w", "w_scale", "bias", "x_scale", "out", "workspace"])
+def test_gated_product(ctx, name):
+    M, N, K = 4, 6, 16
+    args = dict(x=On(torch.zeros(M, K, dtype=torch.int8)), w=On(torch.zeros(2 * N, K, dtype=torch.int8)),
+                w_scale=On(torch.zeros(2 * N)), bias=On(torch.zeros(2 * N)), x_scale=On(torch.zeros(M)), out=On(torch.zeros(M, N)))
+
+    def call(a):
+        return tokens.gated_linear_i8(ctx, **a)
+
+    with pytest.raises(c3c.C3CError):
+        call(args)
+    if name == "workspace":
+        elsewhere(ctx)
+        with pytest.raises(ValueError, match="workspace on 1"):
+            call(args)
+    else:
+        refused(name, call, args)
+
+
+@no_gpu
+@pytest.mark.parametrize("name", ["k", "v", "log_decay", "out", "slots", "state", "cu", "lens", "workspace"])
+def test_linear_attention(ctx, name):
+    T, H, D, i32 = 3, 2, 16, torch.int32
+    args = dict({n: On(torch.zeros(T, H, D)) for n in ("q", "k", "v", "out")}, log_decay=On(torch.zeros(H)),
+                slots=On(torch.zeros(1, dtype=i32)), state=On(torch.zeros(1, H, D, D)), cu=On(torch.zeros(2, dtype=i32)),
+                lens=On(torch.zeros(1, dtype=i32)))
+
+    def call(a):
+        a = dict(a)
+        states = tokens.StateCache(a.pop("state"))
+        batch = tokens.Batch(On(torch.zeros(1, 0, dtype=i32)), a.pop("cu"), a.pop("lens"), max_new=T, max_len=T)
+        return tokens.linear_attention(ctx, states, batch, a.pop("q"), a.pop("k"), a.pop("v"), a.pop("log_decay"), **a)
+
+    with pytest.raises(c3c.C3CError):
+        call(args)
+    if name == "workspace":
+        elsewhere(ctx)
+        with pytest.raises(ValueError, match="workspace on 1"):
+            call(args)
+    else:
+        refused(name, call, args)
