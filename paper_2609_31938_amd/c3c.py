@@ -137,6 +137,8 @@ def _raise(status, ctx=None, what=""):
 class Context:
     """A c3c_ctx: mode bits, route counters and the fallback-shape histogram."""
 
+    _ws_device = None  # of the attached workspace
+
     def __init__(self, mode: int = 0):
         h = _vp()
         _raise(lib.c3c_ctx_create(mode, C.byref(h)), what="c3c_ctx_create")
@@ -194,14 +196,14 @@ class Context:
         The context keeps a reference so the memory outlives its use."""
         if ws is None:
             _raise(lib.c3c_ctx_set_workspace(self._h, None, 0), self, "c3c_ctx_set_workspace")
-            self._ws = None
+            self._ws = self._ws_device = None
             return
         if not ws.is_cuda or not ws.is_contiguous():
             raise ValueError("workspace must be a contiguous device tensor")
         nbytes = ws.numel() * ws.element_size()
         _raise(lib.c3c_ctx_set_workspace(self._h, ws.data_ptr() or None, nbytes), self,
                "c3c_ctx_set_workspace")
-        self._ws = ws
+        self._ws, self._ws_device = ws, ws.get_device()
 
 
 # ---------------------------------------------------------------- host maths

@@ -111,31 +111,29 @@ _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_devic
 
 
 def _here(t):
-    """Refuses a call whose tensors are not on the current device: a stream given
-    as 0 is the current device's."""
-    if t.is_cuda and t.get_device() != _device():
-        raise ValueError(f"the tensors are on device {t.get_device()}, the current one is {_device()}")
-
-
-def _together(ctx, t, *others):
-    """Refuses a call one of whose tensors (None: not given), or whose context's
-    workspace, is on another device than t: a kernel does not reach it."""
+    """The device of a call's first tensor.  Refuses one that is not the current
+    device: a stream given as 0 is the current device's."""
     device = t.get_device()
-    for o in others:
-        if o is not None and o.get_device() != device:
-            raise ValueError(f"the tensors of a call are on devices {device} and {o.get_device()}")
-    ws = getattr(ctx, "_ws", None)
-    if ws is not None and ws.get_device() != device:
-        raise ValueError(f"the tensors are on device {device}, the context's workspace on {ws.get_device()}")
+    if device != _device() and t.is_cuda:
+        raise ValueError(f"the tensors are on device {device}, the current one is {_device()}")
+    return device
 
 
-def _addr(t, name):
+def _not_there(t, name, device):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
+    raise ValueError(f"{name} is on device {t.get_device()}, the call's first tensor on {device}")
+
+
+def _addr(t, name, device=None):
+    """The device address of a tensor; on ``device`` where that is given (in place
+    of the question whether it is on any: either takes the host 0.2 us)."""
+    if not t.is_cuda if device is None else t.get_device() != device:
+        _not_there(t, name, device)
     return t.data_ptr() or None
 
 
-def _check(t, name, dtype, shape):
+def _check(t, name, dtype, shape, device=None):
     """The device address of a contiguous tensor of this dtype and shape."""
     if t.dtype is not dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
@@ -143,9 +141,16 @@ def _check(t, name, dtype, shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
+    if not t.is_cuda if device is None else t.get_device() != device:
+        _not_there(t, name, device)
     return t.data_ptr() or None
+
+
+def _workspace(ctx, device):
+    """Refuses a context whose workspace is on another device than the call's
+    tensors: a kernel does not reach it."""
+    if ctx._ws_device is not None and ctx._ws_device != device:
+        raise ValueError(f"the context's workspace is on device {ctx._ws_device}, the call's tensors on {device}")
 
 
 def _float_dtype(t, name):
@@ -222,20 +227,21 @@ def linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=N
     if out is None:
         out = x.new_empty((M, N), dtype=ydt)
     d = LinearDesc(M, N, K, ld, DTYPES[xd], DTYPES[yd])
-    args = (_addr(x, "x"), None if x_scale is None else _check(x_scale, "x_scale", torch.float32, (M,)),
-            _check(w, "w", torch.int8, (N, K)), _check(w_scale, "w_scale", torch.float32, (N,)),
-            None if bias is None else _check(bias, "bias", torch.float32, (N,)), _check(out, "out", ydt, (M, N)),
+    plain = act == "none" and residual is None and gate is None
+    at = None if plain else _here(x)
+    args = (_addr(x, "x"), None if x_scale is None else _check(x_scale, "x_scale", torch.float32, (M,), at),
+            _check(w, "w", torch.int8, (N, K), at), _check(w_scale, "w_scale", torch.float32, (N,), at),
+            None if bias is None else _check(bias, "bias", torch.float32, (N,), at), _check(out, "out", ydt, (M, N), at),
             _stream(stream, x))
-    if act == "none" and residual is None and gate is None:
+    if plain:
         st = lib.c3c_linear_i8(ctx._h, C.byref(d), *args)
         if st:
             _raise(st, ctx, "c3c_linear_i8")
         return out
-    _here(x)
     groups = -(-M // rows_per_gate) if rows_per_gate > 0 else 0
-    e = _Epilogue(None if gate is None else _check(gate, "gate", ydt, (groups, N)),
-                  None if residual is None else _check(residual, "residual", ydt, (M, N)), rows_per_gate, alpha, _act(act))
-    _together(ctx, x, w, w_scale, bias, x_scale, out, residual, gate)
+    e = _Epilogue(None if gate is None else _check(gate, "gate", ydt, (groups, N), at),
+                  None if residual is None else _check(residual, "residual", ydt, (M, N), at), rows_per_gate, alpha, _act(act))
+    _workspace(ctx, at)
     st = lib.c3c_linear_i8_epilogue(ctx._h, C.byref(d), C.byref(e), *args)
     if st:
         _raise(st, ctx, "c3c_linear_i8_epilogue")
@@ -255,7 +261,7 @@ def gated_linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_d
     feed-forward block: w (2 N, K) int8 holds the gate's rows, then the others,
     w_scale and bias (2 N,) fp32.  x, x_scale, out and out_dtype as linear_i8
     with an epilogue takes them; the context needs gated_linear_i8_workspace_bytes."""
-    _here(x)
+    at = _here(x)
     M, K, ld, xd, yd = _linear_args(x, out, out_dtype)
     rows = w.shape[0]
     if rows % 2:
@@ -264,10 +270,10 @@ def gated_linear_i8(ctx, x, w, w_scale, bias=None, x_scale=None, out=None, out_d
     if out is None:
         out = x.new_empty((M, N), dtype=ydt)
     d = LinearDesc(M, N, K, ld, DTYPES[xd], DTYPES[yd])
-    args = (_act(act), _addr(x, "x"), None if x_scale is None else _check(x_scale, "x_scale", torch.float32, (M,)),
-            _check(w, "w", torch.int8, (rows, K)), _check(w_scale, "w_scale", torch.float32, (rows,)),
-            None if bias is None else _check(bias, "bias", torch.float32, (rows,)), _check(out, "out", ydt, (M, N)))
-    _together(ctx, x, w, w_scale, bias, x_scale, out)
+    args = (_act(act), _addr(x, "x"), None if x_scale is None else _check(x_scale, "x_scale", torch.float32, (M,), at),
+            _check(w, "w", torch.int8, (rows, K), at), _check(w_scale, "w_scale", torch.float32, (rows,), at),
+            None if bias is None else _check(bias, "bias", torch.float32, (rows,), at), _check(out, "out", ydt, (M, N), at))
+    _workspace(ctx, at)
     st = lib.c3c_gated_linear_i8(ctx._h, C.byref(d), *args, _stream(stream, x))
     if st:
         _raise(st, ctx, "c3c_gated_linear_i8")
@@ -353,8 +359,9 @@ class Batch:
         B, cols = table.shape
         self.table, self.cu, self.lens, self.max_new, self.max_len = table, cu, lens, max_new, max_len
         i32 = torch.int32
-        self._d = _BatchDesc(_check(table, "table", i32, (B, cols)), _check(cu, "cu", i32, (B + 1,)),
-                             _check(lens, "lens", i32, (B,)), B, cols, 0, max_new, max_len)
+        self.device = table.get_device()
+        self._d = _BatchDesc(_check(table, "table", i32, (B, cols)), _check(cu, "cu", i32, (B + 1,), self.device),
+                             _check(lens, "lens", i32, (B,), self.device), B, cols, 0, max_new, max_len)
 
     def _of(self, T):
         # a descriptor is never changed once a call may have it: threads with
@@ -367,7 +374,7 @@ class Batch:
         return C.byref(d)
 
 
-def _heads(t, name, dtype, T, heads, dim):
+def _heads(t, name, dtype, T, heads, dim, device=None):
     """(address, token stride) of a (T, heads, dim) tensor whose tokens are
     contiguous; they may be strided, as slices of one projection are."""
     if t.dtype != dtype:
@@ -377,7 +384,7 @@ def _heads(t, name, dtype, T, heads, dim):
     by_token, by_head, by_channel = t.stride()
     if by_channel != 1 or (heads > 1 and by_head != dim):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return _addr(t, name), by_token if T > 1 else heads * dim
+    return _addr(t, name, device), by_token if T > 1 else heads * dim
 
 
 def kv_append(ctx, cache: KVCache, batch: Batch, k, v, *, q=None, cos=None, sin=None, pos=None, pairs="half",
@@ -456,7 +463,7 @@ class StateCache:
     def __init__(self, state):
         if state.dim() != 4:
             raise ValueError("state must be (slots, heads, dim_k, dim_v)")
-        self.state = state
+        self.state, self.device = state, state.get_device()
         slots, self.heads, self.dim_k, self.dim_v = state.shape
         self._d = _StateDesc(_check(state, "state", torch.float32, state.shape), *state.shape)
 
@@ -483,26 +490,29 @@ def linear_attention(ctx, states: StateCache, batch: Batch, q, k, v, log_decay, 
     ``slots`` (B,) int32: where each sequence's state lies (default: in order); a
     sequence whose tokens are all in this call begins at zero.  scale defaults to
     dim_k ** -0.5.  Returns out (T, heads, dim_v)."""
-    _here(q)
+    at = _here(q)
     dtype = _float_dtype(q, "q")
     T, qk_heads, _ = q.shape
     dt, heads = q.dtype, states.heads
     pq, ldq = _heads(q, "q", dt, T, qk_heads, states.dim_k)
-    pk, ldk = _heads(k, "k", dt, T, qk_heads, states.dim_k)
-    pv, ldv = _heads(v, "v", dt, T, heads, states.dim_v)
+    pk, ldk = _heads(k, "k", dt, T, qk_heads, states.dim_k, at)
+    pv, ldv = _heads(v, "v", dt, T, heads, states.dim_v, at)
     if log_decay.dtype is not torch.float32:
         raise ValueError(f"log_decay has dtype {log_decay.dtype}, expected {torch.float32}")
     if log_decay.dim() == 1:
-        pg, ldg = _check(log_decay, "log_decay", torch.float32, (heads,)), 0
+        pg, ldg = _check(log_decay, "log_decay", torch.float32, (heads,), at), 0
     else:
         if log_decay.shape != (T, heads):
             raise ValueError(f"log_decay has shape {tuple(log_decay.shape)}, expected {(heads,)} or {(T, heads)}")
-        pg, ldg = _addr(log_decay, "log_decay"), _rows(log_decay, "log_decay")
+        pg, ldg = _addr(log_decay, "log_decay", at), _rows(log_decay, "log_decay")
     if out is None:
         out = q.new_empty((T, heads, states.dim_v))
-    ps = None if slots is None else _check(slots, "slots", torch.int32, batch.lens.shape)
-    po = _check(out, "out", dt, (T, heads, states.dim_v))
-    _together(ctx, q, k, v, log_decay, out, slots, states.state, batch.cu, batch.lens)
+    ps = None if slots is None else _check(slots, "slots", torch.int32, batch.lens.shape, at)
+    po = _check(out, "out", dt, (T, heads, states.dim_v), at)
+    for name, device in (("state", states.device), ("batch", batch.device)):
+        if device != at:
+            raise ValueError(f"the {name} is on device {device}, the call's first tensor on {at}")
+    _workspace(ctx, at)
     st = lib.c3c_linear_attention(
         ctx._h, C.byref(states._d), batch._of(T), ps, DTYPES[dtype], qk_heads, pq, ldq, pk, ldk, pv, ldv, pg, ldg,
         states.dim_k ** -0.5 if scale is None else scale, po, _stream(stream, q))

@@ -13,14 +13,14 @@ no_gpu = pytest.mark.skipif(torch.cuda.is_available(), reason="fake-device argum
 class On:
     """A tensor of no address that says it is on a device."""
 
-    def __init__(self, t, device=0):
-        self.t, self.device = t, device
+    def __init__(self, t, index=0):
+        self.t, self.index = t, index
 
     def __getattr__(self, name):
-        return {"is_cuda": True, "get_device": lambda: self.device, "data_ptr": lambda: 0}.get(name) or getattr(self.t, name)
+        return {"is_cuda": True, "get_device": lambda: self.index, "data_ptr": lambda: 0}.get(name) or getattr(self.t, name)
 
 
-def refused(name, call, args, match="devices 0 and 1"):
+def refused(name, call, args, match="on device 1, the call's first tensor on 0"):
     args = dict(args)
     args[name] = On(args[name].t, 1)
     with pytest.raises(ValueError, match=match):
@@ -35,7 +35,7 @@ def ctx(monkeypatch):
 
 
 def elsewhere(ctx):
-    ctx._ws = On(torch.zeros(16, dtype=torch.uint8), 1)
+    ctx._ws_device = 1
 
 
 @no_gpu
@@ -53,7 +53,7 @@ def test_product_with_an_epilogue(ctx, name):
         call(args)
     if name == "workspace":
         elsewhere(ctx)
-        with pytest.raises(ValueError, match="workspace on 1"):
+        with pytest.raises(ValueError, match="workspace is on device 1"):
             call(args)
     else:
         refused(name, call, args)
@@ -73,7 +73,7 @@ def test_gated_product(ctx, name):
         call(args)
     if name == "workspace":
         elsewhere(ctx)
-        with pytest.raises(ValueError, match="workspace on 1"):
+        with pytest.raises(ValueError, match="workspace is on device 1"):
             call(args)
     else:
         refused(name, call, args)
@@ -97,7 +97,7 @@ def test_linear_attention(ctx, name):
         call(args)
     if name == "workspace":
         elsewhere(ctx)
-        with pytest.raises(ValueError, match="workspace on 1"):
+        with pytest.raises(ValueError, match="workspace is on device 1"):
             call(args)
     else:
         refused(name, call, args)
