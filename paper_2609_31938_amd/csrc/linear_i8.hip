@@ -90,11 +90,27 @@ __device__ inline Channels<EPI> channels(const LinArgs& a, int64_t n) {
   return c;
 }
 
+// z Phi(z), Phi the normal distribution: Phi(-a) = exp(-a^2 / 2) R(a) for a >= 0,
+// and 1 - that for a > 0 (z/2 (1 + erf) would cancel where z < 0: at -5 to 4% of the
+// result).  R, between 1/2 and 1 / (a sqrt(2 pi)), is t times a polynomial in t = 1 /
+// (1 + 0.35 a): the best one of degree 8, fitted to erfc in 64 bits (relative
+// error 2^-25 up to a = 15, where exp(-a^2 / 2) is 0).  Roundings leave 2^-21 for
+// |z| < 1 and 1.3 z^2 2^-24 of the exponent.  The library's erfc is as good and
+// longer: with it 8192 tokens x 8192 channels of 4096 take 353 us, so 309.
+__device__ inline float gelu(float z) {
+  const float a = fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.35f, a, 1.f));
+  constexpr float c[9] = {0.139621258f, 0.13986434f, 0.119815491f, 0.105574816f, -0.023263881f,
+                          0.159392983f, -0.255901933f, 0.144060835f, -0.0291639324f};
+  float r = c[8];
+#pragma unroll
+  for (int i = 7; i >= 0; --i) r = __builtin_fmaf(r, t, c[i]);
+  const float below = __builtin_amdgcn_exp2f(-0.721347520f * (a * a)) * (r * t);
+  return z * (z < 0.f ? below : 1.f - below);
+}
+
 __device__ inline float activate(int act, float z) {
   if (act == C3C_ACT_NONE) return z;
-  // z/2 (1 + erf(z / sqrt 2)) by the complement: the sum would cancel where z < 0
-  // (at -5 to 4% of the result)
-  if (act == C3C_ACT_GELU) return 0.5f * z * erfcf(-0.707106781f * z);
+  if (act == C3C_ACT_GELU) return gelu(z);
   // z / (1 + exp(-u)); u = z, or 2 sqrt(2 / pi) (z + 0.044715 z^3), since
   // (1 + tanh v) / 2 = 1 / (1 + exp(-2 v))
   const float u = act == C3C_ACT_SILU ? z : 1.59576912f * (z + 0.044715f * z * z * z);
