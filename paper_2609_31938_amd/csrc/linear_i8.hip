@@ -261,7 +261,7 @@ __device__ inline tok_i32x4 piece(const int8_t* p, int64_t m) {
     if (m > 0) v = *reinterpret_cast<const tok_i32x4*>(p);
   } else if (m >= 16) {
     __builtin_memcpy(&v, p, 16);
-  } else {
+  } else if (m > 0) {  // rows past the last would take all the branches in vain
 #pragma unroll
     for (int e = 0; e < 15; ++e)
       if (e < m) v[e >> 2] |= (static_cast<int32_t>(p[e]) & 255) << (8 * (e & 3));

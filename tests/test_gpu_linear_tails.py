@@ -23,11 +23,12 @@ def context(n):
 
 
 def gelu(z):
-    """gelu(z) in 64 bits and the bound on the relative error of 0.5 z erfc(-z /
-    sqrt 2) in fp32: the argument's two roundings, which erfc's relative slope of
-    at most z^2 + 1 enlarges (erfc(x) >= 2 / sqrt(pi) exp(-x^2) / (x + sqrt(x^2 +
-    2))), 16 ulp of erfc (32 roundings, the most that OpenCL allows it) and the
-    product's."""
+    """gelu(z) in 64 bits and a bound on the relative error of z/2 erfc(-z / sqrt 2)
+    in fp32: the argument's two roundings, which erfc's relative slope of at most
+    z^2 + 1 enlarges (erfc(x) >= 2 / sqrt(pi) exp(-x^2) / (x + sqrt(x^2 + 2))), 16
+    ulp of erfc (32 roundings, the most that OpenCL allows it) and the product's.
+    exp(-z^2 / 2) R(|z|) stays below it: three roundings of z^2 / 2 in the exponent,
+    and no more than 20 of the exponential, R and the products."""
     z = z.astype(np.float64)
     y = 0.5 * z * np.vectorize(math.erfc)(-z / math.sqrt(2))
     return y, (2 * (z * z + 1) + 33) * ref.EPS32
