@@ -52,7 +52,10 @@ typedef struct c3c_state_cache {
  *   between tokens, below 2^23; head h reads query and key head h / (heads / qk_heads).
  *   log_decay (g): fp32, [heads] with ld_decay 0, or [T][heads] with ld_decay
  *   elements between tokens.  At most 0; -infinity forgets.  A decay is held to
- *   exp(-110), which is 0 in fp32.  Larger ones are taken as they come.
+ *   exp(-110), which is 0 in fp32, and a weight below 2^-126 counts as 0.  Larger
+ *   ones are taken as they come while their sums stay below 87, over any 32 tokens
+ *   in a row and, where a sequence is split, over all of its new ones; beyond that
+ *   results may be infinite or NaN where the recurrence's are finite.
  *   out: [T][heads][dim_v] contiguous.  Rows of no sequence are left alone.
  * A token does not reach the tokens before it, NaN included; what a NaN or an
  * infinity reaches becomes NaN or infinite (an infinity may become a NaN).
@@ -61,12 +64,15 @@ typedef struct c3c_state_cache {
  * cores with operands split into bf16 terms of 8 bits: inputs into as many as
  * hold them exactly (1 for bf16, 2 for f16, 3 for f32); what multiplies them in
  * out into 2 (3 for f32) terms; in the state into 3.  A value beyond 3.38e38, the
- * largest of bf16, counts as infinite.
+ * largest of bf16, counts as infinite; what is below 2^-133, its smallest, is lost
+ * of a term, so values and products of queries and keys below about 2^-108 keep
+ * fewer bits.
  *
  * max_new bounds the new tokens of a sequence; it only plans the work.
  * Workspace (c3c_linear_attention_workspace_bytes): the states between the
  * parts of sequences that are split because heads and sequences are too few for
- * the device; with a smaller one the call runs unsplit.
+ * the device; with a smaller one the call runs unsplit.  It does not grow steadily
+ * with the tokens or the sequences: ask for every size that is used.
  * EINVAL: NULL ctx, states, batch or required tensor; sizes out of range;
  * unknown dtype; qk_heads not dividing heads; heads or B > 65535; a stride too
  * small; scale not finite; an output overlapping an input or another; the

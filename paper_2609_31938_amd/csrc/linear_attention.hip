@@ -20,17 +20,20 @@
 //   layout of an accumulator is that of an operand whose rows are taken in
 //   another order, so S goes into the first product without passing through LDS,
 //   and no two waves share a column of out.  What the waves share is q, k and P,
-//   in LDS.  A clip of 32760 tokens x 32 heads of 128 (bf16) takes 350 us, and its
-//   loads and stores alone 211; two waves a SIMD (of 247 registers) wait for LDS,
-//   products and barriers in turn: without loads and stores it takes 291, without
-//   any one of the products 300 to 350.  Tried, and slower or no faster there: 16
-//   columns a wave with four waves a SIMD (registers in scratch memory, 410),
-//   chunks of 64 tokens (340 to 400; a frame of 1560 tokens 31 us, 23 so), one
-//   term in place of two or three (370), S scaled only where it has to be.
+//   in LDS.  A clip of 32760 tokens x 32 heads of 128 (bf16) takes 304 to 313
+//   us, at the clock that a card keeps over many of them; 350 in the short runs that
+//   the other figures of this paragraph are from.  Its loads and stores alone take
+//   211; two waves a SIMD (of 247 registers) wait for LDS, products and barriers in
+//   turn: without loads and stores it takes 291, without any one of the products 300
+//   to 350.  Tried, and slower or no faster there: 16 columns a wave with four
+//   waves a SIMD (registers in scratch memory, 410), chunks of 64 tokens (340 to
+//   400; a frame of 1560 tokens 31 us, 23 so), one term in place of two or three
+//   (370), S scaled only where it has to be.
 // parts: few heads and sequences leave compute units idle.  Their sequences
 //   are split into parts of whole chunks: one launch forms each part's own
-//   state (160 us there; it reads k and v once more, whose loads alone take 110),
-//   one joins them in order (13 us), one forms the outputs of all parts.
+//   state (143 us there, 160 in the short runs; it reads k and v once more, whose
+//   loads alone take 110 in these), one joins them in order (13 us), one forms the
+//   outputs of all parts.
 // tokens: few new tokens (single ones, drafted ones) take the recurrence as it
 //   stands, S in registers: it is bound by reading and writing S (64 sequences x
 //   32 heads of 128: 268 MB in 42 to 56 us by what the caches hold).
@@ -827,9 +830,16 @@ RecurPlan plan_recur(const c3c_state_cache& st, const c3c_kv_batch& b) {
   if (most <= kFew || b.B < 1) return p;
   const Tile t = tile_of(st.dim_k, st.dim_v);
   const int64_t chunks = up(most, C), units = b.B * st.heads * up(st.dim_v, t.dvs);
-  // As many parts as there is room for at once, of two chunks at least (6 heads
-  // of 80 x 112 in f32, four sequences of up to 701 tokens: 37 us, of four chunks
-  // 51; twice the room: the same).
+  // Two workgroups a compute unit, or four where they have 64 columns; parts of two
+  // chunks at least (6 heads of 80 x 112 in f32, four sequences of up to 701 tokens:
+  // 37 us, of four chunks 51).  By their registers and LDS four (bf16, 64 x 64) to
+  // one (512 threads; f16 and f32 of 256 x 64) of the outputs' workgroups are on a
+  // compute unit at once; the others run in further rounds.  Half as many parts: a
+  // clip of 32 heads of 128 takes 575 us (468 so), those f32 sequences 38.5 (34.3),
+  // a frame for each of two streams 42 (45); but few heads over long sequences are
+  // faster, since the join takes their parts one by one: 4 heads of 16000 tokens
+  // of 128 x 128 69 us (82 so) in bf16 and 91 (116) in f32, of 64 x 64 68 (105), of
+  // 256 x 64 86 (132).
   const int64_t room = device_compute_units() * (t.dvs == 128 ? 2 : 4);
   int64_t parts = room / units;
   if (parts > chunks / 2) parts = chunks / 2;

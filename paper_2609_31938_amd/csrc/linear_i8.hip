@@ -28,7 +28,7 @@
 //   straight into LDS (the buffer's bounds make rows past M or N and pieces
 //   past K zero); rows of any other length are copied to such rows first where
 //   there is workspace for them (linear_pads), else they go through registers
-//   (4096 x 4095, 8192 tokens: 298 us).
+//   (4096 x 4095, 8192 tokens: 292 us).
 #include "token_dev.h"
 #include "tokens_internal.h"
 
@@ -587,8 +587,10 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void linear_tiled(LinAr
     // Onto a residual without an activation (of 16 bits, a whole tile, its tokens
     // under one row of gates): everything is read before anything is stored, since
     // a load is waited for with every store before it, and all workgroups are
-    // here at once (32760 x 5120 x 5120: 905 us, through LDS 1017, without a residual
-    // 790; loads past the caches 926).
+    // here at once (32760 x 5120 x 5120: 900 us, through LDS 1017, without a residual
+    // 790; loads past the caches 926).  The residual's 64 registers beside 128 sums
+    // leave 136 bytes a lane in scratch memory, and a wave's loads take a quarter of
+    // a line at a time: 3.7 GB are read, of which the residual is 0.3.
     const uint32_t group = static_cast<uint32_t>(m0) / a.e.rows_per_gate;
     if (!a.part && a.e.act == C3C_ACT_NONE && a.e.residual && a.y_dtype != C3C_DTYPE_F32 && n0 + BN <= a.N &&
         static_cast<uint32_t>(m0 + mrows - 1) / a.e.rows_per_gate == group) {
@@ -852,8 +854,10 @@ hipError_t launch_linear_i8(int64_t M, int64_t N, int64_t K, const int8_t* x, in
   return e.kind == EPILOGUE ? run_linear<EPILOGUE>(a, s) : e.kind == GATED ? run_linear<GATED>(a, s) : run_linear<PLAIN>(a, s);
 }
 
-// The copy costs its traffic and a launch, and about halves the products: it
-// pays from some hundred tokens on.
+// The copy costs its traffic and a launch, and up to halves the products: it pays
+// from some hundred tokens on where these are large (channels of 4095, 4096 of
+// them: 400 tokens 35 us, through registers 48; 8000 tokens 148, 292), and costs
+// small ones a launch (777 of 333, 400 tokens: 12.4, 9.1).
 bool linear_pads(int64_t M, int64_t K, int64_t ld) { return M > 64 && (K % 16 != 0 || ld % 16 != 0); }
 
 hipError_t launch_pad_rows(const int8_t* src, int64_t rows, int64_t n, int64_t ld, int8_t* dst, int64_t ldd, hipStream_t s) {
