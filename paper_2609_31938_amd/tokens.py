@@ -114,7 +114,7 @@ def _here(t):
     """The device of a call's first tensor.  Refuses one that is not the current
     device: a stream given as 0 is the current device's."""
     device = t.get_device()
-    if device != _device() and t.is_cuda:
+    if (device >= 0 or t.is_cuda) and device != _device():
         raise ValueError(f"the tensors are on device {device}, the current one is {_device()}")
     return device
 

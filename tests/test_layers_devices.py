@@ -101,3 +101,17 @@ def test_linear_attention(ctx, name):
             call(args)
     else:
         refused(name, call, args)
+
+
+@no_gpu
+def test_host_tensors_are_refused_where_there_is_no_device():
+    """As an argument, without asking a device that does not exist."""
+    ctx, x, w, ws = c3c.Context(), torch.zeros(4, 16), torch.zeros(6, 16, dtype=torch.int8), torch.zeros(6)
+    with pytest.raises(ValueError, match="x must be a device tensor"):
+        tokens.gated_linear_i8(ctx, x, w, ws)
+    with pytest.raises(ValueError, match="x must be a device tensor"):
+        tokens.linear_i8(ctx, x, w, ws, act="silu")
+    s = tokens.StateCache.__new__(tokens.StateCache)
+    s.heads, s.dim_k, s.dim_v = 2, 16, 16
+    with pytest.raises(ValueError, match="q must be a device tensor"):
+        tokens.linear_attention(ctx, s, None, *[torch.zeros(3, 2, 16)] * 3, torch.zeros(2))
